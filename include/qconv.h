@@ -495,6 +495,125 @@ int qconv2d_scheduled(const qconv_desc *d, const void *x, const void *w_prepared
                       const qconv_epilogue *epi, void *y, const qconv_schedule *s, void *workspace,
                       size_t workspace_bytes, void *stream);
 
+/*
+ * The linear layer on 8-bit rows.  A layer of a language model multiplies rows
+ * of activations by k x c weights.  Here both are rows of low-bit codes with
+ * one scale for each row, value = code * scale (the packed operands of Sec. 1,
+ * Sec. 2.1's product with a 1x1 window), and the 8-bit rows of the input are
+ * at once the integer product's operand and what the backward pass keeps of it:
+ *   forward           y[m][k]  = sum_c x[m][c] w[k][c]     (+ adapters, below)
+ *   input gradient    dx[m][c] = sum_k dy[m][k] w[k][c]
+ *   weight gradient   dw[k][c] = sum_m dy[m][k] x[m][c]
+ * Conventions as above: device pointers, nothing allocated or kept, work
+ * enqueued on `stream`, arguments checked before anything is enqueued.
+ * Reading a view is allowed throughout (row strides in elements), and no
+ * alignment beyond the element's is asked of x, y, dy, dx and dw; aligned rows
+ * (16 bytes) are read and written in wider accesses.
+ */
+#define QCONV_BF16 0
+#define QCONV_F16 1
+#define QCONV_F32 2
+
+/*
+ * Rows of codes.
+ *   codes     bits 8: int8, one byte a channel.  bits 4 (weights only): the
+ *             packed layout above, signed (qconv_pack of k x c x 1 x 1
+ *             values), channels % 8 == 0.  16-byte aligned.
+ *   pitch     bytes from row to row: a multiple of 16, at least the row's bytes
+ *             rounded up to 16, at most 2^22.  A row's bytes between its
+ *             channels and the next multiple of 16 must be zero in the input's
+ *             rows (qconv_quantize_rows writes them so).
+ *   scale     one float for each row, any value
+ *   rows, channels   channels at most 131071: int32 sums are then exact
+ */
+typedef struct qconv_rows {
+    const void *codes;
+    const float *scale;
+    int64_t pitch;
+    int32_t rows, channels;
+    int32_t bits;
+} qconv_rows;
+
+/*
+ * qconv_quantize_rows -- rows of floating values to 8 bits:
+ *   e = the least integer, at least -126, with max_c |x[m][c]| <= 127 * 2^e
+ *   scale[m] = 2^e;  codes[m][c] = x[m][c] / 2^e to nearest, ties to even
+ * A row of zeros has scale 0.  A row with an infinity or a NaN has scale NaN
+ * and codes 0: all that is computed from it is NaN.  Scales are powers of two
+ * so that the quotient, and later code * scale in 16-bit floats, are exact.
+ *   x       DEVICE, m x c of `dtype` (QCONV_BF16, _F16 or _F32), ldx >= c
+ *           elements from row to row
+ *   codes   DEVICE, 16-byte aligned, m rows of `pitch` bytes (a multiple of 16,
+ *           >= c rounded up to 16); written up to c rounded up to 16
+ *   scale   DEVICE, m floats
+ * m == 0 is a no-op.  Errors: QCONV_EINVAL, QCONV_EUNSUPPORTED, QCONV_EHIP.
+ */
+int qconv_quantize_rows(const void *x, int32_t dtype, int64_t ldx, int32_t m, int32_t c, void *codes, int64_t pitch,
+                        float *scale, void *stream);
+
+/*
+ * Low-rank adapters of many requests over one projection: row m of the input
+ * belongs to adapter a = row[m] and gets
+ *   alpha[a] * sum_r u[m][r] b[a][k][r],   u[m][r] = sum_c x[m][c] a[a][r][c]
+ * added; a row whose adapter lies outside [0, count) (-1, say) gets nothing.
+ * Rows may name adapters in any order.
+ *   a, b    DEVICE, 16-byte aligned, contiguous: count x rank x c and
+ *           count x k x rank values of y's type
+ *   alpha   DEVICE, count floats;  row: DEVICE, int32 for each row of x
+ *   rank    a multiple of 8 up to 128; c % 8 == 0
+ * u is kept in 32 bits between the two products and rounded once to y's type
+ * for the second, relative to its row's largest value.
+ */
+typedef struct qconv_adapters {
+    const void *a, *b;
+    const float *alpha;
+    const int32_t *row;
+    int32_t count, rank;
+} qconv_adapters;
+
+/*
+ * qconv_linear -- y[m][k] = sum_c x[m][c] w[k][c], plus the adapters' part, as
+ * floats of `dtype` (QCONV_BF16 or QCONV_F16), rounded once.
+ *   x   8-bit rows;  w   8-bit or 4-bit rows with the same channels
+ *   adapters  NULL, or as above (count == 0: none)
+ *   y   DEVICE, x->rows x w->rows, ldy >= w->rows elements from row to row; must
+ *       not overlap an input or the workspace
+ *   workspace  DEVICE, 16-byte aligned, qconv_linear_workspace_bytes (0 without
+ *       adapters); its contents need no preparation and mean nothing afterwards.
+ *       Calls that share one must not overlap in time.
+ * Two launches with adapters, one without.  x->rows == 0 is a no-op.
+ * Limits: rows at most 2^22.  Errors: QCONV_EINVAL, QCONV_EUNSUPPORTED,
+ * QCONV_EWORKSPACE, QCONV_EHIP.
+ */
+int qconv_linear_workspace_bytes(int32_t m, int32_t c, const qconv_adapters *adapters, size_t *bytes);
+int qconv_linear(const qconv_rows *x, const qconv_rows *w, const qconv_adapters *adapters, void *y, int32_t dtype,
+                 int64_t ldy, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The backward pass, from the 8-bit (or 4-bit) forms alone.  `dtype` (QCONV_BF16
+ * or QCONV_F16) is the gradients'; products are formed from dy as it is and code
+ * * scale rounded to that type -- exact where the scale is a power of two (f16: and
+ * no more than 2^21 times smaller than the call's largest) -- and summed in 32 bits.
+ *
+ * qconv_linear_grad_input -- dx[m][c] = sum_k dy[m][k] w[k][c], of dy's type.
+ *   dy  DEVICE, m x w->rows, lddy elements from row to row
+ *   dx  DEVICE, m x w->channels, lddx elements from row to row
+ * qconv_linear_grad_weight -- dw[k][c] = sum_m dy[m][k] x[m][c], 32-bit floats.
+ *   dy  DEVICE, x->rows x k;  dw  DEVICE, k x x->channels; x: 8-bit rows.  With
+ *   x->rows == 0, dw is filled with zeros.
+ * qconv_linear_grad_workspace_bytes -- host only: the workspace of a product of
+ *   `rows` x `cols` results summed over `depth` (input gradient: m, w->channels,
+ *   w->rows; weight gradient: k, x->channels, x->rows).  It holds partial sums
+ *   where a long sum is split to fill the chip; they are added in a fixed order,
+ *   so results do not change from call to call.  Other rules as above.
+ * lddy at most 2^21.  Outputs must not overlap inputs or the workspace.
+ */
+int qconv_linear_grad_workspace_bytes(int32_t rows, int32_t cols, int32_t depth, size_t *bytes);
+int qconv_linear_grad_input(const void *dy, int32_t dtype, int64_t lddy, int32_t m, const qconv_rows *w, void *dx,
+                            int64_t lddx, void *workspace, size_t workspace_bytes, void *stream);
+int qconv_linear_grad_weight(const void *dy, int32_t dtype, int64_t lddy, int32_t k, const qconv_rows *x, float *dw,
+                             int64_t lddw, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Number of compiled tile configurations; ids are 0 .. count-1. */
 int qconv_tile_count(void);
 

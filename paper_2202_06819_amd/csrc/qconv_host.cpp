@@ -19,6 +19,7 @@
 
 #include "qconv.h"
 #include "qconv_internal.h"
+#include "qlinear_internal.h"
 
 using namespace qconv;
 
@@ -31,8 +32,24 @@ using namespace qconv;
 __attribute__((used)) static const char kDigestMarker[] = "QCONV_SOURCE_DIGEST=" QCONV_SOURCE_DIGEST;
 
 namespace {
-
 thread_local char g_err[256] = "";
+}
+
+namespace qconv {
+
+int fail(int code, const char *fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_err, sizeof(g_err), fmt, ap);
+    va_end(ap);
+    return code;
+}
+
+void clear_error() { g_err[0] = 0; }
+
+}  // namespace qconv
+
+namespace {
 
 // How a prepared wide layer runs on the direct kernels: wave tile (32-channel
 // pairs, 16-pixel fragments), waves per output tile and tiles per workgroup,
@@ -50,15 +67,6 @@ struct LaunchRecord {
     DirectChoice choice;
 };
 thread_local LaunchRecord g_last_launch;
-
-int fail(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
-int fail(int code, const char *fmt, ...) {
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(g_err, sizeof(g_err), fmt, ap);
-    va_end(ap);
-    return code;
-}
 
 constexpr int64_t kLdsBytes = 160 * 1024;   // LDS per workgroup on gfx950
 constexpr int64_t kUnrollLdsBytes = 64 * 1024;   // LDS the unroll kernel may stage per row
