@@ -113,12 +113,15 @@ __device__ __forceinline__ int range_bytes(int64_t bytes) {
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t range_of(const void *base, int64_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), (short)0, range_bytes(bytes), 0x00020000);
 }
-// The same as plain words, for copy16.
-__device__ __forceinline__ u32x4_t range_words(const void *base, int64_t bytes) {
+// The same as plain words, for copy16 (32-bit sizes: no clamp).
+__device__ __forceinline__ u32x4_t range_words(const void *base, int bytes) {
     const uint64_t b = (uint64_t)base;
     return u32x4_t{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b),
                    (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32)),
-                   (uint32_t)__builtin_amdgcn_readfirstlane(range_bytes(bytes)), 0x00020000u};
+                   (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
+}
+__device__ __forceinline__ u32x4_t range_words(const void *base, int64_t bytes) {
+    return range_words(base, range_bytes(bytes));
 }
 
 // Global memory straight into LDS: lane i's 16 bytes at buffer offset `off`
@@ -133,7 +136,19 @@ __device__ __forceinline__ void copy16(uint8_t *lds, uint32_t off, u32x4_t rsrc)
                  : "s"(m0v), "v"(off), "s"(rsrc)
                  : "memory", "m0");
 }
+// The same of 4 bytes a lane.
+__device__ __forceinline__ void copy4(uint8_t *lds, uint32_t off, u32x4_t rsrc) {
+    const uint32_t m0v = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr_t *)lds);
+    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+                 :
+                 : "s"(m0v), "v"(off), "s"(rsrc)
+                 : "memory", "m0");
+}
 #pragma clang diagnostic pop
+// Waits until at most N of the wave's copies are outstanding (they land in
+// order), and for its LDS reads.
+template <int N>
+__device__ __forceinline__ void copies_left() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // ROWS rows of a step by a workgroup of THREADS: row r's bytes

@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "qconv.h"
 #include "qlinear_internal.h"
 
@@ -109,9 +111,10 @@ size_t adapter_workspace(int64_t m, int64_t c, const qconv_adapters *ad) {
     return (size_t)linear_adapter_splits(m, c) * (size_t)m * (size_t)ad->rank * 4;
 }
 
+// Enough for either plan: a gradient's alignment is not known before the call.
 size_t grad_workspace(int64_t ni, int64_t nj, int64_t nt) {
-    const GradPlan p = plan_grad(ni, nj, nt);
-    return p.splits > 1 ? (size_t)p.splits * (size_t)ni * (size_t)((nj + 3) / 4 * 4) * 4 : 0;
+    const int splits = std::max(plan_grad(ni, nj, nt, false).splits, plan_grad(ni, nj, nt, true).splits);
+    return splits > 1 ? (size_t)splits * (size_t)ni * (size_t)((nj + 3) / 4 * 4) * 4 : 0;
 }
 
 int run_grad(GradArgs &a, bool transposed, int w_bits, int dtype, int64_t out_size, const qconv_rows *b, void *workspace,
@@ -269,7 +272,8 @@ int qconv_linear_grad_weight(const void *dy, int32_t dtype, int64_t lddy, int32_
     a.ni = k;
     a.nj = x->channels;
     a.nt = x->rows;
-    a.vec_p = wide_rows(dy, lddy, 2, 4) && k % 2 == 0;
+    a.vec_p = wide_rows(dy, lddy, 2, 16);
+    a.pair_p = wide_rows(dy, lddy, 2, 4) && k % 2 == 0;
     a.vec_out = wide_rows(dw, lddw, 4, 16);
     return run_grad(a, true, 8, dtype, 4, x, workspace, workspace_bytes, stream);
 }

@@ -60,7 +60,9 @@ struct GradArgs {
     float *part;         // splits x ni x ldpart partial sums (splits > 1)
     int64_t ldpart;
     int32_t ni, nj, nt;
-    int32_t vec_p, vec_out;
+    int32_t vec_p;       // rows of p start on 16-byte boundaries
+    int32_t pair_p;      // ... on 4-byte boundaries, and ni is even
+    int32_t vec_out;     // rows of out start on 16-byte boundaries
     int32_t tiles_i, tiles_j;
     int32_t splits, steps_per_split, steps;
 };
@@ -76,7 +78,11 @@ struct GradPlan {
     int tile;            // 64, 128 or 256
     int splits, steps_per_split, steps;
 };
-GradPlan plan_grad(int64_t ni, int64_t nj, int64_t nt);
+// Whether p's rows are whole 16-byte vectors, so that they can be copied to LDS.
+inline bool whole_vectors(const GradArgs &a, bool transposed) {
+    return a.vec_p && (transposed ? a.ni : a.nt) % 8 == 0;
+}
+GradPlan plan_grad(int64_t ni, int64_t nj, int64_t nt, bool copies);
 
 // Records a failure for qconv_last_error and returns `code`.
 int fail(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
