@@ -59,13 +59,17 @@ struct MmaT {
 //
 // A step of a product stages 128 bytes of each of its rows (128 int8 or 64
 // 16-bit values of the sum's axis): row r's 16-byte vector v lies at
-// r * 128 + 16 * (v ^ slot(r)).  slot() gives eight different places to the
-// rows that eight neighbouring lanes touch in each access here: eight rows in a
-// run (fragments, copies from memory), every fourth row of 32 and every second
-// of 16 (transposing stores), and the rows 16 g + (0..3) of a lane's 16
-// consecutive outputs.  So no access meets itself on a bank.
+// r * 128 + 16 * (v ^ slot(r)).  A 16-byte LDS read serves 16 lanes at once, 0-3,
+// 12-15, 20-23 and 24-27, then 4-11, 16-19 and 28-31, and so on (so the counters of
+// bank conflicts say): parts of two neighbouring vectors of a fragment; a write
+// serves lanes in a run.  slot() is linear over XOR, and keeps each such set that
+// occurs here on banks of its own: rows in a run (fragments), the rows 16 g +
+// (0..3) of a lane's 16 consecutive outputs, and, for transposing stores, every
+// fourth row of 32 and every second of 16.
 constexpr int kStepBytes = 128;
-__host__ __device__ constexpr int slot(int row) { return ((row >> 2) ^ (row << 1) ^ (row >> 4)) & 7; }
+__host__ __device__ constexpr int slot(int row) {
+    return (row & 7) ^ (row & 8 ? 5 : 0) ^ (row & 16 ? 6 : 0);
+}
 
 // Row of fragment f that lane row r (0..15) of the j operand reads, from the
 // wave's first row: the four rows of the product that a lane receives from
