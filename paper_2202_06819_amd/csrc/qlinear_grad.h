@@ -4,13 +4,11 @@
 // output gradient) and its weight gradient (t: the batch's rows, codes: the
 // 8-bit checkpoint of the input, p the output gradient transposed).
 //
-// A step stages 64 values of t in LDS as 16-bit floats, both operands with t
-// innermost.  A thread takes 4 columns of 8 rows of codes (coalesced words),
-// multiplies code by scale in 32 bits, rounds to the 16-bit type and writes four
-// vectors of 8 t: the transposition is free, since every code is converted on
-// its own anyway.  The rounding is exact for scales that are powers of two (as
-// the quantiser gives them); for others it is one rounding of each operand to the
-// gradient's own precision.  Sums are 32-bit.
+// A step stages 64 values of t in LDS, both operands as they lie in memory, and the
+// operand that has t outermost is read by transposing loads.  A code times its scale
+// is formed in 32 bits and rounded to the 16-bit type: exact for scales that are
+// powers of two (as the quantiser gives them); for others it is one rounding of each
+// operand to the gradient's own precision.  Sums are 32-bit.
 #pragma once
 
 #include "qlinear_device.h"
@@ -45,13 +43,7 @@ __device__ __forceinline__ void scale_window(const float *scale, int begin, int 
     }
 }
 
-// How p reaches LDS: rows of t in whole vectors straight from memory (ROWS_COPY),
-// rows of i likewise, transposed when they are read (COLUMNS_COPY), or either
-// through registers, with any alignment and width.
-enum class PForm { ROWS_COPY, ROWS, COLUMNS_COPY, COLUMNS };
-constexpr bool transposed(PForm p) { return p == PForm::COLUMNS_COPY || p == PForm::COLUMNS; }
-
-// COLUMNS_COPY keeps p as it lies in memory, rows of TI values of one t, and a
+// Transposed, p lies in LDS as in memory, rows of TI values of one t, and a
 // fragment is read by transposing loads: 16 lanes read 16 columns of four rows,
 // and each gets its column of all four.  Row t's 32-byte unit u lies at unit
 // u ^ unit_of(t): the rows of one load fall on different banks.
@@ -91,303 +83,15 @@ __device__ __forceinline__ void store4(typename T::elem *out, f32x4 d, int left,
     }
 }
 
-// Codes through registers, converted on their way to LDS: 4-bit codes, and p of
-// any alignment.  Each step multiplies one LDS buffer while the other is filled for
-// the next: copies go out first, the codes that were loaded a step earlier are
-// converted and stored in the shadow of the matrix instructions, and the codes
-// after them are then loaded.
-template <class T, int WB, PForm P, int TJ, int TI, int WJ, int WI>
-__global__ void __launch_bounds__(WJ *WI * 64) grad_regs(GradArgs a) {
-    constexpr int FJ = 4, FI = TI / (16 * WI), kThreads = WJ * WI * 64, kBuffer = (TJ + TI) * kStepBytes;
-    constexpr int kWaves = kThreads / 64;
-    static_assert(TJ == WJ * 64);
-    using elem = typename T::elem;
-    using v8 = typename T::v8;
-    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-    const int tid = (int)threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-    const int tiles = a.tiles_i * a.tiles_j;
-    const int split = (int)blockIdx.x / tiles;
-    int ti, tj;
-    tile_at(xcd_run((int)blockIdx.x - split * tiles, tiles), a.tiles_i, a.tiles_j, ti, tj);
-    const int i0 = ti * TI, j0 = tj * TJ;
-    const int s0 = split * a.steps_per_split, s1 = min(s0 + a.steps_per_split, a.steps);
-    const elem *p = static_cast<const elem *>(a.p);
-    float to, from;
-    scale_window<T, kThreads>(a.b.scale, s0 * 64, min(s1 * 64, a.nt), reinterpret_cast<uint32_t *>(smem), to, from);
-
-    // codes: a unit is 4 columns (one word, or half a word of 4-bit codes) of 8
-    // rows; a wave of the widest tile takes one group of 8 rows, whose scales are
-    // then scalars
-    constexpr int kGroups = TJ / 4, kUnits = (kGroups * 8 + kThreads - 1) / kThreads;
-    constexpr bool kScalarScale = kGroups == 64 && kUnits == 1;
-    // p in registers, transposed: a unit is 2 columns of 8 rows; in rows: one vector
-    constexpr int kPUnits = P == PForm::COLUMNS ? TI / 2 * 8 / kThreads : P == PForm::ROWS ? TI * 8 / kThreads : 1;
-    uint32_t cw[kUnits][8];
-    float cs[kScalarScale ? 1 : kUnits][8];
-    uint32_t pw[kPUnits][8];
-    const u32x4_t rp_rows = P == PForm::ROWS_COPY
-                                ? range_words(p + (int64_t)i0 * a.ldp, ((int64_t)(a.ni - 1 - i0) * a.ldp + a.nt) * 2)
-                                : u32x4_t{0, 0, 0, 0};
-
-    auto copy_p = [&](int s, uint8_t *buf) {
-        uint8_t *pb = buf + TJ * kStepBytes;
-        if constexpr (P == PForm::ROWS_COPY) {
-            copy_rows<TI, kThreads>(pb, rp_rows, (uint32_t)a.ldp * 2u, s * 128, a.nt * 2, wave, lane);
-        } else if constexpr (P == PForm::COLUMNS_COPY) {
-            const int t0 = s * 64;
-            const u32x4_t rp = range_words(p + (int64_t)t0 * a.ldp + i0, ((int64_t)(a.nt - 1 - t0) * a.ldp + a.ni - i0) * 2);
-            constexpr int kRow = TI * 2;
-#pragma unroll
-            for (int n = 0; n < 64 * kRow / (1024 * kWaves); ++n) {
-                const int at = (n * kWaves + wave) * 1024 + lane * 16, t = at / kRow, in = at % kRow;
-                const int col = ((in >> 5) ^ unit_of<TI>(t)) * 32 + (in & 16);
-                copy16(pb + (n * kWaves + wave) * 1024,
-                       col < (a.ni - i0) * 2 ? (uint32_t)t * (uint32_t)a.ldp * 2u + (uint32_t)col : kNowhere, rp);
-            }
-        }
-    };
-    auto load = [&](int s) {
-        const int t0 = s * 64;
-        const __amdgpu_buffer_rsrc_t rc = range_of(a.b.codes + (int64_t)t0 * a.b.pitch,
-                                                   (int64_t)(a.nt - 1 - t0) * a.b.pitch + a.b.used);
-        const __amdgpu_buffer_rsrc_t rs = range_of(a.b.scale + t0, (int64_t)(a.nt - t0) * 4);
-#pragma unroll
-        for (int n = 0; n < kUnits; ++n) {
-            const int unit = n * kThreads + tid, jg = unit % kGroups, tc = unit / kGroups;
-            const int at = WB == 8 ? j0 + jg * 4 : (j0 + jg * 4) / 2;
-            const bool in = tc < 8 && at < a.b.used;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int t = tc * 8 + e;
-                const int off = (int)(in ? (uint32_t)t * (uint32_t)a.b.pitch + (uint32_t)at : kNowhere);
-                if constexpr (WB == 8)
-                    cw[n][e] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rc, off, 0, 0);
-                else
-                    cw[n][e] = (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rc, off, 0, 0);
-                if constexpr (!kScalarScale)
-                    cs[n][e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, tc < 8 ? t * 4 : (int)kNowhere, 0, 0));
-            }
-        }
-        if constexpr (P == PForm::ROWS) {
-            const __amdgpu_buffer_rsrc_t rp = range_of(p + (int64_t)i0 * a.ldp, ((int64_t)(a.ni - 1 - i0) * a.ldp + a.nt) * 2);
-#pragma unroll
-            for (int n = 0; n < kPUnits; ++n) {
-                const int unit = n * kThreads + tid, row = unit >> 3, t = t0 + (unit & 7) * 8;
-                const uint32_t off = (uint32_t)row * (uint32_t)a.ldp * 2u + (uint32_t)t * 2u;
-                if (a.vec_p && t0 + 64 <= a.nt) {
-                    const auto v = __builtin_amdgcn_raw_buffer_load_b128(rp, (int)off, 0, 0);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) pw[n][e] = v[e];
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t lo = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(
-                            rp, (int)(t + 2 * e < a.nt ? off + 4 * e : kNowhere), 0, 0);
-                        const uint32_t hi = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(
-                            rp, (int)(t + 2 * e + 1 < a.nt ? off + 4 * e + 2 : kNowhere), 0, 0);
-                        pw[n][e] = lo | hi << 16;
-                    }
-                }
-            }
-        } else if constexpr (P == PForm::COLUMNS) {
-            const __amdgpu_buffer_rsrc_t rp = range_of(p + (int64_t)t0 * a.ldp + i0, ((int64_t)(a.nt - 1 - t0) * a.ldp + a.ni - i0) * 2);
-#pragma unroll
-            for (int n = 0; n < kPUnits; ++n) {
-                const int unit = n * kThreads + tid, i = unit % (TI / 2) * 2, tc = unit / (TI / 2);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t off = (uint32_t)(tc * 8 + e) * (uint32_t)a.ldp * 2u + (uint32_t)i * 2u;
-                    // rows past the last are past the range; columns past the last reach
-                    // only results that are not stored
-                    if (a.pair_p) {
-                        pw[n][e] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rp, (int)(i0 + i < a.ni ? off : kNowhere), 0, 0);
-                    } else {
-                        const uint32_t lo = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(
-                            rp, (int)(i0 + i < a.ni ? off : kNowhere), 0, 0);
-                        const uint32_t hi = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(
-                            rp, (int)(i0 + i + 1 < a.ni ? off + 2 : kNowhere), 0, 0);
-                        pw[n][e] = lo | hi << 16;
-                    }
-                }
-            }
-        }
-    };
-    // What load() brought of step s, into a buffer.
-    auto store = [&](int s, uint8_t *buf) {
-        float ss[8];
-        if constexpr (kScalarScale) {
-            const int t = s * 64 + wave * 8;
-            const __attribute__((address_space(4))) float *sc = (const __attribute__((address_space(4))) float *)(a.b.scale);
-            if (t + 8 <= a.nt) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) ss[e] = sc[t + e];
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) ss[e] = t + e < a.nt ? sc[t + e] : 0.0f;
-            }
-        }
-#pragma unroll
-        for (int n = 0; n < kUnits; ++n) {
-            const int unit = n * kThreads + tid, jg = unit % kGroups, tc = unit / kGroups;
-            if (kGroups * 8 % kThreads != 0 && tc >= 8) continue;
-            u32x4_t v[4];
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                float f[2][4];
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const uint32_t w = cw[n][2 * h + b];
-                    const float sc = (kScalarScale ? ss[2 * h + b] : cs[n][2 * h + b]) * to;
-                    if constexpr (WB == 8) {
-                        const uint32_t x = w ^ 0x80808080u;   // code + 128
-                        const float off = -128.0f * sc;
-                        f[b][0] = __builtin_fmaf((float)(x & 255u), sc, off);
-                        f[b][1] = __builtin_fmaf((float)((x >> 8) & 255u), sc, off);
-                        f[b][2] = __builtin_fmaf((float)((x >> 16) & 255u), sc, off);
-                        f[b][3] = __builtin_fmaf((float)(x >> 24), sc, off);
-                    } else {
-                        const uint32_t x = w ^ 0x8888u;       // code + 8
-                        const float off = -8.0f * sc;
-#pragma unroll
-                        for (int c = 0; c < 4; ++c)
-                            f[b][c] = __builtin_fmaf((float)((x >> (4 * c)) & 15u), sc, off);
-                    }
-                }
-#pragma unroll
-                for (int c = 0; c < 4; ++c) v[c][h] = pack2<T>(f[0][c], f[1][c]);
-            }
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const int row = jg * 4 + c;
-                *reinterpret_cast<u32x4_t *>(buf + row * kStepBytes + ((tc ^ slot(row)) << 4)) = v[c];
-            }
-        }
-        uint8_t *pb = buf + TJ * kStepBytes;
-        if constexpr (P == PForm::ROWS) {
-#pragma unroll
-            for (int n = 0; n < kPUnits; ++n) {
-                const int unit = n * kThreads + tid, row = unit >> 3, tc = unit & 7;
-                *reinterpret_cast<u32x4_t *>(pb + row * kStepBytes + ((tc ^ slot(row)) << 4)) =
-                    u32x4_t{pw[n][0], pw[n][1], pw[n][2], pw[n][3]};
-            }
-        } else if constexpr (P == PForm::COLUMNS) {
-#pragma unroll
-            for (int n = 0; n < kPUnits; ++n) {
-                const int unit = n * kThreads + tid, row = unit % (TI / 2) * 2, tc = unit / (TI / 2);
-                u32x4_t even, odd;
-#pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    even[h] = __builtin_amdgcn_perm(pw[n][2 * h + 1], pw[n][2 * h], 0x05040100u);
-                    odd[h] = __builtin_amdgcn_perm(pw[n][2 * h + 1], pw[n][2 * h], 0x07060302u);
-                }
-                *reinterpret_cast<u32x4_t *>(pb + row * kStepBytes + ((tc ^ slot(row)) << 4)) = even;
-                *reinterpret_cast<u32x4_t *>(pb + (row + 1) * kStepBytes + ((tc ^ slot(row + 1)) << 4)) = odd;
-            }
-        }
-    };
-
-    const int jrow0 = (wave / WI) * 64, irow0 = (wave % WI) * FI * 16;
-    const int r = lane & 15, g = lane >> 4;
-    f32x4 acc[FJ][FI];
-#pragma unroll
-    for (int j = 0; j < FJ; ++j)
-#pragma unroll
-        for (int i = 0; i < FI; ++i) acc[j][i] = f32x4{0, 0, 0, 0};
-    // half a step: the 32 values of t of half ks
-    auto multiply = [&](const uint8_t *buf, int ks) {
-        const uint8_t *lj = buf, *li = buf + TJ * kStepBytes;
-        v8 x[FJ], y[FI];
-#pragma unroll
-        for (int f = 0; f < FJ; ++f) {
-            const int row = jrow0 + j_row(f, r);
-            x[f] = *reinterpret_cast<const v8 *>(lj + row * kStepBytes + (((ks * 4 + g) ^ slot(row)) << 4));
-        }
-#pragma unroll
-        for (int f = 0; f < FI; ++f) {
-            if constexpr (P == PForm::COLUMNS_COPY) {
-                const int t = ks * 32 + g * 8 + (r >> 2);
-                y[f] = read_transposed<T>(li + t * (TI * 2) + ((((irow0 >> 4) + f) ^ unit_of<TI>(t)) << 5) + (r & 3) * 8, TI * 2);
-            } else {
-                const int row = irow0 + f * 16 + r;
-                y[f] = *reinterpret_cast<const v8 *>(li + row * kStepBytes + (((ks * 4 + g) ^ slot(row)) << 4));
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < FI; ++i)
-#pragma unroll
-            for (int j = 0; j < FJ; ++j) acc[j][i] = T::mma(x[j], y[i], acc[j][i]);
-    };
-    load(s0);
-    copy_p(s0, smem);
-    store(s0, smem);
-    load(s0 + 1);
-    copies_done();
-    __syncthreads();
-    int buf = 0;
-    for (int s = s0; s < s1; ++s) {
-        uint8_t *cur = smem + buf * kBuffer, *next = smem + (buf ^ 1) * kBuffer;
-        // (past the last step these bring zeros, or another split's values, to a
-        // buffer that is not read)
-        copy_p(s + 1, next);
-        multiply(cur, 0);
-        store(s + 1, next);
-        load(s + 2);
-        multiply(cur, 1);
-        copies_done();
-        __syncthreads();
-        buf ^= 1;
-    }
-    const int col = j0 + jrow0 + g * 16;
-#pragma unroll
-    for (int i = 0; i < FI; ++i) {
-        const int row = i0 + irow0 + i * 16 + r;
-        if (row >= a.ni || col >= a.nj) continue;
-        f32x4 d[FJ];
-#pragma unroll
-        for (int j = 0; j < FJ; ++j) d[j] = acc[j][i] * from;
-        if (a.splits > 1) {
-            float *out = a.part + ((int64_t)split * a.ni + row) * a.ldpart + col;
-#pragma unroll
-            for (int j = 0; j < FJ; ++j)
-                if (col + 4 * j < a.ldpart) *reinterpret_cast<f32x4 *>(out + 4 * j) = d[j];
-        } else if constexpr (transposed(P)) {
-            float *out = static_cast<float *>(a.out) + (int64_t)row * a.ldo + col;
-#pragma unroll
-            for (int j = 0; j < FJ; ++j) {
-                if (a.vec_out && col + 4 * j + 4 <= a.nj) {
-                    *reinterpret_cast<f32x4 *>(out + 4 * j) = d[j];
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (col + 4 * j + e < a.nj) out[4 * j + e] = d[j][e];
-                }
-            }
-        } else {
-            elem *out = static_cast<elem *>(a.out) + (int64_t)row * a.ldo + col;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const f32x4 lo = d[2 * h], hi = d[2 * h + 1];
-                if (a.vec_out && col + 8 * h + 8 <= a.nj) {
-                    *reinterpret_cast<uint4 *>(out + 8 * h) = uint4{pack2<T>(lo[0], lo[1]), pack2<T>(lo[2], lo[3]),
-                                                                    pack2<T>(hi[0], hi[1]), pack2<T>(hi[2], hi[3])};
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (col + 8 * h + e < a.nj) out[8 * h + e] = (elem)(e < 4 ? lo[e & 3] : hi[e & 3]);
-                }
-            }
-        }
-    }
-}
-
-// Everything by copies: 8-bit codes and p both lie in LDS as they lie in memory
-// (three buffers of 64 rows of t: one multiplied, one landed, one on its way), and
-// codes are read by transposing loads, 8 rows of one column a lane, and converted
-// on their way to the matrix cores.  A matrix instruction of 16 cycles hides two
-// vector instructions of a wave (measured: three cost a quarter more, four half),
-// so a wave of the widest tile takes 32 columns of codes by all 256 of p and no
-// code is converted twice; that reads p from LDS eight times over, which LDS can
-// give.
+// Three LDS buffers of 64 rows of t: one is multiplied, one has landed, one is on its
+// way.  8-bit codes, and p where its rows are whole aligned vectors (COPY), go straight
+// from memory to LDS; 4-bit codes (widened to bytes) and any other p go through
+// registers a step ahead.  Codes are read by transposing loads, 8 rows of one column a
+// lane, and converted on their way to the matrix cores.  A matrix instruction of 16
+// cycles hides two vector instructions of a wave (measured: three cost a quarter more,
+// four half), so a wave of the widest tile takes 32 columns of codes by all 256 of p
+// and no code is converted twice; that reads p from LDS eight times over, which LDS
+// can give.
 template <int TJ>
 __device__ __forceinline__ int code_unit_of(int t) {
     return TJ == 256 ? t & 15 : TJ == 128 ? (t >> 1) & 7 : (t >> 2) & 3;
@@ -401,12 +105,12 @@ __device__ __forceinline__ uint32_t scaled_pair(uint32_t w, int half, float s0, 
     return pack2<T>((float)(int8_t)(w >> (16 * half)) * s0, (float)(int8_t)(w >> (16 * half + 8)) * s1);
 }
 
-template <class T, PForm P, int TJ, int TI, int WJ, int WI>
+template <class T, int WB, bool TRANSPOSED, bool COPY, int TJ, int TI, int WJ, int WI>
 __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
-    static_assert(P == PForm::ROWS_COPY || P == PForm::COLUMNS_COPY);
     constexpr int FJ = TJ / (16 * WJ), FI = TI / (16 * WI), kThreads = WJ * WI * 64, kWaves = kThreads / 64;
     constexpr int kCodes = 64 * TJ, kP = TI * 128, kStage = kCodes + kP + 256;
-    constexpr int kCodeCopies = kCodes / (1024 * kWaves), kPCopies = kP / (1024 * kWaves);
+    constexpr int kCodeCopies = WB == 8 ? kCodes / (1024 * kWaves) : 0, kPCopies = COPY ? kP / (1024 * kWaves) : 0;
+    constexpr int kCodeUnits = WB == 4 ? kCodes / (16 * kThreads) : 0, kPUnits = COPY ? 0 : kP / (16 * kThreads);
     constexpr int kCopies = kCodeCopies + kPCopies + 1;   // a wave's copies of a step
     using elem = typename T::elem;
     using v8 = typename T::v8;
@@ -421,6 +125,7 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
     const elem *p = static_cast<const elem *>(a.p);
     float to, from;
     scale_window<T, kThreads>(a.b.scale, s0 * 64, min(s1 * 64, a.nt), reinterpret_cast<uint32_t *>(smem), to, from);
+    if constexpr (WB == 4) to *= 0.0625f;
 
     const u32x4_t rp_rows = range_words(p + (int64_t)i0 * a.ldp, ((int64_t)(a.ni - 1 - i0) * a.ldp + a.nt) * 2);
     // copy n of step s: the codes', p's, then the scales (every wave copies the same
@@ -433,7 +138,7 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
         Step q;
         q.codes = range_words(a.b.codes + (int64_t)t0 * a.b.pitch + j0,
                               rows > 0 ? (rows - 1) * (int)a.b.pitch + a.b.used - j0 : 0);
-        q.p = P == PForm::ROWS_COPY ? rp_rows
+        q.p = !TRANSPOSED ? rp_rows
                                     : range_words(p + (int64_t)t0 * a.ldp + i0,
                                                   rows > 0 ? ((rows - 1) * (int)a.ldp + a.ni - i0) * 2 : 0);
         q.scale = range_words(a.b.scale + t0, rows > 0 ? rows * 4 : 0);
@@ -448,7 +153,7 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
         } else if (n < kCodeCopies + kPCopies) {
             const int at0 = ((n - kCodeCopies) * kWaves + wave) * 1024;
             uint32_t off;
-            if constexpr (P == PForm::ROWS_COPY) {
+            if constexpr (!TRANSPOSED) {
                 const int row = (at0 >> 7) + (lane >> 3), at = s * 128 + (((lane & 7) ^ slot(row)) << 4);
                 off = at < a.nt * 2 ? (uint32_t)row * (uint32_t)a.ldp * 2u + (uint32_t)at : kNowhere;
             } else {
@@ -462,6 +167,88 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
         }
     };
 
+    // What goes through registers: units of 16 bytes of LDS, each from one load (p's of
+    // any alignment).  A unit past the matrix is loaded from within it and put right
+    // when it is stored, so that the loads of a step are always as many.
+    constexpr int kFetches = kCodeUnits + kPUnits;
+    uint2 code_unit[kCodeUnits ? kCodeUnits : 1];
+    u32x4_t p_unit[kPUnits ? kPUnits : 1];
+    const int p_rows = TRANSPOSED ? a.nt : a.ni, p_count = TRANSPOSED ? a.ni : a.nt;   // p as it lies in memory
+    const bool narrow = !COPY && p_count < 8;   // rows shorter than a load: by elements
+    auto p_place = [&](int s, int n, int &row, int &at) {
+        const int unit = n * kThreads + tid;
+        row = TRANSPOSED ? s * 64 + unit / (TI / 8) : i0 + unit / 8;
+        at = TRANSPOSED ? i0 + unit % (TI / 8) * 8 : s * 64 + unit % 8 * 8;
+    };
+    auto fetch = [&](int s) {
+        if constexpr (WB == 4) {
+#pragma unroll
+            for (int n = 0; n < kCodeUnits; ++n) {
+                const int unit = n * kThreads + tid, t = min(s * 64 + unit / (TJ / 16), a.nt - 1);
+                const int at = min((j0 + unit % (TJ / 16) * 16) / 2, a.b.used - 8);
+                code_unit[n] = *reinterpret_cast<const uint2 *>(a.b.codes + (int64_t)t * a.b.pitch + at);
+            }
+        }
+        if constexpr (!COPY) {
+#pragma unroll
+            for (int n = 0; n < kPUnits; ++n) {
+                int row, at;
+                p_place(s, n, row, at);
+                const elem *line = p + (int64_t)min(row, p_rows - 1) * a.ldp;
+                if (narrow) {
+                    u32x4_t v{0, 0, 0, 0};
+#pragma unroll
+                    for (int e = 0; e < 7; ++e)
+                        if (at == 0 && e < p_count)
+                            v[e >> 1] |= (uint32_t)__builtin_bit_cast(uint16_t, line[e]) << (16 * (e & 1));
+                    p_unit[n] = v;
+                } else {
+                    __builtin_memcpy(&p_unit[n], line + min(at, p_count - 8), 16);
+                }
+            }
+        }
+    };
+    auto put = [&](int s, uint8_t *buf) {
+        if constexpr (WB == 4) {
+#pragma unroll
+            for (int n = 0; n < kCodeUnits; ++n) {
+                const int unit = n * kThreads + tid, t = unit / (TJ / 16), u = unit % (TJ / 16);
+                const bool in = s * 64 + t < a.nt && j0 + u * 16 < a.b.used * 2;
+                const uint2 lo = widen8(in ? code_unit[n].x : 0u), hi = widen8(in ? code_unit[n].y : 0u);
+                *reinterpret_cast<uint4 *>(buf + t * TJ + ((u ^ code_unit_of<TJ>(t)) << 4)) = uint4{lo.x, lo.y, hi.x, hi.y};
+            }
+        }
+        if constexpr (!COPY) {
+#pragma unroll
+            for (int n = 0; n < kPUnits; ++n) {
+                const int unit = n * kThreads + tid;
+                int row, at;
+                p_place(s, n, row, at);
+                u32x4_t v = p_unit[n];
+                if (row >= p_rows) {
+                    v = u32x4_t{0, 0, 0, 0};
+                } else if (!narrow && at + 8 > p_count) {
+                    const int past = at + 8 - p_count;   // loaded so many elements too early
+                    v = past < 8 ? __builtin_bit_cast(u32x4_t, __builtin_bit_cast(unsigned __int128, v) >> (16 * past))
+                                 : u32x4_t{0, 0, 0, 0};
+                }
+                int to_lds;
+                if constexpr (TRANSPOSED) {
+                    const int t = unit / (TI / 8), u = unit % (TI / 8);
+                    to_lds = t * (TI * 2) + (((u >> 1) ^ unit_of<TI>(t)) << 5) + (u & 1) * 16;
+                } else {
+                    to_lds = unit / 8 * kStepBytes + ((unit % 8 ^ slot(unit / 8)) << 4);
+                }
+                *reinterpret_cast<u32x4_t *>(buf + kCodes + to_lds) = v;
+            }
+        }
+    };
+    // waits for all copies, not for the fetches issued after them
+    auto copies_landed = [&] {
+        if (kFetches > 0 && !narrow) copies_left<kFetches>();
+        else copies_left<0>();
+    };
+
     const int jrow0 = (wave / WI) * 16 * FJ, irow0 = (wave % WI) * FI * 16;
     const int r = lane & 15, g = lane >> 4;
     f32x4 acc[FJ][FI];
@@ -473,7 +260,7 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
     // as they lie in LDS.
     auto read_p = [&](const uint8_t *buf, int ks, int f) {
         const uint8_t *li = buf + kCodes;
-        if constexpr (P == PForm::COLUMNS_COPY) {
+        if constexpr (TRANSPOSED) {
             const int t = ks * 32 + g * 8 + (r >> 2);
             return read_transposed<T>(
                 li + t * (TI * 2) + ((((irow0 >> 4) + f) ^ unit_of<TI>(t)) << 5) + (r & 3) * 8, TI * 2);
@@ -539,7 +326,16 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
     for (int n = 0; n < kCopies; ++n) copy(n, s0, step_of(s0), smem);
 #pragma unroll
     for (int n = 0; n < kCopies; ++n) copy(n, s0 + 1, step_of(s0 + 1), smem + kStage);
-    copies_left<kCopies>();
+    if constexpr (kFetches > 0) {
+        fetch(s0);
+        put(s0, smem);
+        fetch(s0 + 1);
+        put(s0 + 1, smem + kStage);
+        fetch(s0 + 2);
+        copies_landed();
+    } else {
+        copies_left<kCopies>();
+    }
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     u32x4_t x[FJ];
@@ -562,7 +358,7 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
         half(cur, 0, cur, x, ahead, [](int) {});
         // the next step's copies have landed, and everyone is done with the step
         // before this one
-        copies_left<0>();
+        copies_landed();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         // (past the last step these go to a buffer that is not multiplied)
@@ -570,6 +366,8 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
         half(cur, 1, then, x, ahead, [&](int i) {
 #pragma unroll
             for (int n = i * kCopies / FI; n < (i + 1) * kCopies / FI; ++n) copy(n, s + 2, q, third);
+            if (i == 0) put(s + 2, third);
+            if (i == FI - 1) fetch(s + 3);
         });
         at = after;
     }
@@ -585,7 +383,7 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
             if (a.splits > 1) {
                 if (col < a.ldpart)
                     *reinterpret_cast<f32x4 *>(a.part + ((int64_t)split * a.ni + row) * a.ldpart + col) = d;
-            } else if constexpr (transposed(P)) {
+            } else if constexpr (TRANSPOSED) {
                 store4(static_cast<float *>(a.out) + (int64_t)row * a.ldo + col, d, a.nj - col, a.vec_out);
             } else {
                 store4<T>(static_cast<elem *>(a.out) + (int64_t)row * a.ldo + col, d, a.nj - col, a.vec_out);

@@ -14,20 +14,15 @@ hipError_t tile(const GradArgs &a, hipStream_t stream) {
     return hipGetLastError();
 }
 
-// Copies only: three steps in LDS.
-constexpr int copy_lds(int size) { return 3 * (size * 64 + size * 128 + 256); }
-template <class T, PForm P>
-hipError_t copied(const GradArgs &a, int size, hipStream_t stream) {
-    if (size == 256) return tile<grad_tile<T, P, 256, 256, 8, 1>, copy_lds(256), 512>(a, stream);
-    if (size == 128) return tile<grad_tile<T, P, 128, 128, 4, 1>, copy_lds(128), 256>(a, stream);
-    return tile<grad_tile<T, P, 64, 64, 2, 2>, copy_lds(64), 256>(a, stream);
-}
-
-// Through registers: two steps in LDS, and no tile of 256, which they would not hold.
-template <class T, int WB, PForm P>
-hipError_t held(const GradArgs &a, int size, hipStream_t stream) {
-    if (size == 128) return tile<grad_regs<T, WB, P, 128, 128, 2, 2>, 4 * 128 * kStepBytes, 256>(a, stream);
-    return tile<grad_regs<T, WB, P, 64, 64, 1, 4>, 4 * 64 * kStepBytes, 256>(a, stream);
+// Three steps in LDS: codes, p, scales.
+constexpr int lds_bytes(int size) { return 3 * (size * 64 + size * 128 + 256); }
+template <class T, int WB, bool TRANSPOSED, bool COPY>
+hipError_t product(const GradArgs &a, int size, hipStream_t stream) {
+    // (p through registers would not leave the largest tile enough of them)
+    if constexpr (COPY)
+        if (size == 256) return tile<grad_tile<T, WB, TRANSPOSED, COPY, 256, 256, 8, 1>, lds_bytes(256), 512>(a, stream);
+    if (size == 128) return tile<grad_tile<T, WB, TRANSPOSED, COPY, 128, 128, 4, 1>, lds_bytes(128), 256>(a, stream);
+    return tile<grad_tile<T, WB, TRANSPOSED, COPY, 64, 64, 2, 2>, lds_bytes(64), 256>(a, stream);
 }
 
 template <class Out>
@@ -41,7 +36,8 @@ hipError_t sum(const GradArgs &a, hipStream_t stream) {
 
 template <class T>
 hipError_t grad(GradArgs a, bool transposed, int w_bits, hipStream_t stream) {
-    const bool copies = w_bits == 8 && whole_vectors(a, transposed);
+    // (of no rows nothing is read, and copies then read nothing)
+    const bool copies = a.nt == 0 || whole_vectors(a, transposed);
     const GradPlan plan = plan_grad(a.ni, a.nj, a.nt, copies);
     a.tiles_i = (a.ni + plan.tile - 1) / plan.tile;
     a.tiles_j = (a.nj + plan.tile - 1) / plan.tile;
@@ -49,37 +45,53 @@ hipError_t grad(GradArgs a, bool transposed, int w_bits, hipStream_t stream) {
     a.steps = plan.steps;
     a.steps_per_split = plan.steps_per_split;
     hipError_t e;
-    if (copies)
-        e = transposed ? copied<T, PForm::COLUMNS_COPY>(a, plan.tile, stream) : copied<T, PForm::ROWS_COPY>(a, plan.tile, stream);
-    else if (transposed)
-        e = held<T, 8, PForm::COLUMNS>(a, plan.tile, stream);
+    if (transposed)
+        e = copies ? product<T, 8, true, true>(a, plan.tile, stream) : product<T, 8, true, false>(a, plan.tile, stream);
     else if (w_bits == 8)
-        e = held<T, 8, PForm::ROWS>(a, plan.tile, stream);
-    else if (whole_vectors(a, false))
-        e = held<T, 4, PForm::ROWS_COPY>(a, plan.tile, stream);
+        e = copies ? product<T, 8, false, true>(a, plan.tile, stream) : product<T, 8, false, false>(a, plan.tile, stream);
     else
-        e = held<T, 4, PForm::ROWS>(a, plan.tile, stream);
+        e = copies ? product<T, 4, false, true>(a, plan.tile, stream) : product<T, 4, false, false>(a, plan.tile, stream);
     if (e != hipSuccess || a.splits == 1) return e;
     return transposed ? sum<float>(a, stream) : sum<typename T::elem>(a, stream);
 }
 
 }  // namespace
 
+// The tile and the split that a model of the kernels' times (us) finds fastest.  The
+// constants are measured: a step of 64 of the summed axis takes 1.35 in a tile of
+// 256 (one workgroup fits a CU), 0.85 alone and 1.2 for two on a CU in one of 128, 0.52
+// to 1.15 for one to four in one of 64; a split adds a launch and its partial sums'
+// way through memory.  E.g. 1024 x 1024 from 32768 rows: 80 us in 16 tiles of 256 split
+// 16 ways, 105 in 64 of 128 split 8 ways, 282 in 256 of 64; 1024 x 1024 from 1024: 12 in
+// tiles of 64, 20 in 128, 27 in 256.  With p through registers there is no tile of 256.
 GradPlan plan_grad(int64_t ni, int64_t nj, int64_t nt, bool copies) {
-    GradPlan p{64, 1, 0, 0};
-    p.steps = (int)((nt + 63) / 64);
-    auto tiles = [&](int64_t t) { return ((ni + t - 1) / t) * ((nj + t - 1) / t); };
-    if (copies && tiles(256) >= 192) p.tile = 256;
-    else if (tiles(128) * (p.steps / 4 + 1) >= 192) p.tile = 128;
-    // split the sum until the chip is full, eight steps a split at least
-    int64_t splits = (256 + tiles(p.tile) - 1) / tiles(p.tile);
-    if (p.tile == 256) splits = 1;
-    if (splits > (p.steps + 7) / 8) splits = (p.steps + 7) / 8;
-    if (splits > 32) splits = 32;
-    if (splits < 1) splits = 1;
-    p.steps_per_split = (int)((p.steps + splits - 1) / splits);
-    p.splits = p.steps_per_split ? (p.steps + p.steps_per_split - 1) / p.steps_per_split : 1;
-    return p;
+    static const struct {
+        int tile, resident;
+        double start, step[4];   // step[n]: n + 1 workgroups on a CU
+    } kKinds[] = {{256, 1, 10, {1.35}}, {128, 2, 7, {0.85, 1.2}}, {64, 4, 6, {0.52, 0.7, 0.92, 1.15}}};
+    GradPlan best{64, 1, 0, (int)((nt + 63) / 64)};
+    double best_us = 0;
+    const int64_t steps = best.steps;
+    for (const auto &k : kKinds) {
+        if (k.tile == 256 && !copies) continue;
+        const int64_t tiles = ((ni + k.tile - 1) / k.tile) * ((nj + k.tile - 1) / k.tile);
+        for (int64_t want = 1; want <= 32; want *= 2) {
+            const int64_t per = (steps + want - 1) / want, splits = per ? (steps + per - 1) / per : 1;
+            if (want > 1 && (splits < want || splits * tiles > 4096)) break;
+            const int64_t on_cu = (splits * tiles + 255) / 256;
+            const int64_t rest = on_cu % k.resident;
+            const double step = (on_cu / k.resident) * k.step[k.resident - 1] + (rest ? k.step[rest - 1] : 0.0);
+            double us = k.start + per * step;
+            if (splits > 1) us += 2.5 + 8e-6 * splits * ni * nj / 5.0;
+            if (best_us == 0 || us < best_us) {
+                best_us = us;
+                best.tile = k.tile;
+                best.splits = (int)splits;
+                best.steps_per_split = (int)per;
+            }
+        }
+    }
+    return best;
 }
 
 hipError_t launch_grad(const GradArgs &a, bool transposed, int w_bits, int dtype, hipStream_t stream) {

@@ -273,7 +273,6 @@ int qconv_linear_grad_weight(const void *dy, int32_t dtype, int64_t lddy, int32_
     a.nj = x->channels;
     a.nt = x->rows;
     a.vec_p = wide_rows(dy, lddy, 2, 16);
-    a.pair_p = wide_rows(dy, lddy, 2, 4) && k % 2 == 0;
     a.vec_out = wide_rows(dw, lddw, 4, 16);
     return run_grad(a, true, 8, dtype, 4, x, workspace, workspace_bytes, stream);
 }

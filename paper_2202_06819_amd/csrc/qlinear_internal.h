@@ -61,7 +61,6 @@ struct GradArgs {
     int64_t ldpart;
     int32_t ni, nj, nt;
     int32_t vec_p;       // rows of p start on 16-byte boundaries
-    int32_t pair_p;      // ... on 4-byte boundaries, and ni is even
     int32_t vec_out;     // rows of out start on 16-byte boundaries
     int32_t tiles_i, tiles_j;
     int32_t splits, steps_per_split, steps;

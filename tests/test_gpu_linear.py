@@ -357,10 +357,11 @@ def test_f16_gradients_at_far_scales(L):
     assert not L.linear_grad_weight(dy, zero).any()
 
 
-def test_grad_weight_of_no_rows_is_zero(L):
+@pytest.mark.parametrize("k", [24, 25])
+def test_grad_weight_of_no_rows_is_zero(L, k):
     x = L.Rows(torch.empty((0, 48), dtype=torch.int8, device="cuda"), torch.empty(0, device="cuda"), 40)
-    dw = torch.full((24, 40), 3.0, device="cuda")
-    L.linear_grad_weight(torch.empty((0, 24), dtype=torch.bfloat16, device="cuda"), x, out=dw)
+    dw = torch.full((k, 40), 3.0, device="cuda")
+    L.linear_grad_weight(torch.empty((0, k), dtype=torch.bfloat16, device="cuda"), x, out=dw)
     assert not dw.any()
 
 
