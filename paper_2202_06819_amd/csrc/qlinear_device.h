@@ -177,6 +177,27 @@ __device__ __forceinline__ uint2 widen8(uint32_t v) {
     return uint2{__builtin_amdgcn_perm(odd, even, 0x05010400u), __builtin_amdgcn_perm(odd, even, 0x07030602u)};
 }
 
+// Up to four results from one row, `left` of them within it.
+__device__ __forceinline__ void store4(float *out, f32x4 d, int left, bool vec) {
+    if (vec && left >= 4) {
+        *reinterpret_cast<f32x4 *>(out) = d;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < left) out[e] = d[e];
+    }
+}
+template <class T>
+__device__ __forceinline__ void store4(typename T::elem *out, f32x4 d, int left, bool vec) {
+    if (vec && left >= 4) {
+        *reinterpret_cast<uint2 *>(out) = uint2{pack2<T>(d[0], d[1]), pack2<T>(d[2], d[3])};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < left) out[e] = (typename T::elem)d[e];
+    }
+}
+
 // Workgroups are dispatched to the eight XCDs in turn.  Tile `n` of `count`
 // for workgroup `id`, such that each XCD (its own L2) gets a run of tiles.
 __device__ __forceinline__ int xcd_run(int id, int count) {

@@ -34,44 +34,69 @@ __device__ __forceinline__ int next_adapter(uint32_t &left, int id) {
     return a;
 }
 
+// The adapter of a row; -1: none.
+__device__ __forceinline__ int adapter_of(const LinearArgs &a, int row) {
+    const int id = row < a.m ? a.ad.row[row] : -1;
+    return id < a.ad.count ? max(id, -1) : -1;
+}
+
 // Partial sums of u over one of `splits` runs of channels, without the row
 // scale: sum of codes times A for the row's own adapter.  A workgroup takes 16
-// rows and a run; its waves take the run's 32-channel steps in turn, and for
-// each adapter that the rows name, multiply its A (RF fragments of 16 ranks) by
-// all of them and keep the rows that asked for it.
+// rows and a run of 32-channel steps.  The adapters that the rows name are dealt
+// to its eight waves, and where they are fewer than the waves, several waves share
+// one and take its steps in turn, so that all loads of A are in flight at once
+// whether the rows agree or not.  A wave multiplies its adapter's A (RF fragments of
+// 16 ranks) by all rows and keeps the rows that asked for it.  Bound by reading A.
 template <class T, int RF>
 __global__ void __launch_bounds__(512) adapter_rows(LinearArgs a, int steps_per_split) {
-    constexpr int kWaves = 8;
+    constexpr int kWaves = 8, kDeep = RF == 1 ? 8 : RF == 8 ? 2 : 4;   // steps loaded ahead
     __shared__ f32x4 part[kWaves][RF][64];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int r = lane & 15, g = lane >> 4;
     const int row0 = (int)blockIdx.x * 16, row = row0 + r;
     const int all = (a.c + 31) / 32;
     const int begin = (int)blockIdx.y * steps_per_split, end = min(begin + steps_per_split, all);
-    int id = row < a.m ? a.ad.row[row] : -1;
-    if (id < 0 || id >= a.ad.count) id = -1;
+    const int id = adapter_of(a, row);
+    const uint32_t named = (uint32_t)__ballot(id >= 0) & 0xffffu;
+    int distinct = 0;
+    for (uint32_t left = named; left && distinct < kWaves; ++distinct) next_adapter(left, id);
+    const int classes = distinct > 4 ? 8 : distinct > 2 ? 4 : distinct > 1 ? 2 : 1;
+    const int share = kWaves / classes, mine = wave & (classes - 1), first = begin + wave / classes;
+    const __amdgpu_buffer_rsrc_t rx = range_of(a.x.codes + (int64_t)row0 * a.x.pitch,
+                                               (int64_t)(a.m - 1 - row0) * a.x.pitch + a.x.used);
     f32x4 sum[RF];
 #pragma unroll
     for (int f = 0; f < RF; ++f) sum[f] = f32x4{0, 0, 0, 0};
-    const uint8_t *x = a.x.codes + (int64_t)min(row, a.m - 1) * a.x.pitch;
-    uint32_t left = (uint32_t)__ballot(id >= 0) & 0xffffu;
-    while (left) {
+    int n = 0;
+    for (uint32_t left = named; left; ++n) {
         const int ad = next_adapter(left, id);
-        const typename T::elem *A = static_cast<const typename T::elem *>(a.ad.a) + (int64_t)ad * a.ad.rank * a.c;
+        if ((n & (classes - 1)) != mine) continue;
+        // A's rows past the rank lie past the range, and load as zeros
+        const __amdgpu_buffer_rsrc_t ra = range_of(
+            static_cast<const typename T::elem *>(a.ad.a) + (int64_t)ad * a.ad.rank * a.c, (int64_t)a.ad.rank * a.c * 2);
         f32x4 d[RF];
 #pragma unroll
         for (int f = 0; f < RF; ++f) d[f] = f32x4{0, 0, 0, 0};
-        for (int s = begin + wave; s < end; s += kWaves) {
-            const int at = s * 32 + g * 8;      // c is a multiple of 8: a vector is whole or absent
-            const bool in = at < a.c;
-            const uint2 q = in ? *reinterpret_cast<const uint2 *>(x + at) : uint2{0u, 0u};
-            const typename T::v8 b = codes_to_v8<T>(q);
+        for (int s = first; s < end; s += kDeep * share) {
+            u32x4_t w[kDeep][RF];
+            uint2 q[kDeep];
 #pragma unroll
-            for (int f = 0; f < RF; ++f) {
-                u32x4_t w{0, 0, 0, 0};
-                if (in && f * 16 + r < a.ad.rank)
-                    w = *reinterpret_cast<const u32x4_t *>(A + (int64_t)(f * 16 + r) * a.c + at);
-                d[f] = T::mma(__builtin_bit_cast(typename T::v8, w), b, d[f]);
+            for (int e = 0; e < kDeep; ++e) {
+                const int at = (s + e * share) * 32 + g * 8;   // c is a multiple of 8: a vector is whole or absent
+                const bool in = s + e * share < end && at < a.c;
+                const auto v = __builtin_amdgcn_raw_buffer_load_b64(
+                    rx, (int)(in ? (uint32_t)r * (uint32_t)a.x.pitch + (uint32_t)at : kNowhere), 0, 0);
+                q[e] = uint2{v[0], v[1]};
+#pragma unroll
+                for (int f = 0; f < RF; ++f)
+                    w[e][f] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(
+                        ra, (int)(in ? (uint32_t)((f * 16 + r) * a.c + at) * 2u : kNowhere), 0, 0));
+            }
+#pragma unroll
+            for (int e = 0; e < kDeep; ++e) {
+                const typename T::v8 b = codes_to_v8<T>(q[e]);
+#pragma unroll
+                for (int f = 0; f < RF; ++f) d[f] = T::mma(__builtin_bit_cast(typename T::v8, w[e][f]), b, d[f]);
             }
         }
         if (id == ad)
@@ -94,12 +119,13 @@ __global__ void __launch_bounds__(512) adapter_rows(LinearArgs a, int steps_per_
 
 // ---------------------------------------------------------- adapters, part two
 
-// Eight ranks (32 rc + 8 g ..) of u of the lane's row, summed over the splits.
+// Eight ranks of u of the lane's row, summed over the splits in their order.
 __device__ __forceinline__ void load_u(const LinearArgs &a, int row, int rank, float (&u)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) u[i] = 0.0f;
     if (row >= a.m || rank >= a.ad.rank) return;
     const float *p = a.ad.u + (int64_t)row * a.ad.rank + rank;
+#pragma unroll 4
     for (int s = 0; s < a.ad.splits; ++s, p += (int64_t)a.m * a.ad.rank) {
         const f32x4 lo = *reinterpret_cast<const f32x4 *>(p), hi = *reinterpret_cast<const f32x4 *>(p + 4);
 #pragma unroll
@@ -107,170 +133,335 @@ __device__ __forceinline__ void load_u(const LinearArgs &a, int row, int rank, f
     }
 }
 
-// A power of two that brings the row's largest |u| (over all its ranks, held by
-// the four lanes of the row) into [1, 2), and its inverse: u is rounded to 16
-// bits after it, so the rounding is relative to the row and no f16 overflows.
+// A power of two that brings a row's largest |u| (its float bits) into [1, 2), and its
+// inverse: u is rounded to 16 bits after it, so that the rounding is relative to the
+// row and no f16 overflows.  Within 2^-40 .. 2^40: results scaled by it stay finite.
 __device__ __forceinline__ void row_factor(uint32_t m, float &down, float &up) {
-    m = max(m, (uint32_t)__shfl_xor((int)m, 16));
-    m = max(m, (uint32_t)__shfl_xor((int)m, 32));
-    const int e = min(max((int)(m >> 23), 1), 253);
+    const int e = min(max((int)(m >> 23), 127 - 40), 127 + 40);
     down = __builtin_bit_cast(float, (uint32_t)(254 - e) << 23);
     up = __builtin_bit_cast(float, (uint32_t)e << 23);
 }
 
-constexpr int kMaxRankSteps = 4;   // ranks up to 128, 32 a product
-
-// Adds the adapters' second products for 16 rows (the wave's lanes' row is
-// row0 + (lane & 15)) to FJ fragments of results in `d`: d[f] += alpha up
-// (u B^T).  row_of(f) is the output channel of lane row r of fragment f.  Every
-// `stride`-th adapter from `first` on that the rows name is taken.
-template <class T, int FJ, class RowOf>
+// Adds the adapters' second products for 16 rows to FJ fragments of results: d[j] +=
+// alpha xs (u B^T) for the row row0 + (lane & 15) and the output channels
+// channel_of(j) of lane row r of fragment j.  Takes every `stride`-th adapter from
+// `first` on that the rows name; the next one's B is loaded while one's is
+// multiplied.
+template <class T, int FJ, class ChannelOf>
 __device__ __forceinline__ void add_adapters(const LinearArgs &a, int row0, int lane, int first, int stride,
-                                             RowOf row_of, f32x4 (&d)[FJ]) {
+                                             ChannelOf channel_of, f32x4 (&d)[FJ]) {
+    using v8 = typename T::v8;
     const int r = lane & 15, g = lane >> 4, row = row0 + r;
-    int id = row < a.m ? a.ad.row[row] : -1;
-    if (id < 0 || id >= a.ad.count) id = -1;
-    uint32_t left = (uint32_t)__ballot(id >= 0) & 0xffffu;
-    if (!left) return;
-    const int steps = (a.ad.rank + 31) / 32;
-    float u[kMaxRankSteps][8];
-    uint32_t m = 0;
-#pragma unroll
-    for (int s = 0; s < kMaxRankSteps; ++s)
-        if (s < steps) {
-            load_u(a, row, s * 32 + g * 8, u[s]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) m = max(m, __builtin_bit_cast(uint32_t, u[s][i]) & 0x7fffffffu);
+    const int id = adapter_of(a, row);
+    const uint32_t named = (uint32_t)__ballot(id >= 0) & 0xffffu;
+    if (!named) return;
+    auto next_mine = [&](uint32_t &left, int &n) {
+        int ad = -1;
+        while (left) {
+            ad = next_adapter(left, id);
+            if (n++ % stride == first) return ad;
         }
-    float down, up;
-    row_factor(m, down, up);
-    u32x4_t ub[kMaxRankSteps];
+        return -1;
+    };
+    for (int rank0 = 0; rank0 < a.ad.rank; rank0 += 64) {
+        u32x4_t ub[2];
+        float u[2][8];
+        uint32_t m = 0;
 #pragma unroll
-    for (int s = 0; s < kMaxRankSteps; ++s)
-        if (s < steps) {
+        for (int s = 0; s < 2; ++s) {
+            load_u(a, row, rank0 + s * 32 + g * 8, u[s]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) ub[s][i] = pack2<T>(u[s][2 * i] * down, u[s][2 * i + 1] * down);
+            for (int e = 0; e < 8; ++e) m = max(m, __builtin_bit_cast(uint32_t, u[s][e]) & 0x7fffffffu);
         }
-    const float scale = up * (row < a.m ? a.x.scale[row] : 0.0f);
-    int n = 0;
-    while (left) {
-        const int ad = next_adapter(left, id);
-        if (n++ % stride != first) continue;
-        const typename T::elem *B = static_cast<const typename T::elem *>(a.ad.b) + (int64_t)ad * a.k * a.ad.rank;
-        const float f = id == ad ? scale * a.ad.alpha[ad] : 0.0f;
+        m = max(m, (uint32_t)__shfl_xor((int)m, 16));
+        m = max(m, (uint32_t)__shfl_xor((int)m, 32));
+        float down, up;
+        row_factor(m, down, up);
 #pragma unroll
-        for (int j = 0; j < FJ; ++j) {
-            const int ch = row_of(j);
-            f32x4 t{0, 0, 0, 0};
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int s = 0; s < kMaxRankSteps; ++s)
-                if (s < steps) {
-                    const int rank = s * 32 + g * 8;
-                    u32x4_t w{0, 0, 0, 0};
+            for (int e = 0; e < 4; ++e) ub[s][e] = pack2<T>(u[s][2 * e] * down, u[s][2 * e + 1] * down);
+        const float scale = up * (row < a.m ? a.x.scale[row] : 0.0f);
+        auto load_b = [&](int ad, u32x4_t (&w)[FJ][2]) {
+            const typename T::elem *B = static_cast<const typename T::elem *>(a.ad.b) + (int64_t)ad * a.k * a.ad.rank;
+#pragma unroll
+            for (int j = 0; j < FJ; ++j)
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const int ch = channel_of(j), rank = rank0 + s * 32 + g * 8;
+                    w[j][s] = u32x4_t{0, 0, 0, 0};
                     if (ch < a.k && rank < a.ad.rank)
-                        w = *reinterpret_cast<const u32x4_t *>(B + (int64_t)ch * a.ad.rank + rank);
-                    t = T::mma(__builtin_bit_cast(typename T::v8, w), __builtin_bit_cast(typename T::v8, ub[s]), t);
+                        w[j][s] = *reinterpret_cast<const u32x4_t *>(B + (int64_t)ch * a.ad.rank + rank);
                 }
-            if (id == ad)   // (not by a zero factor: another adapter's product may not be finite)
+        };
+        uint32_t left = named;
+        int n = 0;
+        int ad = next_mine(left, n);
+        u32x4_t w[FJ][2];
+        if (ad >= 0) load_b(ad, w);
+        while (ad >= 0) {
+            const int after = next_mine(left, n);
+            u32x4_t w_after[FJ][2];
+            if (after >= 0) load_b(after, w_after);
+            const float f = scale * a.ad.alpha[ad];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) d[j][i] += f * t[i];
+            for (int j = 0; j < FJ; ++j) {
+                f32x4 t = T::mma(__builtin_bit_cast(v8, w[j][0]), __builtin_bit_cast(v8, ub[0]), f32x4{0, 0, 0, 0});
+                if (rank0 + 32 < a.ad.rank) t = T::mma(__builtin_bit_cast(v8, w[j][1]), __builtin_bit_cast(v8, ub[1]), t);
+                // (chosen, not by a zero factor: another adapter's product may not be finite)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) d[j][e] = id == ad ? __builtin_fmaf(f, t[e], d[j][e]) : d[j][e];
+            }
+#pragma unroll
+            for (int j = 0; j < FJ; ++j)
+#pragma unroll
+                for (int s = 0; s < 2; ++s) w[j][s] = w_after[j][s];
+            ad = after;
         }
     }
 }
 
 // --------------------------------------------------------------- few rows
 
-// Up to 16 FI rows against 16 output channels a workgroup: eight waves take
-// the 128-channel steps in turn, weights and rows straight from memory into
-// registers (each weight is used once, so LDS would only be a detour), and
-// their sums meet in LDS.  Bound by reading the weights.
-template <class T, int WB, int FI, bool AD>
+// 16 FI rows against 16 FJ output channels a workgroup: eight waves take the
+// 128-channel steps in turn, two at a time, weights and rows straight from memory
+// into registers (each weight is used once, so LDS would only be a detour), and
+// their sums meet in LDS.  Bound by reading the weights, and with many rows by
+// reading those from L2 once for each workgroup: hence wider ones where there are
+// enough channels to fill the chip.
+constexpr int few_lds(int fj, int fi, bool ad) { return 8 * 64 * 16 * (fj * fi + (ad ? fj : 0)); }
+template <class T, int WB, int FJ, int FI, bool AD>
 __global__ void __launch_bounds__(512) linear_few(LinearArgs a) {
     constexpr int kWaves = 8, kParts = kWaves / FI;
-    __shared__ i32x4 part[kWaves][FI][64];
-    __shared__ f32x4 extra[AD ? kParts : 1][FI][64];
+    constexpr int kWide = WB == 8 ? 2 : 1;   // 16-byte vectors of weights a lane and step
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    auto part = reinterpret_cast<i32x4(*)[FJ * FI][64]>(smem);                                // waves' sums
+    auto extra = reinterpret_cast<f32x4(*)[FJ][64]>(smem + kWaves * FJ * FI * 64 * 16);   // the adapters' part
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int r = lane & 15, g = lane >> 4;
-    const int ch0 = (int)blockIdx.x * 16;
-    const __amdgpu_buffer_rsrc_t rx = range_of(a.x.codes, (int64_t)(a.m - 1) * a.x.pitch + a.x.used);
-    const uint8_t *w0 = a.w.codes + (int64_t)ch0 * a.w.pitch;
-    const __amdgpu_buffer_rsrc_t rw = range_of(w0, (int64_t)(a.k - 1 - ch0) * a.w.pitch + a.w.used);
-    i32x4 acc[FI];
+    const int ch0 = (int)blockIdx.x * 16 * FJ, row0 = (int)blockIdx.y * 16 * FI;
+    const __amdgpu_buffer_rsrc_t rx = range_of(a.x.codes + (int64_t)row0 * a.x.pitch,
+                                               (int64_t)(a.m - 1 - row0) * a.x.pitch + a.x.used);
+    const __amdgpu_buffer_rsrc_t rw = range_of(a.w.codes + (int64_t)ch0 * a.w.pitch,
+                                               (int64_t)(a.k - 1 - ch0) * a.w.pitch + a.w.used);
+    i32x4 acc[FJ][FI];
 #pragma unroll
-    for (int f = 0; f < FI; ++f) acc[f] = i32x4{0, 0, 0, 0};
-    const uint32_t wrow = (uint32_t)r * (uint32_t)a.w.pitch;
-    auto load_x = [&](int f, int at) {
-        const int row = f * 16 + r;
-        return __builtin_amdgcn_raw_buffer_load_b128(
-            rx, (int)(at < a.x.used && row < a.m ? (uint32_t)row * (uint32_t)a.x.pitch + (uint32_t)at : kNowhere), 0, 0);
+    for (int j = 0; j < FJ; ++j)
+#pragma unroll
+        for (int f = 0; f < FI; ++f) acc[j][f] = i32x4{0, 0, 0, 0};
+    struct Step {
+        u32x4_t w[FJ][kWide], x[FI][2];
     };
-    auto load_w = [&](int at) {
-        return __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(at < a.w.used ? wrow + (uint32_t)at : kNowhere), 0, 0);
-    };
-    for (int s = wave; s < a.steps; s += kWaves) {
-        if constexpr (WB == 8) {
-            // the depth's order is free as long as both operands share it
+    // lane (r, g) takes channels g * 32 .. + 31 of a step of 4-bit weights, g * 16 ..
+    // + 15 of each half of one of 8-bit weights: the depth's order is free as long as
+    // both operands share it
+    auto load = [&](int s, Step &q) {
+#pragma unroll
+        for (int j = 0; j < FJ; ++j)
+#pragma unroll
+            for (int h = 0; h < kWide; ++h) {
+                const int at = WB == 8 ? s * 128 + h * 64 + g * 16 : s * 64 + g * 16;
+                q.w[j][h] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(
+                    rw, (int)(at < a.w.used ? (uint32_t)(j * 16 + r) * (uint32_t)a.w.pitch + (uint32_t)at : kNowhere), 0, 0));
+            }
+#pragma unroll
+        for (int f = 0; f < FI; ++f)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int at = s * 128 + h * 64 + g * 16;
-                const auto w = load_w(at);
-#pragma unroll
-                for (int f = 0; f < FI; ++f)
-                    acc[f] = MmaI8::mma(__builtin_bit_cast(i32x4, w), __builtin_bit_cast(i32x4, load_x(f, at)), acc[f]);
+                const int at = WB == 8 ? s * 128 + h * 64 + g * 16 : s * 128 + g * 32 + h * 16;
+                q.x[f][h] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(
+                    rx, (int)(at < a.x.used ? (uint32_t)(f * 16 + r) * (uint32_t)a.x.pitch + (uint32_t)at : kNowhere), 0, 0));
             }
-        } else {
-            const auto w = load_w(s * 64 + g * 16);   // 32 channels
-            i32x4 lo, hi;
+    };
+    auto multiply = [&](const Step &q) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint2 p = widen8(w[i]), q = widen8(w[i + 2]);
-                lo[2 * i] = (int)p.x, lo[2 * i + 1] = (int)p.y;
-                hi[2 * i] = (int)q.x, hi[2 * i + 1] = (int)q.y;
-            }
-            const int at = s * 128 + g * 32;
+        for (int j = 0; j < FJ; ++j) {
+            i32x4 w[2];
+            if constexpr (WB == 8) {
+                w[0] = __builtin_bit_cast(i32x4, q.w[j][0]);
+                w[1] = __builtin_bit_cast(i32x4, q.w[j][kWide - 1]);
+            } else {
 #pragma unroll
-            for (int f = 0; f < FI; ++f) {
-                acc[f] = MmaI8::mma(lo, __builtin_bit_cast(i32x4, load_x(f, at)), acc[f]);
-                acc[f] = MmaI8::mma(hi, __builtin_bit_cast(i32x4, load_x(f, at + 16)), acc[f]);
+                for (int h = 0; h < 2; ++h) {
+                    const uint2 p = widen8(q.w[j][0][2 * h]), t = widen8(q.w[j][0][2 * h + 1]);
+                    w[h] = i32x4{(int)p.x, (int)p.y, (int)t.x, (int)t.y};
+                }
             }
+#pragma unroll
+            for (int f = 0; f < FI; ++f)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) acc[j][f] = MmaI8::mma(w[h], __builtin_bit_cast(i32x4, q.x[f][h]), acc[j][f]);
         }
+    };
+    // two steps in flight; past the last one loads give zeros
+    Step q[2];
+    load(wave, q[0]);
+    load(wave + kWaves, q[1]);
+    if constexpr (AD) {
+        // wave = part * FI + fragment: the parts share the fragment's adapters.  Here,
+        // so that the weights are on their way meanwhile
+        f32x4 d[FJ];
+#pragma unroll
+        for (int j = 0; j < FJ; ++j) d[j] = f32x4{0, 0, 0, 0};
+        add_adapters<T, FJ>(a, row0 + wave % FI * 16, lane, wave / FI, kParts, [&](int j) { return ch0 + j * 16 + r; }, d);
+#pragma unroll
+        for (int j = 0; j < FJ; ++j) extra[wave][j][lane] = d[j];
+    }
+    for (int s = wave; s < a.steps; s += 2 * kWaves) {
+        multiply(q[0]);
+        load(s + 2 * kWaves, q[0]);
+        multiply(q[1]);
+        load(s + 3 * kWaves, q[1]);
     }
 #pragma unroll
-    for (int f = 0; f < FI; ++f) part[wave][f][lane] = acc[f];
-    if constexpr (AD) {
-        // wave = part * FI + fragment: the parts share the fragment's adapters
-        f32x4 d[1] = {f32x4{0, 0, 0, 0}};
-        add_adapters<T, 1>(a, wave % FI * 16, lane, wave / FI, kParts, [&](int) { return ch0 + r; }, d);
-        extra[wave / FI][wave % FI][lane] = d[0];
-    }
+    for (int j = 0; j < FJ; ++j)
+#pragma unroll
+        for (int f = 0; f < FI; ++f) part[wave][j * FI + f][lane] = acc[j][f];
     __syncthreads();
-    if (wave >= FI) return;
-    const int row = wave * 16 + r, ch = ch0 + g * 4;   // results: channels ch .. ch + 3 of one row
-    i32x4 t = part[0][wave][lane];
+    // results: channels ch .. ch + 3 of one row
 #pragma unroll
-    for (int p = 1; p < kWaves; ++p) t += part[p][wave][lane];
-    if (row >= a.m) return;
-    const float xs = a.x.scale[row] * (WB == 4 ? 0.0625f : 1.0f);
-    float y[4];
+    for (int n = 0; n < (FJ * FI + kWaves - 1) / kWaves; ++n) {
+        const int o = wave + n * kWaves, j = o / FI, f = o % FI;
+        if (o >= FJ * FI) break;
+        const int row = row0 + f * 16 + r, ch = ch0 + j * 16 + g * 4;
+        i32x4 t = part[0][o][lane];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = ch + i < a.k ? (float)t[i] * xs * a.w.scale[ch + i] : 0.0f;
-    if constexpr (AD) {
+        for (int p = 1; p < kWaves; ++p) t += part[p][o][lane];
+        if (row >= a.m || ch >= a.k) continue;
+        const float xs = a.x.scale[row] * (WB == 4 ? 0.0625f : 1.0f);
+        f32x4 y;
 #pragma unroll
-        for (int p = 0; p < kParts; ++p)
+        for (int e = 0; e < 4; ++e) y[e] = (float)t[e] * xs * a.w.scale[min(ch + e, a.k - 1)];
+        if constexpr (AD)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] += extra[p][wave][lane][i];
-    }
-    typename T::elem *out = static_cast<typename T::elem *>(a.y) + (int64_t)row * a.ldy + ch;
-    if (a.vec && ch + 4 <= a.k) {
-        *reinterpret_cast<uint2 *>(out) = uint2{pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3])};
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (ch + i < a.k) out[i] = (typename T::elem)y[i];
+            for (int p = 0; p < kParts; ++p) y += extra[p * FI + f][j][lane];
+        store4<T>(static_cast<typename T::elem *>(a.y) + (int64_t)row * a.ldy + ch, y, a.k - ch, a.vec);
     }
 }
 
 // --------------------------------------------------------------- many rows
+
+// The adapters' second products of a workgroup's tile: further steps of the same tile
+// product, in 16-bit floats.  u (64 ranks of it, scaled and rounded) stays in LDS;
+// each adapter that the tile's rows name has its B copied to one of two buffers and
+// takes a step, whose products go to the rows that named it.  So an adapter's B is
+// read once for a tile, however its rows lie.
+template <class T, int TJ, int TI, int THREADS>
+struct TileAdapters {
+    const LinearArgs &a;
+    uint8_t *smem;   // after the main loop: u | B | B | adapters of the rows | factors
+    int i0, j0;
+    static constexpr int kU = TI * kStepBytes, kB = TJ * kStepBytes, kIds = kU + 2 * kB;
+    static constexpr bool kScaled = __is_same(T, F16);   // bf16 has float's range
+
+    __device__ int *ids() const { return reinterpret_cast<int *>(smem + kIds); }
+    __device__ float *factors() const { return reinterpret_cast<float *>(smem + kIds + TI * 4); }
+    __device__ float down(int row) const { return kScaled ? 1.0f / factors()[row] : 1.0f; }   // (a power of two: exact)
+    __device__ float up(int row) const { return kScaled ? factors()[row] : 1.0f; }
+
+    // alpha xs u of the tile's rows: 64 ranks from rank0, as 16-bit floats in LDS.  The
+    // row's factor comes from all of its ranks.
+    __device__ void fill_u(int rank0) const {
+#pragma unroll
+        for (int n = 0; n < TI * 8 / THREADS; ++n) {
+            const int unit = n * THREADS + (int)threadIdx.x, at = unit >> 3, v = unit & 7, row = i0 + at;
+            const int id = adapter_of(a, row);
+            const float s = id >= 0 ? a.ad.alpha[id] * a.x.scale[row] : 0.0f;
+            float u[8];
+            load_u(a, id >= 0 ? row : a.m, rank0 + v * 8, u);
+            float down = 1.0f, up = 1.0f;
+            if constexpr (kScaled) {
+                uint32_t m = 0;
+                for (int c = 0; c < a.ad.rank; c += 64) {
+                    float other[8];
+                    load_u(a, id >= 0 ? row : a.m, c + v * 8, other);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) m = max(m, __builtin_bit_cast(uint32_t, other[e] * s) & 0x7fffffffu);
+                }
+#pragma unroll
+                for (int b = 1; b < 8; b <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, b));
+                row_factor(m, down, up);
+            }
+            u32x4_t w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = pack2<T>(u[2 * e] * s * down, u[2 * e + 1] * s * down);
+            *reinterpret_cast<u32x4_t *>(smem + at * kStepBytes + ((v ^ slot(at)) << 4)) = w;
+            if (v == 0) ids()[at] = id, factors()[at] = up;
+        }
+    }
+    __device__ void stage_u() const {
+        fill_u(0);
+        __syncthreads();
+    }
+    // the lowest adapter above `last` that a row of the tile names; -1: none
+    __device__ int next(int last, int lane) const {
+        uint32_t best = ~0u;
+#pragma unroll
+        for (int n = 0; n < TI / 64; ++n) {
+            const int id = ids()[n * 64 + lane];
+            if (id > last) best = min(best, (uint32_t)id);
+        }
+#pragma unroll
+        for (int d = 32; d; d >>= 1) best = min(best, (uint32_t)__shfl_xor((int)best, d));
+        return __builtin_amdgcn_readfirstlane((int)best);
+    }
+    __device__ void copy_b(int ad, int rank0, uint8_t *to, int wave, int lane) const {
+        const int64_t row_bytes = (int64_t)a.ad.rank * 2;
+        const u32x4_t rb = range_words(static_cast<const uint8_t *>(a.ad.b) + ((int64_t)ad * a.k + j0) * row_bytes,
+                                       (int64_t)(a.k - j0) * row_bytes);
+        copy_rows<TJ, THREADS>(to, rb, (uint32_t)row_bytes, rank0 * 2, (int)row_bytes, wave, lane);
+    }
+    template <int FJ, int FI>
+    __device__ void add(int jrow0, int irow0, int wave, int lane, f32x4 (&d)[FJ][FI]) const {
+        using v8 = typename T::v8;
+        const int r = lane & 15, g = lane >> 4;
+        for (int rank0 = 0; rank0 < a.ad.rank; rank0 += 64) {
+            if (rank0) {   // everyone is done with the ranks before
+                __syncthreads();
+                fill_u(rank0);
+                __syncthreads();
+            }
+            int ad = next(-1, lane), buf = 0;
+            if (ad >= 0) copy_b(ad, rank0, smem + kU, wave, lane);
+            while (ad >= 0) {
+                const int after = next(ad, lane);
+                copies_done();
+                __syncthreads();
+                // (the other buffer: its step ended before this barrier)
+                if (after >= 0) copy_b(after, rank0, smem + kU + (buf ^ 1) * kB, wave, lane);
+                const uint8_t *lj = smem + kU + buf * kB;
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) {
+                    if (rank0 + ks * 32 >= a.ad.rank) break;
+                    v8 w[FJ];
+#pragma unroll
+                    for (int j = 0; j < FJ; ++j) {
+                        const int row = jrow0 + j_row(j, r);
+                        w[j] = *reinterpret_cast<const v8 *>(lj + row * kStepBytes + (((ks * 4 + g) ^ slot(row)) << 4));
+                    }
+#pragma unroll
+                    for (int i = 0; i < FI; ++i) {
+                        const int row = irow0 + i * 16 + r;
+                        const bool mine = ids()[row] == ad;
+                        const uint64_t who = __ballot(mine);
+                        if (!who) continue;
+                        const v8 u = *reinterpret_cast<const v8 *>(smem + row * kStepBytes + (((ks * 4 + g) ^ slot(row)) << 4));
+                        // (results are chosen, not made zero by u: another adapter's
+                        // product may not be finite)
+#pragma unroll
+                        for (int j = 0; j < FJ; ++j) {
+                            const f32x4 t = T::mma(w[j], u, d[j][i]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) d[j][i][e] = mine ? t[e] : d[j][i][e];
+                        }
+                    }
+                }
+                ad = after;
+                buf ^= 1;
+            }
+        }
+    }
+};
 
 // TJ output channels by TI rows a workgroup of WJ x WI waves, each a tile of 64
 // by 16 FI.  Steps of 128 channels are staged in one of two LDS buffers while
@@ -342,30 +533,36 @@ __global__ void __launch_bounds__(WJ *WI * 64) linear_tile(LinearArgs a) {
     float ws[16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) ws[e] = a.w.scale[min(ch + e, a.k - 1)];
+    TileAdapters<T, TJ, TI, kThreads> ad{a, smem, i0, j0};
+    if constexpr (AD) ad.stage_u();
+    f32x4 d[FJ][FI];
 #pragma unroll
     for (int i = 0; i < FI; ++i) {
         const int row = i0 + irow0 + i * 16 + r;
-        const float xs = row < a.m ? a.x.scale[row] * (WB == 4 ? 0.0625f : 1.0f) : 0.0f;
-        f32x4 d[FJ];
+        float xs = row < a.m ? a.x.scale[row] * (WB == 4 ? 0.0625f : 1.0f) : 0.0f;
+        if constexpr (AD) xs *= ad.down(irow0 + i * 16 + r);
 #pragma unroll
         for (int j = 0; j < FJ; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) d[j][e] = (float)acc[j][i][e] * xs * ws[4 * j + e];
-        if constexpr (AD)
-            add_adapters<T, FJ>(a, i0 + irow0 + i * 16, lane, 0, 1,
-                                [&](int j) { return j0 + jrow0 + j_row(j, r); }, d);
-        if (row < a.m) {
-            typename T::elem *out = static_cast<typename T::elem *>(a.y) + (int64_t)row * a.ldy + ch;
-            if (a.vec && ch + 16 <= a.k) {
+            for (int e = 0; e < 4; ++e) d[j][i][e] = (float)acc[j][i][e] * xs * ws[4 * j + e];
+    }
+    if constexpr (AD) ad.template add<FJ, FI>(jrow0, irow0, wave, lane, d);
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    *reinterpret_cast<uint4 *>(out + 8 * h) =
-                        uint4{pack2<T>(d[2 * h][0], d[2 * h][1]), pack2<T>(d[2 * h][2], d[2 * h][3]),
-                              pack2<T>(d[2 * h + 1][0], d[2 * h + 1][1]), pack2<T>(d[2 * h + 1][2], d[2 * h + 1][3])};
+    for (int i = 0; i < FI; ++i) {
+        const int row = i0 + irow0 + i * 16 + r;
+        if (row >= a.m) continue;
+        const float up = AD ? ad.up(irow0 + i * 16 + r) : 1.0f;
+        typename T::elem *out = static_cast<typename T::elem *>(a.y) + (int64_t)row * a.ldy + ch;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const f32x4 lo = d[2 * h][i] * up, hi = d[2 * h + 1][i] * up;
+            if (a.vec && ch + 8 * h + 8 <= a.k) {
+                *reinterpret_cast<uint4 *>(out + 8 * h) = uint4{pack2<T>(lo[0], lo[1]), pack2<T>(lo[2], lo[3]),
+                                                                pack2<T>(hi[0], hi[1]), pack2<T>(hi[2], hi[3])};
             } else {
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (ch + e < a.k) out[e] = (typename T::elem)d[e >> 2][e & 3];
+                for (int e = 0; e < 8; ++e)
+                    if (ch + 8 * h + e < a.k) out[8 * h + e] = (typename T::elem)(e < 4 ? lo[e & 3] : hi[e & 3]);
             }
         }
     }

@@ -62,27 +62,6 @@ __device__ __forceinline__ typename T::v8 read_transposed(const uint8_t *lds, in
     return __builtin_bit_cast(typename T::v8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// Up to four results from one row, `left` of them within it.
-__device__ __forceinline__ void store4(float *out, f32x4 d, int left, bool vec) {
-    if (vec && left >= 4) {
-        *reinterpret_cast<f32x4 *>(out) = d;
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < left) out[e] = d[e];
-    }
-}
-template <class T>
-__device__ __forceinline__ void store4(typename T::elem *out, f32x4 d, int left, bool vec) {
-    if (vec && left >= 4) {
-        *reinterpret_cast<uint2 *>(out) = uint2{pack2<T>(d[0], d[1]), pack2<T>(d[2], d[3])};
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < left) out[e] = (typename T::elem)d[e];
-    }
-}
-
 // Three LDS buffers of 64 rows of t: one is multiplied, one has landed, one is on its
 // way.  8-bit codes, and p where its rows are whole aligned vectors (COPY), go straight
 // from memory to LDS; 4-bit codes (widened to bytes) and any other p go through
