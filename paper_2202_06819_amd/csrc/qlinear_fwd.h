@@ -43,13 +43,14 @@ __device__ __forceinline__ int adapter_of(const LinearArgs &a, int row) {
 // Partial sums of u over one of `splits` runs of channels, without the row
 // scale: sum of codes times A for the row's own adapter.  A workgroup takes 16
 // rows and a run of 32-channel steps.  The adapters that the rows name are dealt
-// to its eight waves, and where they are fewer than the waves, several waves share
-// one and take its steps in turn, so that all loads of A are in flight at once
-// whether the rows agree or not.  A wave multiplies its adapter's A (RF fragments of
+// to its waves, and where they are fewer than the waves, several waves share one,
+// each with a run of its steps (so that a wave's loads lie side by side in A's rows),
+// and all loads of A are in flight at once whether the rows agree or not.  A wave multiplies its adapter's A (RF fragments of
 // 16 ranks) by all rows and keeps the rows that asked for it.  Bound by reading A.
+constexpr int adapter_waves(int rf) { return rf == 8 ? 8 : 16; }
 template <class T, int RF>
-__global__ void __launch_bounds__(512) adapter_rows(LinearArgs a, int steps_per_split) {
-    constexpr int kWaves = 8, kDeep = RF == 1 ? 8 : RF == 8 ? 2 : 4;   // steps loaded ahead
+__global__ void __launch_bounds__(adapter_waves(RF) * 64) adapter_rows(LinearArgs a, int steps_per_split) {
+    constexpr int kWaves = adapter_waves(RF), kDeep = RF == 1 ? 8 : RF == 2 ? 4 : 2;   // steps loaded at once
     __shared__ f32x4 part[kWaves][RF][64];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int r = lane & 15, g = lane >> 4;
@@ -60,8 +61,10 @@ __global__ void __launch_bounds__(512) adapter_rows(LinearArgs a, int steps_per_
     const uint32_t named = (uint32_t)__ballot(id >= 0) & 0xffffu;
     int distinct = 0;
     for (uint32_t left = named; left && distinct < kWaves; ++distinct) next_adapter(left, id);
-    const int classes = distinct > 4 ? 8 : distinct > 2 ? 4 : distinct > 1 ? 2 : 1;
-    const int share = kWaves / classes, mine = wave & (classes - 1), first = begin + wave / classes;
+    int classes = 1;
+    while (classes < distinct) classes *= 2;
+    const int mine = wave & (classes - 1), share = kWaves / classes;
+    const int run = (end - begin + share - 1) / share, first = begin + wave / classes * run, last = min(first + run, end);
     const __amdgpu_buffer_rsrc_t rx = range_of(a.x.codes + (int64_t)row0 * a.x.pitch,
                                                (int64_t)(a.m - 1 - row0) * a.x.pitch + a.x.used);
     f32x4 sum[RF];
@@ -77,13 +80,13 @@ __global__ void __launch_bounds__(512) adapter_rows(LinearArgs a, int steps_per_
         f32x4 d[RF];
 #pragma unroll
         for (int f = 0; f < RF; ++f) d[f] = f32x4{0, 0, 0, 0};
-        for (int s = first; s < end; s += kDeep * share) {
+        for (int s = first; s < last; s += kDeep) {
             u32x4_t w[kDeep][RF];
             uint2 q[kDeep];
 #pragma unroll
             for (int e = 0; e < kDeep; ++e) {
-                const int at = (s + e * share) * 32 + g * 8;   // c is a multiple of 8: a vector is whole or absent
-                const bool in = s + e * share < end && at < a.c;
+                const int at = (s + e) * 32 + g * 8;   // c is a multiple of 8: a vector is whole or absent
+                const bool in = s + e < last && at < a.c;
                 const auto v = __builtin_amdgcn_raw_buffer_load_b64(
                     rx, (int)(in ? (uint32_t)r * (uint32_t)a.x.pitch + (uint32_t)at : kNowhere), 0, 0);
                 q[e] = uint2{v[0], v[1]};
@@ -125,7 +128,7 @@ __device__ __forceinline__ void load_u(const LinearArgs &a, int row, int rank, f
     for (int i = 0; i < 8; ++i) u[i] = 0.0f;
     if (row >= a.m || rank >= a.ad.rank) return;
     const float *p = a.ad.u + (int64_t)row * a.ad.rank + rank;
-#pragma unroll 4
+#pragma unroll 8
     for (int s = 0; s < a.ad.splits; ++s, p += (int64_t)a.m * a.ad.rank) {
         const f32x4 lo = *reinterpret_cast<const f32x4 *>(p), hi = *reinterpret_cast<const f32x4 *>(p + 4);
 #pragma unroll
@@ -145,14 +148,15 @@ __device__ __forceinline__ void row_factor(uint32_t m, float &down, float &up) {
 // Adds the adapters' second products for 16 rows to FJ fragments of results: d[j] +=
 // alpha xs (u B^T) for the row row0 + (lane & 15) and the output channels
 // channel_of(j) of lane row r of fragment j.  Takes every `stride`-th adapter from
-// `first` on that the rows name; the next one's B is loaded while one's is
-// multiplied.
-template <class T, int FJ, class ChannelOf>
-__device__ __forceinline__ void add_adapters(const LinearArgs &a, int row0, int lane, int first, int stride,
+// `first` on that the rows name (`id`: the lane's row's), kBatch at a time, whose B
+// are loaded together.  RS:
+// products of 32 ranks at a time (2: ranks above 32, 64 at a time).
+template <class T, int FJ, int RS, class ChannelOf>
+__device__ __forceinline__ void add_adapters(const LinearArgs &a, int id, int row0, int lane, int first, int stride,
                                              ChannelOf channel_of, f32x4 (&d)[FJ]) {
     using v8 = typename T::v8;
+    constexpr int kBatch = FJ * RS <= 2 ? 4 : 2;
     const int r = lane & 15, g = lane >> 4, row = row0 + r;
-    const int id = adapter_of(a, row);
     const uint32_t named = (uint32_t)__ballot(id >= 0) & 0xffffu;
     if (!named) return;
     auto next_mine = [&](uint32_t &left, int &n) {
@@ -163,12 +167,37 @@ __device__ __forceinline__ void add_adapters(const LinearArgs &a, int row0, int 
         }
         return -1;
     };
-    for (int rank0 = 0; rank0 < a.ad.rank; rank0 += 64) {
-        u32x4_t ub[2];
-        float u[2][8];
+    for (int rank0 = 0; rank0 < a.ad.rank; rank0 += 32 * RS) {
+        int ad[kBatch];
+        float alpha[kBatch];
+        u32x4_t w[kBatch][FJ][RS];
+        uint32_t left = named;
+        int n = 0;
+        auto load_batch = [&] {
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) {
+                ad[b] = next_mine(left, n);
+                alpha[b] = ad[b] >= 0 ? a.ad.alpha[ad[b]] : 0.0f;
+                const typename T::elem *B =
+                    static_cast<const typename T::elem *>(a.ad.b) + (int64_t)max(ad[b], 0) * a.k * a.ad.rank;
+#pragma unroll
+                for (int j = 0; j < FJ; ++j)
+#pragma unroll
+                    for (int s = 0; s < RS; ++s) {
+                        const int ch = channel_of(j), rank = rank0 + s * 32 + g * 8;
+                        w[b][j][s] = u32x4_t{0, 0, 0, 0};
+                        if (ad[b] >= 0 && ch < a.k && rank < a.ad.rank)
+                            w[b][j][s] = *reinterpret_cast<const u32x4_t *>(B + (int64_t)ch * a.ad.rank + rank);
+                    }
+            }
+        };
+        load_batch();
+        if (ad[0] < 0) return;   // nothing for this wave
+        u32x4_t ub[RS];
+        float u[RS][8];
         uint32_t m = 0;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
+        for (int s = 0; s < RS; ++s) {
             load_u(a, row, rank0 + s * 32 + g * 8, u[s]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) m = max(m, __builtin_bit_cast(uint32_t, u[s][e]) & 0x7fffffffu);
@@ -178,45 +207,25 @@ __device__ __forceinline__ void add_adapters(const LinearArgs &a, int row0, int 
         float down, up;
         row_factor(m, down, up);
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+        for (int s = 0; s < RS; ++s)
 #pragma unroll
             for (int e = 0; e < 4; ++e) ub[s][e] = pack2<T>(u[s][2 * e] * down, u[s][2 * e + 1] * down);
         const float scale = up * (row < a.m ? a.x.scale[row] : 0.0f);
-        auto load_b = [&](int ad, u32x4_t (&w)[FJ][2]) {
-            const typename T::elem *B = static_cast<const typename T::elem *>(a.ad.b) + (int64_t)ad * a.k * a.ad.rank;
+        while (ad[0] >= 0) {
 #pragma unroll
-            for (int j = 0; j < FJ; ++j)
+            for (int b = 0; b < kBatch; ++b)
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const int ch = channel_of(j), rank = rank0 + s * 32 + g * 8;
-                    w[j][s] = u32x4_t{0, 0, 0, 0};
-                    if (ch < a.k && rank < a.ad.rank)
-                        w[j][s] = *reinterpret_cast<const u32x4_t *>(B + (int64_t)ch * a.ad.rank + rank);
+                for (int j = 0; j < FJ; ++j) {
+                    f32x4 t{0, 0, 0, 0};
+#pragma unroll
+                    for (int s = 0; s < RS; ++s)
+                        t = T::mma(__builtin_bit_cast(v8, w[b][j][s]), __builtin_bit_cast(v8, ub[s]), t);
+                    // (chosen, not by a zero factor: another adapter's product may not be finite)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        d[j][e] = id >= 0 && id == ad[b] ? __builtin_fmaf(scale * alpha[b], t[e], d[j][e]) : d[j][e];
                 }
-        };
-        uint32_t left = named;
-        int n = 0;
-        int ad = next_mine(left, n);
-        u32x4_t w[FJ][2];
-        if (ad >= 0) load_b(ad, w);
-        while (ad >= 0) {
-            const int after = next_mine(left, n);
-            u32x4_t w_after[FJ][2];
-            if (after >= 0) load_b(after, w_after);
-            const float f = scale * a.ad.alpha[ad];
-#pragma unroll
-            for (int j = 0; j < FJ; ++j) {
-                f32x4 t = T::mma(__builtin_bit_cast(v8, w[j][0]), __builtin_bit_cast(v8, ub[0]), f32x4{0, 0, 0, 0});
-                if (rank0 + 32 < a.ad.rank) t = T::mma(__builtin_bit_cast(v8, w[j][1]), __builtin_bit_cast(v8, ub[1]), t);
-                // (chosen, not by a zero factor: another adapter's product may not be finite)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) d[j][e] = id == ad ? __builtin_fmaf(f, t[e], d[j][e]) : d[j][e];
-            }
-#pragma unroll
-            for (int j = 0; j < FJ; ++j)
-#pragma unroll
-                for (int s = 0; s < 2; ++s) w[j][s] = w_after[j][s];
-            ad = after;
+            load_batch();
         }
     }
 }
@@ -293,17 +302,24 @@ __global__ void __launch_bounds__(512) linear_few(LinearArgs a) {
                 for (int h = 0; h < 2; ++h) acc[j][f] = MmaI8::mma(w[h], __builtin_bit_cast(i32x4, q.x[f][h]), acc[j][f]);
         }
     };
+    // wave = part * FI + fragment: the parts share the fragment's adapters.  Which ones
+    // is asked first, their part computed while the first weights are on their way
+    int id = -1;
+    if constexpr (AD) id = adapter_of(a, row0 + wave % FI * 16 + r);
+    asm volatile("" ::: "memory");
     // two steps in flight; past the last one loads give zeros
     Step q[2];
     load(wave, q[0]);
     load(wave + kWaves, q[1]);
     if constexpr (AD) {
-        // wave = part * FI + fragment: the parts share the fragment's adapters.  Here,
-        // so that the weights are on their way meanwhile
         f32x4 d[FJ];
 #pragma unroll
         for (int j = 0; j < FJ; ++j) d[j] = f32x4{0, 0, 0, 0};
-        add_adapters<T, FJ>(a, row0 + wave % FI * 16, lane, wave / FI, kParts, [&](int j) { return ch0 + j * 16 + r; }, d);
+        const auto channel_of = [&](int j) { return ch0 + j * 16 + r; };
+        if (a.ad.rank <= 32)
+            add_adapters<T, FJ, 1>(a, id, row0 + wave % FI * 16, lane, wave / FI, kParts, channel_of, d);
+        else
+            add_adapters<T, FJ, 2>(a, id, row0 + wave % FI * 16, lane, wave / FI, kParts, channel_of, d);
 #pragma unroll
         for (int j = 0; j < FJ; ++j) extra[wave][j][lane] = d[j];
     }

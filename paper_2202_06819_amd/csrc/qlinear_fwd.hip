@@ -15,15 +15,10 @@ hipError_t start(const LinearArgs &a, dim3 grid, int threads, hipStream_t stream
     return hipSuccess;
 }
 
-template <class T, int WB, int FJ, int FI>
+template <class T, int WB, int FJ, int FI, bool AD>
 hipError_t few(const LinearArgs &a, hipStream_t stream) {
     const dim3 grid((unsigned)((a.k + 16 * FJ - 1) / (16 * FJ)), (unsigned)((a.m + 16 * FI - 1) / (16 * FI)));
-    if (a.ad.count) return start<linear_few<T, WB, FJ, FI, true>, few_lds(FJ, FI, true)>(a, grid, 512, stream);
-    return start<linear_few<T, WB, FJ, FI, false>, few_lds(FJ, FI, false)>(a, grid, 512, stream);
-}
-template <class T, int WB, int FI>
-hipError_t few_channels(const LinearArgs &a, hipStream_t stream) {
-    return a.k >= 32 * 192 ? few<T, WB, 2, FI>(a, stream) : few<T, WB, 1, FI>(a, stream);
+    return start<linear_few<T, WB, FJ, FI, AD>, few_lds(FJ, FI, AD)>(a, grid, 512, stream);
 }
 
 template <auto Kernel, int TJ, int TI, int THREADS>
@@ -33,17 +28,68 @@ hipError_t tile(LinearArgs a, hipStream_t stream) {
     return start<Kernel, 2 * (TJ + TI) * kStepBytes>(a, dim3((unsigned)a.tiles_i * (unsigned)a.tiles_j), THREADS, stream);
 }
 
+// The kernels, and a model of their times (us), its constants measured.  A workgroup
+// of the few-row kernel takes `start` and `step` for each 1024 channels in its turn on
+// a CU; a tile takes `steps[n]` for a step of 128 channels with n + 1 on a CU, where
+// `resident` fit.  E.g. 4096 x 4096 4-bit weights: 8 rows 4.4 (16 channels and rows a
+// workgroup; a tile of 64: 15.3); 48 rows 9.2 (32 x 32; tile 15.3); 160 rows 15.6 (tile
+// of 64; few-row kernels 20, tile of 128 26); 2048 rows 43 (tile of 128; of 64 60, of 256
+// 68); 8-bit, 8192 rows: 119 (tile of 256).
+enum class Kind { FEW_1x1, FEW_2x1, FEW_2x2, FEW_2x4, TILE_64, TILE_128, TILE_256 };
+
+Kind plan_linear(const LinearArgs &a, int w_bits) {
+    static const struct {
+        Kind kind;
+        int channels, rows;
+        double start, step, adapters;
+    } kFew[] = {{Kind::FEW_1x1, 16, 16, 0.9, 0.45, 2.5}, {Kind::FEW_2x1, 32, 16, 0.85, 0.8, 3.0},
+                {Kind::FEW_2x2, 32, 32, 1.4, 1.15, 4.0}, {Kind::FEW_2x4, 32, 64, 3.2, 1.95, 6.0}};
+    static const struct {
+        Kind kind;
+        int size, resident;
+        double start, steps8[4], steps4[4], adapters;
+    } kTiles[] = {{Kind::TILE_64, 64, 4, 2.0, {0.42, 0.55, 0.74, 0.9}, {0.45, 0.57, 0.76, 0.93}, 3.0},
+                  {Kind::TILE_128, 128, 2, 3.5, {0.75, 1.2}, {0.8, 1.22}, 5.0},
+                  {Kind::TILE_256, 256, 1, 6.0, {1.7}, {2.2}, 8.0}};
+    const auto on_cu = [&](int64_t channels, int64_t rows) {
+        return (((a.k + channels - 1) / channels) * ((a.m + rows - 1) / rows) + 255) / 256;
+    };
+    Kind best = Kind::TILE_64;
+    double best_us = 0;
+    const auto consider = [&](Kind kind, double us) {
+        if (best_us == 0 || us < best_us) best = kind, best_us = us;
+    };
+    for (const auto &f : kFew)
+        consider(f.kind, 1.5 + on_cu(f.channels, f.rows) * (f.start + f.step * (w_bits == 8 ? 1.2 : 1.0) * a.c / 1024.0 +
+                                                            (a.ad.count ? f.adapters : 0.0)));
+    for (const auto &t : kTiles) {
+        const int64_t n = on_cu(t.size, t.size), rest = n % t.resident;
+        const double *steps = w_bits == 8 ? t.steps8 : t.steps4;
+        const double step = (n / t.resident) * steps[t.resident - 1] + (rest ? steps[rest - 1] : 0.0);
+        const int64_t turns = (n + t.resident - 1) / t.resident;
+        consider(t.kind, t.start + a.steps * step + turns * (a.ad.count ? t.adapters : 0.0));
+    }
+    return best;
+}
+
 template <class T, int WB, bool AD>
-hipError_t many(const LinearArgs &a, hipStream_t stream) {
-    const int64_t big = (int64_t)((a.k + 255) / 256) * ((a.m + 255) / 256);
-    if (big >= 192) return tile<linear_tile<T, WB, 256, 256, 4, 2, AD>, 256, 256, 512>(a, stream);
-    return tile<linear_tile<T, WB, 128, 128, 2, 2, AD>, 128, 128, 256>(a, stream);
+hipError_t product(const LinearArgs &a, hipStream_t stream) {
+    switch (plan_linear(a, WB)) {
+        case Kind::FEW_1x1: return few<T, WB, 1, 1, AD>(a, stream);
+        case Kind::FEW_2x1: return few<T, WB, 2, 1, AD>(a, stream);
+        case Kind::FEW_2x2: return few<T, WB, 2, 2, AD>(a, stream);
+        case Kind::FEW_2x4: return few<T, WB, 2, 4, AD>(a, stream);
+        case Kind::TILE_64: return tile<linear_tile<T, WB, 64, 64, 1, 4, AD>, 64, 64, 256>(a, stream);
+        case Kind::TILE_128: return tile<linear_tile<T, WB, 128, 128, 2, 2, AD>, 128, 128, 256>(a, stream);
+        default: return tile<linear_tile<T, WB, 256, 256, 4, 2, AD>, 256, 256, 512>(a, stream);
+    }
 }
 
 template <class T, int RF>
 void rows(const LinearArgs &a, hipStream_t stream) {
     const int steps = (a.c + 31) / 32, per = (steps + a.ad.splits - 1) / a.ad.splits;
-    hipLaunchKernelGGL((adapter_rows<T, RF>), dim3((unsigned)((a.m + 15) / 16), (unsigned)a.ad.splits), dim3(512), 0,
+    hipLaunchKernelGGL((adapter_rows<T, RF>), dim3((unsigned)((a.m + 15) / 16), (unsigned)a.ad.splits),
+                       dim3(adapter_waves(RF) * 64), 0,
                        stream, a, per);
 }
 
@@ -55,22 +101,21 @@ hipError_t linear(const LinearArgs &a, hipStream_t stream) {
         else if (a.ad.rank <= 64) rows<T, 4>(a, stream);
         else rows<T, 8>(a, stream);
     }
-    hipError_t e;
-    if (a.m <= 16) e = few_channels<T, WB, 1>(a, stream);
-    else if (a.m <= 32) e = few_channels<T, WB, 2>(a, stream);
-    else if (a.m <= 64) e = few_channels<T, WB, 4>(a, stream);
-    else e = a.ad.count ? many<T, WB, true>(a, stream) : many<T, WB, false>(a, stream);
+    const hipError_t e = a.ad.count ? product<T, WB, true>(a, stream) : product<T, WB, false>(a, stream);
     return e != hipSuccess ? e : hipGetLastError();
 }
 
 }  // namespace
 
 int linear_adapter_splits(int64_t m, int64_t c) {
-    // about 128 workgroups of 16 rows, each with a step of 32 channels for every wave
+    // about 256 workgroups of 16 rows, with eight steps of 32 channels each at least;
+    // fewer partial sums for more rows, since every workgroup of the product adds them
     const int64_t tiles = (m + 15) / 16, steps = (c + 31) / 32;
-    int64_t splits = 128 / tiles;
+    int64_t splits = 256 / tiles;
+    const int64_t most = m <= 64 ? 16 : m <= 512 ? 1024 / m : 2;
+    if (splits > most) splits = most;
     if (splits > (steps + 7) / 8) splits = (steps + 7) / 8;
-    return (int)(splits < 1 ? 1 : splits > 16 ? 16 : splits);
+    return (int)(splits < 1 ? 1 : splits);
 }
 
 hipError_t launch_linear(const LinearArgs &a, int w_bits, int dtype, hipStream_t stream) {

@@ -86,7 +86,7 @@ def _lib():
 
 
 def _matrix(t: torch.Tensor, name: str, dtypes=(torch.bfloat16, torch.float16)) -> None:
-    if t.dim() != 2 or t.dtype not in dtypes:
+    if t.dtype not in dtypes or t.dim() != 2:
         raise QConvError(EINVAL, f"{name} must be a matrix of {' or '.join(str(d).split('.')[1] for d in dtypes)}")
     if not t.is_cuda:
         raise QConvError(EINVAL, f"{name} must be a device tensor")
@@ -101,22 +101,24 @@ def _ld(t: torch.Tensor) -> int:
 
 def _rows_arg(r: Rows, name: str, device: torch.device) -> QConvRows:
     codes, scale, channels, bits = r
-    four = bits == 4
-    if codes.dim() != 2 or codes.dtype is not (torch.int32 if four else torch.int8):
-        raise QConvError(EINVAL, f"{name}.codes must be a matrix of {'int32 words' if four else 'int8'}")
+    if codes.dim() != 2 or codes.dtype is not (torch.int32 if bits == 4 else torch.int8):
+        raise QConvError(EINVAL, f"{name}.codes must be a matrix of {'int32 words' if bits == 4 else 'int8'}")
     m, width = codes.shape
-    size = 4 if four else 1
-    if width > 1 and codes.stride(1) != 1:
+    pitch, step = codes.stride()
+    if width > 1 and step != 1:
         raise QConvError(EINVAL, f"{name}.codes: the codes of a row must be contiguous")
-    if width * size < (int(channels) * (4 if four else 8) // 8 + 15) // 16 * 16:
-        raise QConvError(EINVAL, f"{name}.codes: rows of {width * size} bytes do not hold {channels} channels in "
-                                 "whole 16-byte vectors")
-    if scale.dtype is not torch.float32 or scale.dim() != 1 or scale.shape[0] != m or not scale.is_contiguous():
+    if m < 2:
+        pitch = width
+    if bits == 4:
+        width, pitch = width * 4, pitch * 4
+    if width < (channels * bits // 8 + 15) // 16 * 16:
+        raise QConvError(EINVAL, f"{name}.codes: rows of {width} bytes do not hold {channels} channels in whole "
+                                 "16-byte vectors")
+    if scale.dtype is not torch.float32 or scale.shape != (m,) or not scale.is_contiguous():
         raise QConvError(EINVAL, f"{name}.scale must be one float32 for each row")
-    if codes.device != device or scale.device != device:
+    if codes.get_device() != device.index or scale.get_device() != device.index:
         raise QConvError(EINVAL, f"{name} must be on {device}")
-    pitch = codes.stride(0) * size if m > 1 else width * size
-    return QConvRows(codes.data_ptr(), scale.data_ptr(), pitch, m, int(channels), int(bits))
+    return QConvRows(codes.data_ptr(), scale.data_ptr(), pitch, m, channels, bits)
 
 
 def _on(device: torch.device, out: torch.Tensor | None, shape: tuple, dtype: torch.dtype, name: str) -> torch.Tensor:
@@ -155,7 +157,7 @@ def _stream(stream, device: torch.device) -> int:
 
 def _call(device: torch.device, fn, *args) -> int:
     """fn on the tensors' device (a launch goes to the current one)."""
-    if torch.cuda.current_device() == device.index:
+    if torch._C._cuda_getDevice() == device.index:
         return fn(*args)
     with torch.cuda.device(device):
         return fn(*args)
@@ -168,17 +170,21 @@ def rows_pitch(channels: int) -> int:
 
 def quantize_rows(x: torch.Tensor, out: Rows | None = None, stream=None) -> Rows:
     """Rows of bfloat16, float16 or float32 to 8 bits (qconv_quantize_rows)."""
-    _matrix(x, "x", (torch.bfloat16, torch.float16, torch.float32))
+    _matrix(x, "x", tuple(DTYPES))
     m, c = x.shape
     device = x.device
     if out is None:
-        out = Rows(torch.empty((m, rows_pitch(c)), dtype=torch.int8, device=device),
-                   torch.empty(m, dtype=torch.float32, device=device), c)
-    elif out.bits != 8 or out.channels != c or out.codes.shape[0] != m:
-        raise QConvError(EINVAL, f"out must be 8-bit rows, {m} of {c} channels")
-    r = _rows_arg(out, "out", device)
-    L = _lib()
-    _check(_call(device, L.qconv_quantize_rows, x.data_ptr(), DTYPES[x.dtype], _ld(x), m, c, r.codes, r.pitch, r.scale,
+        pitch = rows_pitch(c)
+        codes, scale = torch.empty((m, pitch), dtype=torch.int8, device=device), torch.empty(m, device=device,
+                                                                                            dtype=torch.float32)
+        out = Rows(codes, scale, c)
+        to = (codes.data_ptr(), pitch, scale.data_ptr())
+    else:
+        if out.bits != 8 or out.channels != c or out.codes.shape[0] != m:
+            raise QConvError(EINVAL, f"out must be 8-bit rows, {m} of {c} channels")
+        r = _rows_arg(out, "out", device)
+        to = (r.codes, r.pitch, r.scale)
+    _check(_call(device, _lib().qconv_quantize_rows, x.data_ptr(), DTYPES[x.dtype], _ld(x), m, c, *to,
                  _stream(stream, device)), "qconv_quantize_rows")
     return out
 
@@ -198,19 +204,21 @@ def pack_rows4(codes: torch.Tensor, scale: torch.Tensor, stream=None) -> Rows:
 
 
 def _adapters_arg(ad: Adapters, row_adapter, m: int, c: int, k: int, dtype, device) -> QConvAdapters:
-    n, rank = ad.a.shape[0], ad.a.shape[1] if ad.a.dim() == 3 else 0
-    if tuple(ad.a.shape) != (n, rank, c) or tuple(ad.b.shape) != (n, k, rank):
+    a, b, alpha = ad
+    n, rank = a.shape[:2] if a.dim() == 3 else (0, 0)
+    if a.shape != (n, rank, c) or b.shape != (n, k, rank):
         raise QConvError(EINVAL, f"adapters: a must be n x rank x {c} and b n x {k} x rank")
-    if ad.a.dtype is not dtype or ad.b.dtype is not dtype:
+    if a.dtype is not dtype or b.dtype is not dtype:
         raise QConvError(EINVAL, f"adapters: a and b must be of y's type, {dtype}")
-    if ad.alpha.dtype is not torch.float32 or tuple(ad.alpha.shape) != (n,):
+    if alpha.dtype is not torch.float32 or alpha.shape != (n,):
         raise QConvError(EINVAL, "adapters: alpha must be one float32 for each adapter")
-    if row_adapter is None or row_adapter.dtype is not torch.int32 or tuple(row_adapter.shape) != (m,):
+    if row_adapter is None or row_adapter.dtype is not torch.int32 or row_adapter.shape != (m,):
         raise QConvError(EINVAL, "row_adapter must be one int32 for each row of x")
-    for t, name in ((ad.a, "a"), (ad.b, "b"), (ad.alpha, "alpha"), (row_adapter, "row_adapter")):
-        if t.device != device or not t.is_contiguous():
-            raise QConvError(EINVAL, f"adapters: {name} must be contiguous and on {device}")
-    return QConvAdapters(ad.a.data_ptr(), ad.b.data_ptr(), ad.alpha.data_ptr(), row_adapter.data_ptr(), n, rank)
+    on = device.index
+    for t in (a, b, alpha, row_adapter):
+        if t.get_device() != on or not t.is_contiguous():
+            raise QConvError(EINVAL, f"adapters: a, b, alpha and row_adapter must be contiguous and on {device}")
+    return QConvAdapters(a.data_ptr(), b.data_ptr(), alpha.data_ptr(), row_adapter.data_ptr(), n, rank)
 
 
 def linear(x: Rows, w: Rows, *, dtype: torch.dtype = torch.bfloat16, adapters: Adapters | None = None,
