@@ -177,10 +177,10 @@ __device__ __forceinline__ uint2 widen8(uint32_t v) {
     return uint2{__builtin_amdgcn_perm(odd, even, 0x05010400u), __builtin_amdgcn_perm(odd, even, 0x07030602u)};
 }
 
-// Up to four results from one row, `left` of them within it.
-__device__ __forceinline__ void store4(float *out, f32x4 d, int left, bool vec) {
-    if (vec && left >= 4) {
-        *reinterpret_cast<f32x4 *>(out) = d;
+// Up to `left` of four results from one row; whole ones in one store, of any alignment.
+__device__ __forceinline__ void store4(float *out, f32x4 d, int left) {
+    if (left >= 4) {
+        __builtin_memcpy(out, &d, 16);
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -188,9 +188,10 @@ __device__ __forceinline__ void store4(float *out, f32x4 d, int left, bool vec) 
     }
 }
 template <class T>
-__device__ __forceinline__ void store4(typename T::elem *out, f32x4 d, int left, bool vec) {
-    if (vec && left >= 4) {
-        *reinterpret_cast<uint2 *>(out) = uint2{pack2<T>(d[0], d[1]), pack2<T>(d[2], d[3])};
+__device__ __forceinline__ void store4(typename T::elem *out, f32x4 d, int left) {
+    if (left >= 4) {
+        const uint2 w{pack2<T>(d[0], d[1]), pack2<T>(d[2], d[3])};
+        __builtin_memcpy(out, &w, 8);
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)

@@ -45,7 +45,8 @@ __device__ __forceinline__ int adapter_of(const LinearArgs &a, int row) {
 // rows and a run of 32-channel steps.  The adapters that the rows name are dealt
 // to its waves, and where they are fewer than the waves, several waves share one,
 // each with a run of its steps (so that a wave's loads lie side by side in A's rows),
-// and all loads of A are in flight at once whether the rows agree or not.  A wave multiplies its adapter's A (RF fragments of
+// and all loads of A are in flight at once whether the rows agree or not; where there
+// are few such workgroups, the adapters are dealt to several of them first (grid z).  A wave multiplies its adapter's A (RF fragments of
 // 16 ranks) by all rows and keeps the rows that asked for it.  Bound by reading A.
 constexpr int adapter_waves(int rf) { return rf == 8 ? 8 : 16; }
 template <class T, int RF>
@@ -59,10 +60,15 @@ __global__ void __launch_bounds__(adapter_waves(RF) * 64) adapter_rows(LinearArg
     const int begin = (int)blockIdx.y * steps_per_split, end = min(begin + steps_per_split, all);
     const int id = adapter_of(a, row);
     const uint32_t named = (uint32_t)__ballot(id >= 0) & 0xffffu;
-    int distinct = 0;
-    for (uint32_t left = named; left && distinct < kWaves; ++distinct) next_adapter(left, id);
+    // the n-th adapter that the rows name is for workgroup z = n mod Z of this place
+    const int Z = (int)gridDim.z, z = (int)blockIdx.z;
+    int distinct = 0, own = -1;
+    for (uint32_t left = named; left; ++distinct)
+        if (next_adapter(left, id) == id) own = distinct;
+    const int here = (distinct - z + Z - 1) / Z;
+    if (here <= 0) return;
     int classes = 1;
-    while (classes < distinct) classes *= 2;
+    while (classes < here && classes < kWaves) classes *= 2;
     const int mine = wave & (classes - 1), share = kWaves / classes;
     const int run = (end - begin + share - 1) / share, first = begin + wave / classes * run, last = min(first + run, end);
     const __amdgpu_buffer_rsrc_t rx = range_of(a.x.codes + (int64_t)row0 * a.x.pitch,
@@ -73,7 +79,7 @@ __global__ void __launch_bounds__(adapter_waves(RF) * 64) adapter_rows(LinearArg
     int n = 0;
     for (uint32_t left = named; left; ++n) {
         const int ad = next_adapter(left, id);
-        if ((n & (classes - 1)) != mine) continue;
+        if (n % Z != z || (n / Z & (classes - 1)) != mine) continue;
         // A's rows past the rank lie past the range, and load as zeros
         const __amdgpu_buffer_rsrc_t ra = range_of(
             static_cast<const typename T::elem *>(a.ad.a) + (int64_t)ad * a.ad.rank * a.c, (int64_t)a.ad.rank * a.c * 2);
@@ -115,7 +121,7 @@ __global__ void __launch_bounds__(adapter_waves(RF) * 64) adapter_rows(LinearArg
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) t += part[w][f][lane];
         const int rank = f * 16 + g * 4;
-        if (row < a.m && rank < a.ad.rank)
+        if (own >= 0 && own % Z == z && rank < a.ad.rank)   // (rows without an adapter have no u)
             *reinterpret_cast<f32x4 *>(a.ad.u + ((int64_t)blockIdx.y * a.m + row) * a.ad.rank + rank) = t;
     }
 }
@@ -351,7 +357,7 @@ __global__ void __launch_bounds__(512) linear_few(LinearArgs a) {
         if constexpr (AD)
 #pragma unroll
             for (int p = 0; p < kParts; ++p) y += extra[p * FI + f][j][lane];
-        store4<T>(static_cast<typename T::elem *>(a.y) + (int64_t)row * a.ldy + ch, y, a.k - ch, a.vec);
+        store4<T>(static_cast<typename T::elem *>(a.y) + (int64_t)row * a.ldy + ch, y, a.k - ch);
     }
 }
 
@@ -572,9 +578,9 @@ __global__ void __launch_bounds__(WJ *WI * 64) linear_tile(LinearArgs a) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const f32x4 lo = d[2 * h][i] * up, hi = d[2 * h + 1][i] * up;
-            if (a.vec && ch + 8 * h + 8 <= a.k) {
-                *reinterpret_cast<uint4 *>(out + 8 * h) = uint4{pack2<T>(lo[0], lo[1]), pack2<T>(lo[2], lo[3]),
-                                                                pack2<T>(hi[0], hi[1]), pack2<T>(hi[2], hi[3])};
+            if (ch + 8 * h + 8 <= a.k) {
+                const u32x4_t w{pack2<T>(lo[0], lo[1]), pack2<T>(lo[2], lo[3]), pack2<T>(hi[0], hi[1]), pack2<T>(hi[2], hi[3])};
+                __builtin_memcpy(out + 8 * h, &w, 16);   // of any alignment
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)

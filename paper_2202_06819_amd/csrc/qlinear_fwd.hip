@@ -1,4 +1,6 @@
 // Launches of the projection with adapters.
+#include <algorithm>
+
 #include "qlinear_fwd.h"
 
 namespace qconv {
@@ -87,10 +89,10 @@ hipError_t product(const LinearArgs &a, hipStream_t stream) {
 
 template <class T, int RF>
 void rows(const LinearArgs &a, hipStream_t stream) {
-    const int steps = (a.c + 31) / 32, per = (steps + a.ad.splits - 1) / a.ad.splits;
-    hipLaunchKernelGGL((adapter_rows<T, RF>), dim3((unsigned)((a.m + 15) / 16), (unsigned)a.ad.splits),
-                       dim3(adapter_waves(RF) * 64), 0,
-                       stream, a, per);
+    const int steps = (a.c + 31) / 32, per = (steps + a.ad.splits - 1) / a.ad.splits, tiles = (a.m + 15) / 16;
+    const int z = std::min({256 / (tiles * a.ad.splits) + 1, a.ad.count, 4});
+    hipLaunchKernelGGL((adapter_rows<T, RF>), dim3((unsigned)tiles, (unsigned)a.ad.splits, (unsigned)z),
+                       dim3(adapter_waves(RF) * 64), 0, stream, a, per);
 }
 
 template <class T, int WB>

@@ -63,8 +63,9 @@ __device__ __forceinline__ typename T::v8 read_transposed(const uint8_t *lds, in
 }
 
 // Three LDS buffers of 64 rows of t: one is multiplied, one has landed, one is on its
-// way.  8-bit codes, and p where its rows are whole aligned vectors (COPY), go straight
-// from memory to LDS; 4-bit codes (widened to bytes) and any other p go through
+// way (five, in the smallest tile, made no step shorter: its steps are bound by their
+// instructions).  8-bit codes, and p where its rows are whole aligned vectors (COPY), go
+// straight from memory to LDS; 4-bit codes (widened to bytes) and any other p go through
 // registers a step ahead.  Codes are read by transposing loads, 8 rows of one column a
 // lane, and converted on their way to the matrix cores.  A matrix instruction of 16
 // cycles hides two vector instructions of a wave (measured: three cost a quarter more,
@@ -84,6 +85,7 @@ __device__ __forceinline__ uint32_t scaled_pair(uint32_t w, int half, float s0, 
     return pack2<T>((float)(int8_t)(w >> (16 * half)) * s0, (float)(int8_t)(w >> (16 * half + 8)) * s1);
 }
 
+constexpr int kGradStages = 3;
 template <class T, int WB, bool TRANSPOSED, bool COPY, int TJ, int TI, int WJ, int WI>
 __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
     constexpr int FJ = TJ / (16 * WJ), FI = TI / (16 * WI), kThreads = WJ * WI * 64, kWaves = kThreads / 64;
@@ -108,22 +110,35 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
 
     const u32x4_t rp_rows = range_words(p + (int64_t)i0 * a.ldp, ((int64_t)(a.ni - 1 - i0) * a.ldp + a.nt) * 2);
     // copy n of step s: the codes', p's, then the scales (every wave copies the same
-    // ones to the same place, so that all have the same copies to wait for)
+    // ones to the same place, so that all have the same copies to wait for).  A Step
+    // holds where its rows of t begin; it moves on by addition (the scalar instructions
+    // of finding it anew were most of a small tile's step).
     struct Step {
+        uint64_t codes, p, scale;
+        int rows;   // of t, from here on
+    };
+    const int codes_step = 64 * (int)a.b.pitch, p_step = 64 * (int)a.ldp * 2;
+    const int codes_last = a.b.used - j0, p_last = (a.ni - i0) * 2;   // bytes in reach of a step's last row
+    Step place{(uint64_t)(a.b.codes + (int64_t)s0 * 64 * a.b.pitch + j0), (uint64_t)(p + (int64_t)s0 * 64 * a.ldp + i0),
+               (uint64_t)(a.b.scale + s0 * 64), a.nt - s0 * 64};
+    const auto move_on = [&] {
+        place.codes += codes_step;
+        if (TRANSPOSED) place.p += p_step;
+        place.scale += 256;
+        place.rows -= 64;
+    };
+    struct Words {
         u32x4_t codes, p, scale;
     };
-    auto step_of = [&](int s) {   // (a step's rows of t: 32-bit ranges from 64-bit bases)
-        const int t0 = s * 64, rows = min(a.nt - t0, 64);
-        Step q;
-        q.codes = range_words(a.b.codes + (int64_t)t0 * a.b.pitch + j0,
-                              rows > 0 ? (rows - 1) * (int)a.b.pitch + a.b.used - j0 : 0);
-        q.p = !TRANSPOSED ? rp_rows
-                                    : range_words(p + (int64_t)t0 * a.ldp + i0,
-                                                  rows > 0 ? ((rows - 1) * (int)a.ldp + a.ni - i0) * 2 : 0);
-        q.scale = range_words(a.b.scale + t0, rows > 0 ? rows * 4 : 0);
+    const auto words_here = [&] {
+        const int rows = min(place.rows, 64), before = rows - 1;
+        Words q;
+        q.codes = range_words((const void *)place.codes, rows > 0 ? before * (int)a.b.pitch + codes_last : 0);
+        q.p = !TRANSPOSED ? rp_rows : range_words((const void *)place.p, rows > 0 ? before * (int)a.ldp * 2 + p_last : 0);
+        q.scale = range_words((const void *)place.scale, rows > 0 ? rows * 4 : 0);
         return q;
     };
-    auto copy = [&](int n, int s, const Step &q, uint8_t *buf) {
+    auto copy = [&](int n, int s, const Words &q, uint8_t *buf) {
         if (n < kCodeCopies) {
             const int at = (n * kWaves + wave) * 1024 + lane * 16, t = at / TJ, in = at % TJ;
             const int col = ((in >> 4) ^ code_unit_of<TJ>(t)) << 4;
@@ -149,7 +164,7 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
     // What goes through registers: units of 16 bytes of LDS, each from one load (p's of
     // any alignment).  A unit past the matrix is loaded from within it and put right
     // when it is stored, so that the loads of a step are always as many.
-    constexpr int kFetches = kCodeUnits + kPUnits;
+    constexpr int kFetches = kCodeUnits + kPUnits, kStages = kGradStages;
     uint2 code_unit[kCodeUnits ? kCodeUnits : 1];
     u32x4_t p_unit[kPUnits ? kPUnits : 1];
     const int p_rows = TRANSPOSED ? a.nt : a.ni, p_count = TRANSPOSED ? a.ni : a.nt;   // p as it lies in memory
@@ -222,12 +237,6 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
             }
         }
     };
-    // waits for all copies, not for the fetches issued after them
-    auto copies_landed = [&] {
-        if (kFetches > 0 && !narrow) copies_left<kFetches>();
-        else copies_left<0>();
-    };
-
     const int jrow0 = (wave / WI) * 16 * FJ, irow0 = (wave % WI) * FI * 16;
     const int r = lane & 15, g = lane >> 4;
     f32x4 acc[FJ][FI];
@@ -302,19 +311,24 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
         for (int f = 0; f < kAhead; ++f) ahead[f] = y[FI + f];
     };
 #pragma unroll
-    for (int n = 0; n < kCopies; ++n) copy(n, s0, step_of(s0), smem);
+    for (int m = 0; m < kStages - 1; ++m) {
+        const Words q = words_here();
 #pragma unroll
-    for (int n = 0; n < kCopies; ++n) copy(n, s0 + 1, step_of(s0 + 1), smem + kStage);
-    if constexpr (kFetches > 0) {
-        fetch(s0);
-        put(s0, smem);
-        fetch(s0 + 1);
-        put(s0 + 1, smem + kStage);
-        fetch(s0 + 2);
-        copies_landed();
-    } else {
-        copies_left<kCopies>();
+        for (int n = 0; n < kCopies; ++n) copy(n, s0 + m, q, smem + m * kStage);
+        move_on();
     }
+    if constexpr (kFetches > 0) {
+#pragma unroll
+        for (int m = 0; m < kStages - 1; ++m) {
+            fetch(s0 + m);
+            put(s0 + m, smem + m * kStage);
+        }
+        copies_left<0>();
+        fetch(s0 + kStages - 1);
+    } else {
+        copies_left<kCopies *(kStages - 2)>();
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     u32x4_t x[FJ];
@@ -332,21 +346,25 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
     }
     int at = 0;
     for (int s = s0; s < s1; ++s) {
-        const int after = at + 1 == 3 ? 0 : at + 1, fill = after + 1 == 3 ? 0 : after + 1;
-        uint8_t *cur = smem + at * kStage, *then = smem + after * kStage, *third = smem + fill * kStage;
+        const int after = at + 1 == kStages ? 0 : at + 1, fill = at == 0 ? kStages - 1 : at - 1;
+        uint8_t *cur = smem + at * kStage, *then = smem + after * kStage, *last = smem + fill * kStage;
         half(cur, 0, cur, x, ahead, [](int) {});
-        // the next step's copies have landed, and everyone is done with the step
-        // before this one
-        copies_landed();
+        // The next step's copies have landed (each step issues its copies and then its
+        // fetches: all that came later may be on the way), and everyone is done with
+        // the step before this one.
+        if (kFetches > 0 && narrow) copies_left<0>();
+        else copies_left<kFetches + (kStages - 3) * (kCopies + kFetches)>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         // (past the last step these go to a buffer that is not multiplied)
-        const Step q = step_of(s + 2);
+        const int far = s + kStages - 1;
+        const Words q = words_here();
+        move_on();
         half(cur, 1, then, x, ahead, [&](int i) {
 #pragma unroll
-            for (int n = i * kCopies / FI; n < (i + 1) * kCopies / FI; ++n) copy(n, s + 2, q, third);
-            if (i == 0) put(s + 2, third);
-            if (i == FI - 1) fetch(s + 3);
+            for (int n = i * kCopies / FI; n < (i + 1) * kCopies / FI; ++n) copy(n, far, q, last);
+            if (i == 0) put(far, last);
+            if (i == FI - 1) fetch(far + 1);
         });
         at = after;
     }
@@ -363,9 +381,9 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
                 if (col < a.ldpart)
                     *reinterpret_cast<f32x4 *>(a.part + ((int64_t)split * a.ni + row) * a.ldpart + col) = d;
             } else if constexpr (TRANSPOSED) {
-                store4(static_cast<float *>(a.out) + (int64_t)row * a.ldo + col, d, a.nj - col, a.vec_out);
+                store4(static_cast<float *>(a.out) + (int64_t)row * a.ldo + col, d, a.nj - col);
             } else {
-                store4<T>(static_cast<elem *>(a.out) + (int64_t)row * a.ldo + col, d, a.nj - col, a.vec_out);
+                store4<T>(static_cast<elem *>(a.out) + (int64_t)row * a.ldo + col, d, a.nj - col);
             }
         }
     }

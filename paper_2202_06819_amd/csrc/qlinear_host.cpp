@@ -160,7 +160,7 @@ int qconv_quantize_rows(const void *x, int32_t dtype, int64_t ldx, int32_t m, in
     const Span in(x, strided_bytes(m, c, ldx, size)), out(codes, strided_bytes(m, round16(c), pitch, 1)),
         sc(scale, (int64_t)m * 4);
     if (in.meets(out) || in.meets(sc) || out.meets(sc)) return fail(QCONV_EINVAL, "x, codes and scale must not overlap");
-    const QuantizeArgs a{x, ldx, static_cast<uint8_t *>(codes), pitch, scale, m, c, wide_rows(x, ldx, size, 16)};
+    const QuantizeArgs a{x, ldx, static_cast<uint8_t *>(codes), pitch, scale, m, c};
     const hipError_t e = launch_quantize_rows(a, dtype, (hipStream_t)stream);
     if (e != hipSuccess) return fail(QCONV_EHIP, "quantiser launch: %s", hipGetErrorString(e));
     return QCONV_OK;
@@ -205,7 +205,6 @@ int qconv_linear(const qconv_rows *x, const qconv_rows *w, const qconv_adapters 
     a.c = x->channels;
     a.k = w->rows;
     a.steps = (x->channels + 127) / 128;
-    a.vec = wide_rows(y, ldy, 2, 16);
     if (adapters && adapters->count) {
         const int64_t n = adapters->count, r = adapters->rank;
         for (const Span &s : {Span(adapters->a, n * r * a.c * 2), Span(adapters->b, n * r * a.k * 2),
@@ -249,7 +248,6 @@ int qconv_linear_grad_input(const void *dy, int32_t dtype, int64_t lddy, int32_t
     a.nj = w->channels;
     a.nt = w->rows;
     a.vec_p = wide_rows(dy, lddy, 2, 16);
-    a.vec_out = wide_rows(dx, lddx, 2, 16);
     return run_grad(a, false, w->bits, dtype, 2, w, workspace, workspace_bytes, stream);
 }
 
@@ -273,7 +271,6 @@ int qconv_linear_grad_weight(const void *dy, int32_t dtype, int64_t lddy, int32_
     a.nj = x->channels;
     a.nt = x->rows;
     a.vec_p = wide_rows(dy, lddy, 2, 16);
-    a.vec_out = wide_rows(dw, lddw, 4, 16);
     return run_grad(a, true, 8, dtype, 4, x, workspace, workspace_bytes, stream);
 }
 

@@ -26,7 +26,6 @@ struct QuantizeArgs {
     int64_t pitch;
     float *scale;
     int32_t m, c;
-    int32_t vec;         // rows of x start on 16-byte boundaries
 };
 
 struct AdapterArgs {
@@ -44,7 +43,6 @@ struct LinearArgs {
     int64_t ldy;         // elements from row to row
     int32_t m, c, k;
     int32_t steps;       // 128-channel steps
-    int32_t vec;         // rows of y start on 16-byte boundaries
     int32_t tiles_j, tiles_i;
     AdapterArgs ad;
 };
@@ -61,7 +59,6 @@ struct GradArgs {
     int64_t ldpart;
     int32_t ni, nj, nt;
     int32_t vec_p;       // rows of p start on 16-byte boundaries
-    int32_t vec_out;     // rows of out start on 16-byte boundaries
     int32_t tiles_i, tiles_j;
     int32_t splits, steps_per_split, steps;
 };
