@@ -506,9 +506,9 @@ int qconv2d_scheduled(const qconv_desc *d, const void *x, const void *w_prepared
  *   weight gradient   dw[k][c] = sum_m dy[m][k] x[m][c]
  * Conventions as above: device pointers, nothing allocated or kept, work
  * enqueued on `stream`, arguments checked before anything is enqueued.
- * Reading a view is allowed throughout (row strides in elements), and no
- * alignment beyond the element's is asked of x, y, dy, dx and dw; aligned rows
- * (16 bytes) are read and written in wider accesses.
+ * Views are allowed throughout (row strides in elements), and no alignment
+ * beyond the element's is asked of x, y, dy, dx and dw; a dy whose rows start on
+ * 16-byte boundaries and hold a multiple of 8 values is read the fastest way.
  */
 #define QCONV_BF16 0
 #define QCONV_F16 1
@@ -562,7 +562,8 @@ int qconv_quantize_rows(const void *x, int32_t dtype, int64_t ldx, int32_t m, in
  *   alpha   DEVICE, count floats;  row: DEVICE, int32 for each row of x
  *   rank    a multiple of 8 up to 128; c % 8 == 0
  * u is kept in 32 bits between the two products and rounded once to y's type
- * for the second, relative to its row's largest value.
+ * for the second (f16: after scaling its row by a power of two, so that only y
+ * itself can overflow).
  */
 typedef struct qconv_adapters {
     const void *a, *b;

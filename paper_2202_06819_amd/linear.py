@@ -121,11 +121,20 @@ def _rows_arg(r: Rows, name: str, device: torch.device) -> QConvRows:
     return QConvRows(codes.data_ptr(), scale.data_ptr(), pitch, m, channels, bits)
 
 
-def _on(device: torch.device, out: torch.Tensor | None, shape: tuple, dtype: torch.dtype, name: str) -> torch.Tensor:
+def _used_on(t: torch.Tensor, stream) -> torch.Tensor:
+    """A tensor that the call made on the current stream's pool and uses on ``stream``."""
+    if stream is not None:
+        t.record_stream(stream if isinstance(stream, torch.cuda.Stream)
+                        else torch.cuda.ExternalStream(int(stream), device=t.device))
+    return t
+
+
+def _on(device: torch.device, out: torch.Tensor | None, shape: tuple, dtype: torch.dtype, name: str,
+        stream) -> torch.Tensor:
     """The output: new, or the caller's after a check."""
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    if tuple(out.shape) != shape or out.dtype is not dtype or out.device != device:
+        return _used_on(torch.empty(shape, dtype=dtype, device=device), stream)
+    if out.shape != shape or out.dtype is not dtype or out.device != device:
         raise QConvError(EINVAL, f"{name} must be {shape} of {dtype} on {device}")
     if shape[1] > 1 and out.stride(1) != 1:
         raise QConvError(EINVAL, f"{name}: the columns of a row must be contiguous")
@@ -134,18 +143,14 @@ def _on(device: torch.device, out: torch.Tensor | None, shape: tuple, dtype: tor
 
 def _workspace(need: int, workspace: torch.Tensor | None, device: torch.device, stream):
     """(tensor to keep, pointer, bytes) of the call's scratch: the caller's, or
-    from torch's allocator, which keeps it for the stream it is used on."""
+    from torch's allocator."""
     if workspace is not None:
         if workspace.device != device or not workspace.is_contiguous():
             raise QConvError(EINVAL, f"workspace must be contiguous and on {device}")
         return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
     if not need:
         return None, None, 0
-    t = torch.empty(need, dtype=torch.uint8, device=device)
-    if isinstance(stream, torch.cuda.Stream):
-        t.record_stream(stream)
-    elif stream is not None:
-        t.record_stream(torch.cuda.ExternalStream(int(stream), device=device))
+    t = _used_on(torch.empty(need, dtype=torch.uint8, device=device), stream)
     return t, t.data_ptr(), need
 
 
@@ -175,8 +180,8 @@ def quantize_rows(x: torch.Tensor, out: Rows | None = None, stream=None) -> Rows
     device = x.device
     if out is None:
         pitch = rows_pitch(c)
-        codes, scale = torch.empty((m, pitch), dtype=torch.int8, device=device), torch.empty(m, device=device,
-                                                                                            dtype=torch.float32)
+        codes = _used_on(torch.empty((m, pitch), dtype=torch.int8, device=device), stream)
+        scale = _used_on(torch.empty(m, dtype=torch.float32, device=device), stream)
         out = Rows(codes, scale, c)
         to = (codes.data_ptr(), pitch, scale.data_ptr())
     else:
@@ -242,7 +247,7 @@ def linear(x: Rows, w: Rows, *, dtype: torch.dtype = torch.bfloat16, adapters: A
         ad = ctypes.byref(ad)
     elif row_adapter is not None:
         raise QConvError(EINVAL, "row_adapter without adapters")
-    y = _on(device, out, (rx.rows, rw.rows), dtype, "out")
+    y = _on(device, out, (rx.rows, rw.rows), dtype, "out", stream)
     keep, ws, ws_bytes = _workspace(need, workspace, device, stream)
     _check(_call(device, L.qconv_linear, ctypes.byref(rx), ctypes.byref(rw), ad, y.data_ptr(), DTYPES[dtype], _ld(y), ws,
                  ws_bytes, _stream(stream, device)), "qconv_linear")
@@ -278,7 +283,7 @@ def linear_grad_input(dy: torch.Tensor, w: Rows, *, out: torch.Tensor | None = N
     m = dy.shape[0]
     if dy.shape[1] != rw.rows:
         raise QConvError(EINVAL, f"dy has {dy.shape[1]} columns, w {rw.rows} rows")
-    dx = _on(device, out, (m, rw.channels), dy.dtype, "out")
+    dx = _on(device, out, (m, rw.channels), dy.dtype, "out", stream)
     keep, ws, ws_bytes = _workspace(grad_workspace_bytes(m, rw.channels, rw.rows), workspace, device, stream)
     _check(_call(device, _lib().qconv_linear_grad_input, dy.data_ptr(), DTYPES[dy.dtype], _ld(dy), m, ctypes.byref(rw),
                  dx.data_ptr(), _ld(dx), ws, ws_bytes, _stream(stream, device)), "qconv_linear_grad_input")
@@ -295,7 +300,7 @@ def linear_grad_weight(dy: torch.Tensor, x: Rows, *, out: torch.Tensor | None = 
     m, k = dy.shape
     if m != rx.rows:
         raise QConvError(EINVAL, f"dy has {m} rows, x {rx.rows}")
-    dw = _on(device, out, (k, rx.channels), torch.float32, "out")
+    dw = _on(device, out, (k, rx.channels), torch.float32, "out", stream)
     keep, ws, ws_bytes = _workspace(grad_workspace_bytes(k, rx.channels, m), workspace, device, stream)
     _check(_call(device, _lib().qconv_linear_grad_weight, dy.data_ptr(), DTYPES[dy.dtype], _ld(dy), k, ctypes.byref(rx),
                  dw.data_ptr(), _ld(dw), ws, ws_bytes, _stream(stream, device)), "qconv_linear_grad_weight")
@@ -314,6 +319,7 @@ class _LinearLayer(torch.autograd.Function):
         return linear(x8, w8, dtype=x.dtype)
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         x_codes, x_scale, w_codes, w_scale = ctx.saved_tensors
         if dy.shape[1] > 1 and dy.stride(1) != 1 or dy.stride(0) < dy.shape[1]:

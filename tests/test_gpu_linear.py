@@ -510,3 +510,17 @@ def test_refusals_of_tensors(L):
         with pytest.raises(L.QConvError):
             call()
             pytest.fail(f"case {i} was accepted")
+
+
+# ------------------------------------------------------------------- example
+
+def test_demo_trains_and_serves():
+    """The operators together: the loss falls, half the bytes are kept, and the
+    served block is the 64-bit one but for the two 8-bit roundings of its
+    activations (each at most half a step of 1/64 of a row's largest, so about 1 %
+    of a normal row) and bfloat16."""
+    from paper_2202_06819_amd import linear_demo
+    got = linear_demo.main(width=128, hidden=256, rows=512, steps=30)
+    assert got["last_loss"] < 0.8 * got["first_loss"]
+    assert got["kept_bytes"] < 0.55 * got["bytes_in_16_bits"]
+    assert got["serving_error"] < 0.05
