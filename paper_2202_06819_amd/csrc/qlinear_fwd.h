@@ -41,30 +41,51 @@ __device__ __forceinline__ int adapter_of(const LinearArgs &a, int row) {
 }
 
 // Partial sums of u over one of `splits` runs of channels, without the row
-// scale: sum of codes times A for the row's own adapter.  A workgroup takes 16
-// rows and a run of 32-channel steps.  The adapters that the rows name are dealt
+// scale: sum of codes times A for the row's own adapter.  A workgroup takes 16 NI
+// rows (NI 2: an A that is read serves twice the rows) and a run of 32-channel steps.  The adapters that the rows name are dealt
 // to its waves, and where they are fewer than the waves, several waves share one,
 // each with a run of its steps (so that a wave's loads lie side by side in A's rows),
 // and all loads of A are in flight at once whether the rows agree or not; where there
 // are few such workgroups, the adapters are dealt to several of them first (grid z).  A wave multiplies its adapter's A (RF fragments of
 // 16 ranks) by all rows and keeps the rows that asked for it.  Bound by reading A.
 constexpr int adapter_waves(int rf) { return rf == 8 ? 8 : 16; }
-template <class T, int RF>
+constexpr int adapter_lds(int rf, int ni) { return adapter_waves(rf) * rf * ni * 1024; }
+template <class T, int RF, int NI>
 __global__ void __launch_bounds__(adapter_waves(RF) * 64) adapter_rows(LinearArgs a, int steps_per_split) {
-    constexpr int kWaves = adapter_waves(RF), kDeep = RF == 1 ? 8 : RF == 2 ? 4 : 2;   // steps loaded at once
-    __shared__ f32x4 part[kWaves][RF][64];
+    constexpr int kWaves = adapter_waves(RF), kDeep = RF == 1 ? 8 / NI : RF == 2 ? 4 / NI : 2;   // steps loaded at once
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    auto part = reinterpret_cast<f32x4(*)[RF * NI][64]>(smem);
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int r = lane & 15, g = lane >> 4;
-    const int row0 = (int)blockIdx.x * 16, row = row0 + r;
+    const int row0 = (int)blockIdx.x * 16 * NI;
     const int all = (a.c + 31) / 32;
     const int begin = (int)blockIdx.y * steps_per_split, end = min(begin + steps_per_split, all);
-    const int id = adapter_of(a, row);
-    const uint32_t named = (uint32_t)__ballot(id >= 0) & 0xffffu;
+    int id[NI];
+    uint32_t named = 0;   // 16 rows of each fragment
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+        id[i] = adapter_of(a, row0 + i * 16 + r);
+        named |= ((uint32_t)__ballot(id[i] >= 0) & 0xffffu) << (16 * i);
+    }
+    // the lowest row of `left` gives the next adapter; its rows leave the mask
+    const auto next = [&](uint32_t &left) {
+        const int at = __builtin_ctz(left);
+        int ad = __builtin_amdgcn_readlane(id[0], at & 15);
+        if (NI > 1 && at >= 16) ad = __builtin_amdgcn_readlane(id[NI - 1], at & 15);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) left &= ~(((uint32_t)__ballot(id[i] == ad) & 0xffffu) << (16 * i));
+        return ad;
+    };
     // the n-th adapter that the rows name is for workgroup z = n mod Z of this place
     const int Z = (int)gridDim.z, z = (int)blockIdx.z;
-    int distinct = 0, own = -1;
-    for (uint32_t left = named; left; ++distinct)
-        if (next_adapter(left, id) == id) own = distinct;
+    int distinct = 0, own[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) own[i] = -1;
+    for (uint32_t left = named; left; ++distinct) {
+        const int ad = next(left);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) own[i] = id[i] == ad ? distinct : own[i];
+    }
     const int here = (distinct - z + Z - 1) / Z;
     if (here <= 0) return;
     int classes = 1;
@@ -73,55 +94,69 @@ __global__ void __launch_bounds__(adapter_waves(RF) * 64) adapter_rows(LinearArg
     const int run = (end - begin + share - 1) / share, first = begin + wave / classes * run, last = min(first + run, end);
     const __amdgpu_buffer_rsrc_t rx = range_of(a.x.codes + (int64_t)row0 * a.x.pitch,
                                                (int64_t)(a.m - 1 - row0) * a.x.pitch + a.x.used);
-    f32x4 sum[RF];
+    f32x4 sum[RF][NI];
 #pragma unroll
-    for (int f = 0; f < RF; ++f) sum[f] = f32x4{0, 0, 0, 0};
+    for (int f = 0; f < RF; ++f)
+#pragma unroll
+        for (int i = 0; i < NI; ++i) sum[f][i] = f32x4{0, 0, 0, 0};
     int n = 0;
     for (uint32_t left = named; left; ++n) {
-        const int ad = next_adapter(left, id);
+        const int ad = next(left);
         if (n % Z != z || (n / Z & (classes - 1)) != mine) continue;
         // A's rows past the rank lie past the range, and load as zeros
         const __amdgpu_buffer_rsrc_t ra = range_of(
             static_cast<const typename T::elem *>(a.ad.a) + (int64_t)ad * a.ad.rank * a.c, (int64_t)a.ad.rank * a.c * 2);
-        f32x4 d[RF];
+        f32x4 d[RF][NI];
 #pragma unroll
-        for (int f = 0; f < RF; ++f) d[f] = f32x4{0, 0, 0, 0};
+        for (int f = 0; f < RF; ++f)
+#pragma unroll
+            for (int i = 0; i < NI; ++i) d[f][i] = f32x4{0, 0, 0, 0};
         for (int s = first; s < last; s += kDeep) {
             u32x4_t w[kDeep][RF];
-            uint2 q[kDeep];
+            uint2 q[kDeep][NI];
 #pragma unroll
             for (int e = 0; e < kDeep; ++e) {
                 const int at = (s + e) * 32 + g * 8;   // c is a multiple of 8: a vector is whole or absent
                 const bool in = s + e < last && at < a.c;
-                const auto v = __builtin_amdgcn_raw_buffer_load_b64(
-                    rx, (int)(in ? (uint32_t)r * (uint32_t)a.x.pitch + (uint32_t)at : kNowhere), 0, 0);
-                q[e] = uint2{v[0], v[1]};
+#pragma unroll
+                for (int i = 0; i < NI; ++i) {
+                    const auto v = __builtin_amdgcn_raw_buffer_load_b64(
+                        rx, (int)(in ? (uint32_t)(i * 16 + r) * (uint32_t)a.x.pitch + (uint32_t)at : kNowhere), 0, 0);
+                    q[e][i] = uint2{v[0], v[1]};
+                }
 #pragma unroll
                 for (int f = 0; f < RF; ++f)
                     w[e][f] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(
                         ra, (int)(in ? (uint32_t)((f * 16 + r) * a.c + at) * 2u : kNowhere), 0, 0));
             }
 #pragma unroll
-            for (int e = 0; e < kDeep; ++e) {
-                const typename T::v8 b = codes_to_v8<T>(q[e]);
+            for (int e = 0; e < kDeep; ++e)
 #pragma unroll
-                for (int f = 0; f < RF; ++f) d[f] = T::mma(__builtin_bit_cast(typename T::v8, w[e][f]), b, d[f]);
-            }
+                for (int i = 0; i < NI; ++i) {
+                    const typename T::v8 b = codes_to_v8<T>(q[e][i]);
+#pragma unroll
+                    for (int f = 0; f < RF; ++f) d[f][i] = T::mma(__builtin_bit_cast(typename T::v8, w[e][f]), b, d[f][i]);
+                }
         }
-        if (id == ad)
 #pragma unroll
-            for (int f = 0; f < RF; ++f) sum[f] = d[f];
+        for (int i = 0; i < NI; ++i)
+            if (id[i] == ad)
+#pragma unroll
+                for (int f = 0; f < RF; ++f) sum[f][i] = d[f][i];
     }
 #pragma unroll
-    for (int f = 0; f < RF; ++f) part[wave][f][lane] = sum[f];
-    __syncthreads();
-    // lane (r, g) of fragment f holds ranks 16 f + 4 g + 0..3 of row r
-    for (int f = wave; f < RF; f += kWaves) {
-        f32x4 t = part[0][f][lane];
+    for (int f = 0; f < RF; ++f)
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) t += part[w][f][lane];
-        const int rank = f * 16 + g * 4;
-        if (own >= 0 && own % Z == z && rank < a.ad.rank)   // (rows without an adapter have no u)
+        for (int i = 0; i < NI; ++i) part[wave][f * NI + i][lane] = sum[f][i];
+    __syncthreads();
+    // lane (r, g) of fragment (f, i) holds ranks 16 f + 4 g + 0..3 of row 16 i + r
+    for (int o = wave; o < RF * NI; o += kWaves) {
+        const int f = o / NI, i = o % NI, row = row0 + i * 16 + r, rank = f * 16 + g * 4;
+        f32x4 t = part[0][o][lane];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) t += part[w][o][lane];
+        const int whose = NI > 1 && i ? own[NI - 1] : own[0];
+        if (whose >= 0 && whose % Z == z && rank < a.ad.rank)   // (rows without an adapter have no u)
             *reinterpret_cast<f32x4 *>(a.ad.u + ((int64_t)blockIdx.y * a.m + row) * a.ad.rank + rank) = t;
     }
 }
@@ -239,7 +274,7 @@ __device__ __forceinline__ void add_adapters(const LinearArgs &a, int id, int ro
 // --------------------------------------------------------------- few rows
 
 // 16 FI rows against 16 FJ output channels a workgroup: eight waves take the
-// 128-channel steps in turn, two at a time, weights and rows straight from memory
+// 128-channel steps in turn, several in flight, weights and rows straight from memory
 // into registers (each weight is used once, so LDS would only be a detour), and
 // their sums meet in LDS.  Bound by reading the weights, and with many rows by
 // reading those from L2 once for each workgroup: hence wider ones where there are
@@ -313,10 +348,13 @@ __global__ void __launch_bounds__(512) linear_few(LinearArgs a) {
     int id = -1;
     if constexpr (AD) id = adapter_of(a, row0 + wave % FI * 16 + r);
     asm volatile("" ::: "memory");
-    // two steps in flight; past the last one loads give zeros
-    Step q[2];
-    load(wave, q[0]);
-    load(wave + kWaves, q[1]);
+    // kFlight steps in flight (4 for 16 rows, where they are short; more made wider ones
+    // slower)
+    constexpr int kFlight = FI == 1 ? 4 : 2;
+    Step q[kFlight];
+#pragma unroll
+    for (int e = 0; e < kFlight; ++e)
+        if (wave + e * kWaves < a.steps) load(wave + e * kWaves, q[e]);
     if constexpr (AD) {
         f32x4 d[FJ];
 #pragma unroll
@@ -329,11 +367,12 @@ __global__ void __launch_bounds__(512) linear_few(LinearArgs a) {
 #pragma unroll
         for (int j = 0; j < FJ; ++j) extra[wave][j][lane] = d[j];
     }
-    for (int s = wave; s < a.steps; s += 2 * kWaves) {
-        multiply(q[0]);
-        load(s + 2 * kWaves, q[0]);
-        multiply(q[1]);
-        load(s + 3 * kWaves, q[1]);
+    for (int s = wave; s < a.steps; s += kFlight * kWaves) {
+#pragma unroll
+        for (int e = 0; e < kFlight; ++e) {
+            if (s + e * kWaves < a.steps) multiply(q[e]);
+            if (s + (kFlight + e) * kWaves < a.steps) load(s + (kFlight + e) * kWaves, q[e]);
+        }
     }
 #pragma unroll
     for (int j = 0; j < FJ; ++j)

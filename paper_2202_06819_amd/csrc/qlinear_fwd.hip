@@ -87,21 +87,29 @@ hipError_t product(const LinearArgs &a, hipStream_t stream) {
     }
 }
 
-template <class T, int RF>
-void rows(const LinearArgs &a, hipStream_t stream) {
-    const int steps = (a.c + 31) / 32, per = (steps + a.ad.splits - 1) / a.ad.splits, tiles = (a.m + 15) / 16;
+template <class T, int RF, int NI>
+hipError_t rows_of(const LinearArgs &a, hipStream_t stream) {
+    constexpr auto kKernel = adapter_rows<T, RF, NI>;
+    static const hipError_t set = hipFuncSetAttribute(reinterpret_cast<const void *>(kKernel),
+                                                      hipFuncAttributeMaxDynamicSharedMemorySize, adapter_lds(RF, NI));
+    if (set != hipSuccess) return set;
+    const int steps = (a.c + 31) / 32, per = (steps + a.ad.splits - 1) / a.ad.splits, tiles = (a.m + 16 * NI - 1) / (16 * NI);
     const int z = std::min({256 / (tiles * a.ad.splits) + 1, a.ad.count, 4});
-    hipLaunchKernelGGL((adapter_rows<T, RF>), dim3((unsigned)tiles, (unsigned)a.ad.splits, (unsigned)z),
-                       dim3(adapter_waves(RF) * 64), 0, stream, a, per);
+    hipLaunchKernelGGL(kKernel, dim3((unsigned)tiles, (unsigned)a.ad.splits, (unsigned)z), dim3(adapter_waves(RF) * 64),
+                       adapter_lds(RF, NI), stream, a, per);
+    return hipSuccess;
+}
+template <class T, int RF>
+hipError_t rows(const LinearArgs &a, hipStream_t stream) {
+    return a.m > 512 ? rows_of<T, RF, 2>(a, stream) : rows_of<T, RF, 1>(a, stream);
 }
 
 template <class T, int WB>
 hipError_t linear(const LinearArgs &a, hipStream_t stream) {
     if (a.ad.count) {
-        if (a.ad.rank <= 16) rows<T, 1>(a, stream);
-        else if (a.ad.rank <= 32) rows<T, 2>(a, stream);
-        else if (a.ad.rank <= 64) rows<T, 4>(a, stream);
-        else rows<T, 8>(a, stream);
+        const hipError_t e = a.ad.rank <= 16 ? rows<T, 1>(a, stream) : a.ad.rank <= 32 ? rows<T, 2>(a, stream)
+                             : a.ad.rank <= 64 ? rows<T, 4>(a, stream) : rows<T, 8>(a, stream);
+        if (e != hipSuccess) return e;
     }
     const hipError_t e = a.ad.count ? product<T, WB, true>(a, stream) : product<T, WB, false>(a, stream);
     return e != hipSuccess ? e : hipGetLastError();
@@ -114,7 +122,7 @@ int linear_adapter_splits(int64_t m, int64_t c) {
     // fewer partial sums for more rows, since every workgroup of the product adds them
     const int64_t tiles = (m + 15) / 16, steps = (c + 31) / 32;
     int64_t splits = 256 / tiles;
-    const int64_t most = m <= 64 ? 16 : m <= 512 ? 1024 / m : 2;
+    const int64_t most = m <= 16 ? 4 : m <= 64 ? 16 : m <= 512 ? 1024 / m : 2;
     if (splits > most) splits = most;
     if (splits > (steps + 7) / 8) splits = (steps + 7) / 8;
     return (int)(splits < 1 ? 1 : splits);
