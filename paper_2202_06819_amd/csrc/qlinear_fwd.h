@@ -163,13 +163,15 @@ __global__ void __launch_bounds__(adapter_waves(RF) * 64) adapter_rows(LinearArg
 
 // ---------------------------------------------------------- adapters, part two
 
-// Eight ranks of u of the lane's row, summed over the splits in their order.
+// Eight ranks of u of the lane's row, summed over the splits in their order, DEEP of
+// them loaded at once.
+template <int DEEP>
 __device__ __forceinline__ void load_u(const LinearArgs &a, int row, int rank, float (&u)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) u[i] = 0.0f;
     if (row >= a.m || rank >= a.ad.rank) return;
     const float *p = a.ad.u + (int64_t)row * a.ad.rank + rank;
-#pragma unroll 8
+#pragma unroll DEEP
     for (int s = 0; s < a.ad.splits; ++s, p += (int64_t)a.m * a.ad.rank) {
         const f32x4 lo = *reinterpret_cast<const f32x4 *>(p), hi = *reinterpret_cast<const f32x4 *>(p + 4);
 #pragma unroll
@@ -239,7 +241,7 @@ __device__ __forceinline__ void add_adapters(const LinearArgs &a, int id, int ro
         uint32_t m = 0;
 #pragma unroll
         for (int s = 0; s < RS; ++s) {
-            load_u(a, row, rank0 + s * 32 + g * 8, u[s]);
+            load_u<8>(a, row, rank0 + s * 32 + g * 8, u[s]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) m = max(m, __builtin_bit_cast(uint32_t, u[s][e]) & 0x7fffffffu);
         }
@@ -429,13 +431,13 @@ struct TileAdapters {
             const int id = adapter_of(a, row);
             const float s = id >= 0 ? a.ad.alpha[id] * a.x.scale[row] : 0.0f;
             float u[8];
-            load_u(a, id >= 0 ? row : a.m, rank0 + v * 8, u);
+            load_u<2>(a, id >= 0 ? row : a.m, rank0 + v * 8, u);
             float down = 1.0f, up = 1.0f;
             if constexpr (kScaled) {
                 uint32_t m = 0;
                 for (int c = 0; c < a.ad.rank; c += 64) {
                     float other[8];
-                    load_u(a, id >= 0 ? row : a.m, c + v * 8, other);
+                    load_u<2>(a, id >= 0 ? row : a.m, c + v * 8, other);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) m = max(m, __builtin_bit_cast(uint32_t, other[e] * s) & 0x7fffffffu);
                 }
@@ -529,7 +531,7 @@ struct TileAdapters {
 // the other is multiplied; rows and 8-bit weights go straight from memory to
 // LDS, 4-bit ones through registers, where they are widened.
 template <class T, int WB, int TJ, int TI, int WJ, int WI, bool AD>
-__global__ void __launch_bounds__(WJ *WI * 64) linear_tile(LinearArgs a) {
+__global__ void __launch_bounds__(WJ *WI * 64, TJ == 64 ? 4 : 2) linear_tile(LinearArgs a) {
     constexpr int FJ = 4, FI = TI / (16 * WI), kThreads = WJ * WI * 64, kBuffer = (TJ + TI) * kStepBytes;
     static_assert(TJ == WJ * 64);
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
@@ -591,11 +593,11 @@ __global__ void __launch_bounds__(WJ *WI * 64) linear_tile(LinearArgs a) {
     // lane (r, g): channels ch .. ch + 15 of one row of each fragment i
     const int r = lane & 15, g = lane >> 4;
     const int ch = j0 + jrow0 + g * 16;
+    TileAdapters<T, TJ, TI, kThreads> ad{a, smem, i0, j0};
+    if constexpr (AD) ad.stage_u();
     float ws[16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) ws[e] = a.w.scale[min(ch + e, a.k - 1)];
-    TileAdapters<T, TJ, TI, kThreads> ad{a, smem, i0, j0};
-    if constexpr (AD) ad.stage_u();
     f32x4 d[FJ][FI];
 #pragma unroll
     for (int i = 0; i < FI; ++i) {

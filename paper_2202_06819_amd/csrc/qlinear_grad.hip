@@ -18,9 +18,7 @@ hipError_t tile(const GradArgs &a, hipStream_t stream) {
 constexpr int lds_bytes(int size) { return kGradStages * (size * 64 + size * 128 + 256); }
 template <class T, int WB, bool TRANSPOSED, bool COPY>
 hipError_t product(const GradArgs &a, int size, hipStream_t stream) {
-    // (p through registers would not leave the largest tile enough of them)
-    if constexpr (COPY)
-        if (size == 256) return tile<grad_tile<T, WB, TRANSPOSED, COPY, 256, 256, 8, 1>, lds_bytes(256), 512>(a, stream);
+    if (size == 256) return tile<grad_tile<T, WB, TRANSPOSED, COPY, 256, 256, 8, 1>, lds_bytes(256), 512>(a, stream);
     if (size == 128) return tile<grad_tile<T, WB, TRANSPOSED, COPY, 128, 128, 4, 1>, lds_bytes(128), 256>(a, stream);
     // (waves of 16 x 64 convert no code twice, waves of 32 x 32 read p from LDS less often:
     // a step takes 0.46 against 0.52 us transposed, 0.56 against 0.52 in rows)
@@ -41,7 +39,7 @@ template <class T>
 hipError_t grad(GradArgs a, bool transposed, int w_bits, hipStream_t stream) {
     // (of no rows nothing is read, and copies then read nothing)
     const bool copies = a.nt == 0 || whole_vectors(a, transposed);
-    const GradPlan plan = plan_grad(a.ni, a.nj, a.nt, copies);
+    const GradPlan plan = plan_grad(a.ni, a.nj, a.nt);
     a.tiles_i = (a.ni + plan.tile - 1) / plan.tile;
     a.tiles_j = (a.nj + plan.tile - 1) / plan.tile;
     a.splits = plan.splits;
@@ -66,8 +64,8 @@ hipError_t grad(GradArgs a, bool transposed, int w_bits, hipStream_t stream) {
 // to 1.15 for one to four in one of 64; a split adds a launch and its partial sums'
 // way through memory.  E.g. 1024 x 1024 from 32768 rows: 80 us in 16 tiles of 256 split
 // 16 ways, 105 in 64 of 128 split 8 ways, 282 in 256 of 64; 1024 x 1024 from 1024: 12 in
-// tiles of 64, 20 in 128, 27 in 256.  With p through registers there is no tile of 256.
-GradPlan plan_grad(int64_t ni, int64_t nj, int64_t nt, bool copies) {
+// tiles of 64, 20 in 128, 27 in 256.
+GradPlan plan_grad(int64_t ni, int64_t nj, int64_t nt) {
     static const struct {
         int tile, resident;
         double start, step[4];   // step[n]: n + 1 workgroups on a CU
@@ -76,7 +74,6 @@ GradPlan plan_grad(int64_t ni, int64_t nj, int64_t nt, bool copies) {
     double best_us = 0;
     const int64_t steps = best.steps;
     for (const auto &k : kKinds) {
-        if (k.tile == 256 && !copies) continue;
         const int64_t tiles = ((ni + k.tile - 1) / k.tile) * ((nj + k.tile - 1) / k.tile);
         for (int64_t want = 1; want <= 32; want *= 2) {
             const int64_t per = (steps + want - 1) / want, splits = per ? (steps + per - 1) / per : 1;

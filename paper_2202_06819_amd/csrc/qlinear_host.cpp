@@ -3,8 +3,6 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include <algorithm>
-
 #include "qconv.h"
 #include "qlinear_internal.h"
 
@@ -111,9 +109,8 @@ size_t adapter_workspace(int64_t m, int64_t c, const qconv_adapters *ad) {
     return (size_t)linear_adapter_splits(m, c) * (size_t)m * (size_t)ad->rank * 4;
 }
 
-// Enough for either plan: a gradient's alignment is not known before the call.
 size_t grad_workspace(int64_t ni, int64_t nj, int64_t nt) {
-    const int splits = std::max(plan_grad(ni, nj, nt, false).splits, plan_grad(ni, nj, nt, true).splits);
+    const int splits = plan_grad(ni, nj, nt).splits;
     return splits > 1 ? (size_t)splits * (size_t)ni * (size_t)((nj + 3) / 4 * 4) * 4 : 0;
 }
 

@@ -78,7 +78,7 @@ struct GradPlan {
 inline bool whole_vectors(const GradArgs &a, bool transposed) {
     return a.vec_p && (transposed ? a.ni : a.nt) % 8 == 0;
 }
-GradPlan plan_grad(int64_t ni, int64_t nj, int64_t nt, bool copies);
+GradPlan plan_grad(int64_t ni, int64_t nj, int64_t nt);
 
 // Records a failure for qconv_last_error and returns `code`.
 int fail(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
