@@ -408,26 +408,32 @@ __global__ void __launch_bounds__(512) linear_few(LinearArgs a) {
 // product, in 16-bit floats.  u (64 ranks of it, scaled and rounded) stays in LDS;
 // each adapter that the tile's rows name has its B copied to one of two buffers and
 // takes a step, whose products go to the rows that named it.  So an adapter's B is
-// read once for a tile, however its rows lie.
-template <class T, int TJ, int TI, int THREADS>
+// read once for a tile, however its rows lie.  KS groups of THREADS threads deal the
+// adapters out among them; a row's products are in the group that had its adapter.
+template <class T, int TJ, int TI, int THREADS, int KS>
 struct TileAdapters {
     const LinearArgs &a;
-    uint8_t *smem;   // after the main loop: u | B | B | adapters of the rows | factors
+    uint8_t *smem;   // after the main loop: adapters of the rows | factors | adapters named | u | two B of each group
     int i0, j0;
-    static constexpr int kU = TI * kStepBytes, kB = TJ * kStepBytes, kIds = kU + 2 * kB;
+    static constexpr int kU = TI * 12 + 16, kB = TJ * kStepBytes;
+    static constexpr int kFill = THREADS * (KS < 2 ? KS : 2);   // threads that write u
     static constexpr bool kScaled = __is_same(T, F16);   // bf16 has float's range
 
-    __device__ int *ids() const { return reinterpret_cast<int *>(smem + kIds); }
-    __device__ float *factors() const { return reinterpret_cast<float *>(smem + kIds + TI * 4); }
+    __device__ int *ids() const { return reinterpret_cast<int *>(smem); }
+    __device__ float *factors() const { return reinterpret_cast<float *>(smem + TI * 4); }
+    __device__ int *named() const { return reinterpret_cast<int *>(smem + TI * 8); }
+    __device__ int *count() const { return reinterpret_cast<int *>(smem + TI * 12); }
+    __device__ uint8_t *buffer(int group, int buf) const { return smem + kU + TI * kStepBytes + (group * 2 + buf) * kB; }
     __device__ float down(int row) const { return kScaled ? 1.0f / factors()[row] : 1.0f; }   // (a power of two: exact)
     __device__ float up(int row) const { return kScaled ? factors()[row] : 1.0f; }
 
     // alpha xs u of the tile's rows: 64 ranks from rank0, as 16-bit floats in LDS.  The
     // row's factor comes from all of its ranks.
     __device__ void fill_u(int rank0) const {
+        if ((int)threadIdx.x >= kFill) return;
 #pragma unroll
-        for (int n = 0; n < TI * 8 / THREADS; ++n) {
-            const int unit = n * THREADS + (int)threadIdx.x, at = unit >> 3, v = unit & 7, row = i0 + at;
+        for (int n = 0; n < TI * 8 / kFill; ++n) {
+            const int unit = n * kFill + (int)threadIdx.x, at = unit >> 3, v = unit & 7, row = i0 + at;
             const int id = adapter_of(a, row);
             const float s = id >= 0 ? a.ad.alpha[id] * a.x.scale[row] : 0.0f;
             float u[8];
@@ -448,25 +454,42 @@ struct TileAdapters {
             u32x4_t w;
 #pragma unroll
             for (int e = 0; e < 4; ++e) w[e] = pack2<T>(u[2 * e] * s * down, u[2 * e + 1] * s * down);
-            *reinterpret_cast<u32x4_t *>(smem + at * kStepBytes + ((v ^ slot(at)) << 4)) = w;
+            *reinterpret_cast<u32x4_t *>(smem + kU + at * kStepBytes + ((v ^ slot(at)) << 4)) = w;
             if (v == 0) ids()[at] = id, factors()[at] = up;
         }
     }
-    __device__ void stage_u() const {
+    // u of the first ranks, and the adapters that the rows name, each once.  (Their order
+    // changes no result: a row has one.)
+    __device__ void stage() const {
+        if (threadIdx.x == 0) *count() = 0;
         fill_u(0);
         __syncthreads();
-    }
-    // the lowest adapter above `last` that a row of the tile names; -1: none
-    __device__ int next(int last, int lane) const {
-        uint32_t best = ~0u;
+        const int rows64 = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+        if (rows64 < TI / 64) {   // those of its 64 rows that no row before them names
+            int id[TI / 64];
 #pragma unroll
-        for (int n = 0; n < TI / 64; ++n) {
-            const int id = ids()[n * 64 + lane];
-            if (id > last) best = min(best, (uint32_t)id);
+            for (int n = 0; n < TI / 64; ++n) id[n] = n <= rows64 ? ids()[n * 64 + lane] : -1;
+            const int own = ids()[rows64 * 64 + lane];
+            int found = 0, mine = -1;
+            for (uint64_t left = __ballot(own >= 0); left;) {
+                const int ad = __builtin_amdgcn_readlane(own, __builtin_ctzll(left));
+                left &= ~__ballot(own == ad);
+                bool before = false;
+#pragma unroll
+                for (int n = 0; n < TI / 64 - 1; ++n) before = before || (n < rows64 && __ballot(id[n] == ad));
+                if (before) continue;
+                mine = lane == found ? ad : mine;
+                ++found;
+            }
+            int base = 0;
+            if (lane == 0) base = atomicAdd(count(), found);
+            base = __builtin_amdgcn_readfirstlane(base);
+            if (lane < found) named()[base + lane] = mine;
         }
-#pragma unroll
-        for (int d = 32; d; d >>= 1) best = min(best, (uint32_t)__shfl_xor((int)best, d));
-        return __builtin_amdgcn_readfirstlane((int)best);
+        __syncthreads();
+    }
+    __device__ int named_at(int n, int total) const {
+        return n < total ? __builtin_amdgcn_readfirstlane(named()[n]) : -1;
     }
     __device__ void copy_b(int ad, int rank0, uint8_t *to, int wave, int lane) const {
         const int64_t row_bytes = (int64_t)a.ad.rank * 2;
@@ -475,27 +498,28 @@ struct TileAdapters {
         copy_rows<TJ, THREADS>(to, rb, (uint32_t)row_bytes, rank0 * 2, (int)row_bytes, wave, lane);
     }
     template <int FJ, int FI>
-    __device__ void add(int jrow0, int irow0, int wave, int lane, f32x4 (&d)[FJ][FI]) const {
+    __device__ void add(int jrow0, int irow0, int group, int wave, int lane, f32x4 (&d)[FJ][FI]) const {
         using v8 = typename T::v8;
         const int r = lane & 15, g = lane >> 4;
+        const int total = __builtin_amdgcn_readfirstlane(*count());
         for (int rank0 = 0; rank0 < a.ad.rank; rank0 += 64) {
             if (rank0) {   // everyone is done with the ranks before
                 __syncthreads();
                 fill_u(rank0);
                 __syncthreads();
             }
-            int ad = next(-1, lane), buf = 0;
-            if (ad >= 0) copy_b(ad, rank0, smem + kU, wave, lane);
-            while (ad >= 0) {
-                const int after = next(ad, lane);
+            int ad = named_at(group, total), buf = 0;
+            if (ad >= 0) copy_b(ad, rank0, buffer(group, 0), wave, lane);
+            for (int n = 0; n < total; n += KS) {
+                const int after = named_at(n + KS + group, total);
                 copies_done();
                 __syncthreads();
                 // (the other buffer: its step ended before this barrier)
-                if (after >= 0) copy_b(after, rank0, smem + kU + (buf ^ 1) * kB, wave, lane);
-                const uint8_t *lj = smem + kU + buf * kB;
+                if (after >= 0) copy_b(after, rank0, buffer(group, buf ^ 1), wave, lane);
+                const uint8_t *lj = buffer(group, buf);
 #pragma unroll
                 for (int ks = 0; ks < 2; ++ks) {
-                    if (rank0 + ks * 32 >= a.ad.rank) break;
+                    if (ad < 0 || rank0 + ks * 32 >= a.ad.rank) break;
                     v8 w[FJ];
 #pragma unroll
                     for (int j = 0; j < FJ; ++j) {
@@ -508,7 +532,7 @@ struct TileAdapters {
                         const bool mine = ids()[row] == ad;
                         const uint64_t who = __ballot(mine);
                         if (!who) continue;
-                        const v8 u = *reinterpret_cast<const v8 *>(smem + row * kStepBytes + (((ks * 4 + g) ^ slot(row)) << 4));
+                        const v8 u = *reinterpret_cast<const v8 *>(smem + kU + row * kStepBytes + (((ks * 4 + g) ^ slot(row)) << 4));
                         // (results are chosen, not made zero by u: another adapter's
                         // product may not be finite)
 #pragma unroll
@@ -529,13 +553,18 @@ struct TileAdapters {
 // TJ output channels by TI rows a workgroup of WJ x WI waves, each a tile of 64
 // by 16 FI.  Steps of 128 channels are staged in one of two LDS buffers while
 // the other is multiplied; rows and 8-bit weights go straight from memory to
-// LDS, 4-bit ones through registers, where they are widened.
-template <class T, int WB, int TJ, int TI, int WJ, int WI, bool AD>
-__global__ void __launch_bounds__(WJ *WI * 64, TJ == 64 ? 4 : 2) linear_tile(LinearArgs a) {
+// LDS, 4-bit ones through registers, where they are widened.  KS such groups of
+// waves deal the steps out among them, each with buffers of its own, and their sums
+// meet in LDS: where there are too few tiles to fill the chip, a CU's waves then still
+// hide each other's waits.
+template <class T, int WB, int TJ, int TI, int WJ, int WI, int KS, bool AD>
+__global__ void __launch_bounds__(KS *WJ *WI * 64, TJ == 64 ? 4 : 2) linear_tile(LinearArgs a) {
     constexpr int FJ = 4, FI = TI / (16 * WI), kThreads = WJ * WI * 64, kBuffer = (TJ + TI) * kStepBytes;
     static_assert(TJ == WJ * 64);
+    static_assert(KS == 1 || FI == 1);
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int group = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kThreads), thread = (int)threadIdx.x % kThreads;
+    const int wave = __builtin_amdgcn_readfirstlane(thread >> 6), lane = threadIdx.x & 63;
     int ti, tj;
     tile_at(xcd_run((int)blockIdx.x, a.tiles_i * a.tiles_j), a.tiles_i, a.tiles_j, ti, tj);
     const int i0 = ti * TI, j0 = tj * TJ;
@@ -553,7 +582,7 @@ __global__ void __launch_bounds__(WJ *WI * 64, TJ == 64 ? 4 : 2) linear_tile(Lin
         } else {
 #pragma unroll
             for (int n = 0; n < kUnits; ++n) {
-                const int unit = n * kThreads + (int)threadIdx.x, row = unit >> 2, at = s * 64 + (unit & 3) * 16;
+                const int unit = n * kThreads + thread, row = unit >> 2, at = s * 64 + (unit & 3) * 16;
                 held[n] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(
                     rw4, (int)(at < a.w.used ? (uint32_t)row * (uint32_t)a.w.pitch + (uint32_t)at : kNowhere), 0, 0));
             }
@@ -563,7 +592,7 @@ __global__ void __launch_bounds__(WJ *WI * 64, TJ == 64 ? 4 : 2) linear_tile(Lin
         if constexpr (WB == 4) {
 #pragma unroll
             for (int n = 0; n < kUnits; ++n) {
-                const int unit = n * kThreads + (int)threadIdx.x, row = unit >> 2, v = (unit & 3) * 2;
+                const int unit = n * kThreads + thread, row = unit >> 2, v = (unit & 3) * 2;
                 const uint2 p = widen8(held[n][0]), q = widen8(held[n][1]);
                 const uint2 s = widen8(held[n][2]), t = widen8(held[n][3]);
                 *reinterpret_cast<uint4 *>(buf + row * kStepBytes + ((v ^ slot(row)) << 4)) = uint4{p.x, p.y, q.x, q.y};
@@ -578,23 +607,40 @@ __global__ void __launch_bounds__(WJ *WI * 64, TJ == 64 ? 4 : 2) linear_tile(Lin
     for (int j = 0; j < FJ; ++j)
 #pragma unroll
         for (int i = 0; i < FI; ++i) acc[j][i] = i32x4{0, 0, 0, 0};
-    fetch(0, smem);
-    settle(smem);
+    // (a group's step past the last one is all zeros)
+    uint8_t *const own = smem + group * 2 * kBuffer;
+    fetch(group, own);
+    settle(own);
     __syncthreads();
     int buf = 0;
-    for (int s = 0; s < a.steps; ++s) {
-        uint8_t *cur = smem + buf * kBuffer, *next = smem + (buf ^ 1) * kBuffer;
-        if (s + 1 < a.steps) fetch(s + 1, next);
+    for (int s = 0; s < a.steps; s += KS) {
+        uint8_t *cur = own + buf * kBuffer, *next = own + (buf ^ 1) * kBuffer;
+        if (s + KS < a.steps) fetch(s + KS + group, next);
         mma_step<MmaI8, FJ, FI>(cur, cur + TJ * kStepBytes, jrow0, irow0, lane, acc);
-        if (s + 1 < a.steps) settle(next);
+        if (s + KS < a.steps) settle(next);
         __syncthreads();
         buf ^= 1;
     }
     // lane (r, g): channels ch .. ch + 15 of one row of each fragment i
     const int r = lane & 15, g = lane >> 4;
     const int ch = j0 + jrow0 + g * 16;
-    TileAdapters<T, TJ, TI, kThreads> ad{a, smem, i0, j0};
-    if constexpr (AD) ad.stage_u();
+    if constexpr (KS > 1) {
+        // (in a group's own buffers: not where the adapters' part begins)
+        auto part = [&](int from, int j) {
+            return reinterpret_cast<i32x4 *>(smem + from * 2 * kBuffer) + (wave * FJ + j) * 64 + lane;
+        };
+        if (group)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j) *part(group, j) = acc[j][0], acc[j][0] = i32x4{0, 0, 0, 0};
+        __syncthreads();
+        if (!group)
+#pragma unroll
+            for (int from = 1; from < KS; ++from)
+#pragma unroll
+                for (int j = 0; j < FJ; ++j) acc[j][0] += *part(from, j);
+    }
+    TileAdapters<T, TJ, TI, kThreads, KS> ad{a, smem, i0, j0};
+    if constexpr (AD) ad.stage();
     float ws[16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) ws[e] = a.w.scale[min(ch + e, a.k - 1)];
@@ -609,7 +655,29 @@ __global__ void __launch_bounds__(WJ *WI * 64, TJ == 64 ? 4 : 2) linear_tile(Lin
 #pragma unroll
             for (int e = 0; e < 4; ++e) d[j][i][e] = (float)acc[j][i][e] * xs * ws[4 * j + e];
     }
-    if constexpr (AD) ad.template add<FJ, FI>(jrow0, irow0, wave, lane, d);
+    if constexpr (AD) {
+        // (of a row whose scales are not finite, the groups past the first hold NaN too)
+        if (KS > 1 && group)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j) d[j][0] = f32x4{0, 0, 0, 0};
+        ad.template add<FJ, FI>(jrow0, irow0, group, wave, lane, d);
+        if constexpr (KS > 1) {
+            __syncthreads();   // B's buffers are free
+            auto part = [&](int from, int j) {
+                return reinterpret_cast<f32x4 *>(ad.buffer(from, 0)) + (wave * FJ + j) * 64 + lane;
+            };
+            if (group)
+#pragma unroll
+                for (int j = 0; j < FJ; ++j) *part(group, j) = d[j][0];
+            __syncthreads();
+            if (!group)
+#pragma unroll
+                for (int from = 1; from < KS; ++from)
+#pragma unroll
+                    for (int j = 0; j < FJ; ++j) d[j][0] += *part(from, j);
+        }
+    }
+    if (group) return;
 #pragma unroll
     for (int i = 0; i < FI; ++i) {
         const int row = i0 + irow0 + i * 16 + r;

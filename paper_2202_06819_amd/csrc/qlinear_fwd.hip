@@ -23,36 +23,40 @@ hipError_t few(const LinearArgs &a, hipStream_t stream) {
     return start<linear_few<T, WB, FJ, FI, AD>, few_lds(FJ, FI, AD)>(a, grid, 512, stream);
 }
 
-template <auto Kernel, int TJ, int TI, int THREADS>
+template <auto Kernel, int TJ, int TI, int KS, int THREADS>
 hipError_t tile(LinearArgs a, hipStream_t stream) {
     a.tiles_j = (a.k + TJ - 1) / TJ;
     a.tiles_i = (a.m + TI - 1) / TI;
-    return start<Kernel, 2 * (TJ + TI) * kStepBytes>(a, dim3((unsigned)a.tiles_i * (unsigned)a.tiles_j), THREADS, stream);
+    return start<Kernel, KS * 2 * (TJ + TI) * kStepBytes>(a, dim3((unsigned)a.tiles_i * (unsigned)a.tiles_j), THREADS, stream);
 }
 
 // The kernels, and a model of their times (us), its constants measured.  A workgroup
 // of the few-row kernel takes `start` and `step` for each 1024 channels in its turn on
-// a CU; a tile takes `steps[n]` for a step of 128 channels with n + 1 on a CU, where
-// `resident` fit.  E.g. 4096 x 4096 4-bit weights: 8 rows 4.4 (16 channels and rows a
-// workgroup; a tile of 64: 15.3); 48 rows 9.2 (32 x 32; tile 15.3); 160 rows 15.6 (tile
-// of 64; few-row kernels 20, tile of 128 26); 2048 rows 43 (tile of 128; of 64 60, of 256
-// 68); 8-bit, 8192 rows: 119 (tile of 256).
-enum class Kind { FEW_1x1, FEW_2x1, FEW_2x2, FEW_2x4, TILE_64, TILE_128, TILE_256 };
+// a CU; a tile takes `steps[n]` for a step of 128 channels (of each of its groups of
+// waves) with n + 1 on a CU, where `resident` fit.  E.g. 4-bit weights of 2048 channels,
+// 4096 outputs: 16 rows 3.6 (16 channels and rows a workgroup; a tile of 64 with two
+// groups 7.1); 64 rows 5.3 (32 x 32; tile 7.3); 160 rows 7.6 (tile of 64, two groups; with
+// one 9.6, four 8.1, few-row kernel 11.8); 2048 rows 24 (tile of 128; of 64 33, of 256 38).
+// Of 8192 channels, 256 rows: 19.5 (tile of 64, four groups; two 21.6, one 32, tile of
+// 128 48).  8-bit, 4096 x 4096, 8192 rows: 119 (tile of 256).
+enum class Kind { FEW_1x1, FEW_2x1, FEW_2x2, FEW_2x4, TILE_64x4, TILE_64x2, TILE_64, TILE_128, TILE_256 };
 
 Kind plan_linear(const LinearArgs &a, int w_bits) {
     static const struct {
         Kind kind;
         int channels, rows;
         double start, step, adapters;
-    } kFew[] = {{Kind::FEW_1x1, 16, 16, 0.9, 0.45, 2.5}, {Kind::FEW_2x1, 32, 16, 0.85, 0.8, 3.0},
+    } kFew[] = {{Kind::FEW_1x1, 16, 16, 0.9, 0.55, 2.5}, {Kind::FEW_2x1, 32, 16, 0.85, 0.8, 3.0},
                 {Kind::FEW_2x2, 32, 32, 1.4, 1.15, 4.0}, {Kind::FEW_2x4, 32, 64, 3.2, 1.95, 6.0}};
     static const struct {
         Kind kind;
-        int size, resident;
+        int size, groups, resident;
         double start, steps8[4], steps4[4], adapters;
-    } kTiles[] = {{Kind::TILE_64, 64, 4, 2.0, {0.42, 0.55, 0.74, 0.9}, {0.45, 0.57, 0.76, 0.93}, 3.0},
-                  {Kind::TILE_128, 128, 2, 3.5, {0.75, 1.2}, {0.8, 1.22}, 5.0},
-                  {Kind::TILE_256, 256, 1, 6.0, {1.7}, {2.2}, 8.0}};
+    } kTiles[] = {{Kind::TILE_64x4, 64, 4, 1, 4.2, {0.85}, {0.95}, 2.0},
+                  {Kind::TILE_64x2, 64, 2, 2, 3.4, {0.5, 0.82}, {0.53, 0.89}, 2.0},
+                  {Kind::TILE_64, 64, 1, 4, 2.9, {0.38, 0.5, 0.68, 0.82}, {0.44, 0.58, 0.72, 0.88}, 2.0},
+                  {Kind::TILE_128, 128, 1, 2, 4.2, {0.7, 1.1}, {0.74, 1.17}, 4.0},
+                  {Kind::TILE_256, 256, 1, 1, 6.0, {1.7}, {2.2}, 6.0}};
     const auto on_cu = [&](int64_t channels, int64_t rows) {
         return (((a.k + channels - 1) / channels) * ((a.m + rows - 1) / rows) + 255) / 256;
     };
@@ -69,7 +73,12 @@ Kind plan_linear(const LinearArgs &a, int w_bits) {
         const double *steps = w_bits == 8 ? t.steps8 : t.steps4;
         const double step = (n / t.resident) * steps[t.resident - 1] + (rest ? steps[rest - 1] : 0.0);
         const int64_t turns = (n + t.resident - 1) / t.resident;
-        consider(t.kind, t.start + a.steps * step + turns * (a.ad.count ? t.adapters : 0.0));
+        // each adapter that a tile's rows name is a step of one of its groups: few rows are
+        // taken to name any, many to lie in runs of one
+        const int64_t most = std::min<int64_t>(a.ad.count, a.m < t.size ? a.m : t.size);
+        const int64_t named = a.m <= 256 ? most : std::min(most, (int64_t)a.ad.count * t.size / a.m + 1);
+        const double adapters = a.ad.count ? t.adapters + 1.2 * (double)((named + t.groups - 1) / t.groups) : 0.0;
+        consider(t.kind, t.start + (a.steps + t.groups - 1) / t.groups * step + turns * adapters);
     }
     return best;
 }
@@ -81,9 +90,11 @@ hipError_t product(const LinearArgs &a, hipStream_t stream) {
         case Kind::FEW_2x1: return few<T, WB, 2, 1, AD>(a, stream);
         case Kind::FEW_2x2: return few<T, WB, 2, 2, AD>(a, stream);
         case Kind::FEW_2x4: return few<T, WB, 2, 4, AD>(a, stream);
-        case Kind::TILE_64: return tile<linear_tile<T, WB, 64, 64, 1, 4, AD>, 64, 64, 256>(a, stream);
-        case Kind::TILE_128: return tile<linear_tile<T, WB, 128, 128, 2, 2, AD>, 128, 128, 256>(a, stream);
-        default: return tile<linear_tile<T, WB, 256, 256, 4, 2, AD>, 256, 256, 512>(a, stream);
+        case Kind::TILE_64x4: return tile<linear_tile<T, WB, 64, 64, 1, 4, 4, AD>, 64, 64, 4, 1024>(a, stream);
+        case Kind::TILE_64x2: return tile<linear_tile<T, WB, 64, 64, 1, 4, 2, AD>, 64, 64, 2, 512>(a, stream);
+        case Kind::TILE_64: return tile<linear_tile<T, WB, 64, 64, 1, 4, 1, AD>, 64, 64, 1, 256>(a, stream);
+        case Kind::TILE_128: return tile<linear_tile<T, WB, 128, 128, 2, 2, 1, AD>, 128, 128, 1, 256>(a, stream);
+        default: return tile<linear_tile<T, WB, 256, 256, 4, 2, 1, AD>, 256, 256, 1, 512>(a, stream);
     }
 }
 
