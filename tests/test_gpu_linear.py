@@ -250,6 +250,34 @@ def test_linear_large_tiles_with_adapters(L):
     assert ((y.double() - base - part).abs() <= tol).all()
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,c,k,n,rank,bits", [
+    (250, 8200, 4000, 6, 72, 4), (129, 8200, 4100, 40, 16, 8), (250, 2056, 4000, 3, 128, 8), (161, 2056, 4001, 30, 24, 4),
+    (385, 264, 8200, 12, 40, 4), (700, 264, 8200, 300, 8, 8), (100, 1160, 8000, 64, 64, 8)])
+def test_linear_with_long_rows_and_middling_many(L, m, c, k, n, rank, bits, dtype):
+    """Too few tiles to fill the chip: steps and adapters are dealt to groups of waves."""
+    g = _gen(m + c + k + n)
+    x = _rows8(L, g, m, c)
+    w, q = _rows4(L, g, k, c) if bits == 4 else (_rows8(L, g, k, c), None)
+    base = _product(x, w, q)
+    _near(L.linear(x, w, dtype=dtype), base, base.abs(), 4, dtype)
+    ad = _adapters(L, g, n, rank, c, k, dtype)
+    ids = torch.randint(-1, n, (m,), generator=g, device="cuda", dtype=torch.int32)
+    part, size, coarse = _adapter_part(x, ad, ids)
+    want = base + part
+    tol = (HALF_ULP[dtype] * (coarse + want.abs()) * 1.01 + size * (c + rank + 8) * 2.0 ** -24 + base.abs() * 2.0 ** -22
+           + (2.0 ** -25 if dtype == torch.float16 else 0.0))
+    y = L.linear(x, w, dtype=dtype, adapters=ad, row_adapter=ids)
+    assert ((y.double() - want).abs() <= tol).all()
+    # a row's scale and an adapter that are not finite reach only the rows that use them
+    x.scale[3] = math.nan
+    ad.a[1].fill_(math.inf)
+    ad.b[1].fill_(math.inf)
+    hit = (ids == 1) | (torch.arange(m, device="cuda") == 3)
+    z = L.linear(x, w, dtype=dtype, adapters=ad, row_adapter=ids)
+    assert torch.equal(z[~hit], y[~hit]) and not torch.isfinite(z[hit]).any()
+
+
 @pytest.mark.parametrize("m", [8, 80])
 def test_one_rows_fault_stays_in_its_row(L, m):
     """A row with a NaN scale, and an adapter with infinite weights, reach only
@@ -337,6 +365,26 @@ def test_grads_large_tiles(L, dtype):
     _near(L.linear_grad_input(dy, w), want, size, k, dtype)
     m, c, k = 333, 4005, 3602
     dy, x = _dy(g, m, k, dtype), _rows8(L, g, m, c)
+    want, size = dy.double().t().contiguous() @ _values(x), dy.double().abs().t().contiguous() @ _values(x).abs()
+    _near(L.linear_grad_weight(dy, x), want, size, m, torch.float32)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("bits", [4, 8])
+def test_grads_large_tiles_of_any_alignment(L, bits, dtype):
+    g = _gen(12 + bits)
+    m, c, k = 1541, 2712 if bits == 4 else 2710, 5113   # (4-bit rows have multiples of 8 channels)
+    dy = _dy(g, m, k, dtype, k + 4, 3)
+    if bits == 4:
+        w, q = _rows4(L, g, k, c)
+        values, extra = _values(w, q), HALF_ULP[dtype] * 1.01
+    else:
+        w = _rows8(L, g, k, c)
+        values, extra = _values(w), 0.0
+    want, size = dy.double().contiguous() @ values, dy.double().abs().contiguous() @ values.abs()
+    _near(L.linear_grad_input(dy, w), want, size, k, dtype, extra=extra)
+    m, c, k = 4111, 2690, 3001
+    dy, x = _dy(g, m, k, dtype, k + 2, 1), _rows8(L, g, m, c)
     want, size = dy.double().t().contiguous() @ _values(x), dy.double().abs().t().contiguous() @ _values(x).abs()
     _near(L.linear_grad_weight(dy, x), want, size, m, torch.float32)
 
