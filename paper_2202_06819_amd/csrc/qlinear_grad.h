@@ -105,9 +105,6 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
     const int s0 = split * a.steps_per_split, s1 = min(s0 + a.steps_per_split, a.steps);
     const elem *p = static_cast<const elem *>(a.p);
     float to, from;
-    scale_window<T, kThreads>(a.b.scale, s0 * 64, min(s1 * 64, a.nt), reinterpret_cast<uint32_t *>(smem), to, from);
-    if constexpr (WB == 4) to *= 0.0625f;
-
     const u32x4_t rp_rows = range_words(p + (int64_t)i0 * a.ldp, ((int64_t)(a.ni - 1 - i0) * a.ldp + a.nt) * 2);
     // copy n of step s: the codes', p's, then the scales (every wave copies the same
     // ones to the same place, so that all have the same copies to wait for).  A Step
@@ -165,8 +162,11 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
     // any alignment).  A unit past the matrix is loaded from within it and put right
     // when it is stored, so that the loads of a step are always as many.
     constexpr int kFetches = kCodeUnits + kPUnits, kStages = kGradStages;
-    uint2 code_unit[kCodeUnits ? kCodeUnits : 1];
-    u32x4_t p_unit[kPUnits ? kPUnits : 1];
+    constexpr int kFlight = TJ < 256 && kFetches > 0 ? 2 : 1;   // steps whose loads are on their way
+    struct Units {
+        uint2 code[kCodeUnits ? kCodeUnits : 1];
+        u32x4_t p[kPUnits ? kPUnits : 1];
+    };
     const int p_rows = TRANSPOSED ? a.nt : a.ni, p_count = TRANSPOSED ? a.ni : a.nt;   // p as it lies in memory
     const bool narrow = !COPY && p_count < 8;   // rows shorter than a load: by elements
     auto p_place = [&](int s, int n, int &row, int &at) {
@@ -174,13 +174,13 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
         row = TRANSPOSED ? s * 64 + unit / (TI / 8) : i0 + unit / 8;
         at = TRANSPOSED ? i0 + unit % (TI / 8) * 8 : s * 64 + unit % 8 * 8;
     };
-    auto fetch = [&](int s) {
+    auto fetch = [&](int s, Units &q) {
         if constexpr (WB == 4) {
 #pragma unroll
             for (int n = 0; n < kCodeUnits; ++n) {
                 const int unit = n * kThreads + tid, t = min(s * 64 + unit / (TJ / 16), a.nt - 1);
                 const int at = min((j0 + unit % (TJ / 16) * 16) / 2, a.b.used - 8);
-                code_unit[n] = *reinterpret_cast<const uint2 *>(a.b.codes + (int64_t)t * a.b.pitch + at);
+                q.code[n] = *reinterpret_cast<const uint2 *>(a.b.codes + (int64_t)t * a.b.pitch + at);
             }
         }
         if constexpr (!COPY) {
@@ -195,20 +195,20 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
                     for (int e = 0; e < 7; ++e)
                         if (at == 0 && e < p_count)
                             v[e >> 1] |= (uint32_t)__builtin_bit_cast(uint16_t, line[e]) << (16 * (e & 1));
-                    p_unit[n] = v;
+                    q.p[n] = v;
                 } else {
-                    __builtin_memcpy(&p_unit[n], line + min(at, p_count - 8), 16);
+                    __builtin_memcpy(&q.p[n], line + min(at, p_count - 8), 16);
                 }
             }
         }
     };
-    auto put = [&](int s, uint8_t *buf) {
+    auto put = [&](int s, const Units &q, uint8_t *buf) {
         if constexpr (WB == 4) {
 #pragma unroll
             for (int n = 0; n < kCodeUnits; ++n) {
                 const int unit = n * kThreads + tid, t = unit / (TJ / 16), u = unit % (TJ / 16);
                 const bool in = s * 64 + t < a.nt && j0 + u * 16 < a.b.used * 2;
-                const uint2 lo = widen8(in ? code_unit[n].x : 0u), hi = widen8(in ? code_unit[n].y : 0u);
+                const uint2 lo = widen8(in ? q.code[n].x : 0u), hi = widen8(in ? q.code[n].y : 0u);
                 *reinterpret_cast<uint4 *>(buf + t * TJ + ((u ^ code_unit_of<TJ>(t)) << 4)) = uint4{lo.x, lo.y, hi.x, hi.y};
             }
         }
@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
                 const int unit = n * kThreads + tid;
                 int row, at;
                 p_place(s, n, row, at);
-                u32x4_t v = p_unit[n];
+                u32x4_t v = q.p[n];
                 if (row >= p_rows) {
                     v = u32x4_t{0, 0, 0, 0};
                 } else if (!narrow && at + 8 > p_count) {
@@ -317,14 +317,20 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
         for (int n = 0; n < kCopies; ++n) copy(n, s0 + m, q, smem + m * kStage);
         move_on();
     }
+    Units units[kStages - 1];
+    if constexpr (kFetches > 0)
+#pragma unroll
+        for (int m = 0; m < kStages - 1; ++m) fetch(s0 + m, units[m]);
+    // (found while those are on their way; the last buffer is free until the first step)
+    scale_window<T, kThreads>(a.b.scale, s0 * 64, min(s1 * 64, a.nt),
+                              reinterpret_cast<uint32_t *>(smem + (kStages - 1) * kStage), to, from);
+    if constexpr (WB == 4) to *= 0.0625f;
     if constexpr (kFetches > 0) {
 #pragma unroll
-        for (int m = 0; m < kStages - 1; ++m) {
-            fetch(s0 + m);
-            put(s0 + m, smem + m * kStage);
-        }
+        for (int m = 0; m < kStages - 1; ++m) put(s0 + m, units[m], smem + m * kStage);
         copies_left<0>();
-        fetch(s0 + kStages - 1);
+#pragma unroll
+        for (int m = 0; m < kFlight; ++m) fetch(s0 + kStages - 1 + m, units[m]);
     } else {
         copies_left<kCopies *(kStages - 2)>();
     }
@@ -345,7 +351,7 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
         for (int f = 0; f < kAhead; ++f) ahead[f] = read_p(smem, 0, f);
     }
     int at = 0;
-    for (int s = s0; s < s1; ++s) {
+    auto step = [&](int s, Units &q_units) {
         const int after = at + 1 == kStages ? 0 : at + 1, fill = at == 0 ? kStages - 1 : at - 1;
         uint8_t *cur = smem + at * kStage, *then = smem + after * kStage, *last = smem + fill * kStage;
         half(cur, 0, cur, x, ahead, [](int) {});
@@ -361,12 +367,16 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
         const Words q = words_here();
         move_on();
         half(cur, 1, then, x, ahead, [&](int i) {
+            if (i == 0) put(far, q_units, last);   // (before this step's copies: it waits for older loads only)
 #pragma unroll
             for (int n = i * kCopies / FI; n < (i + 1) * kCopies / FI; ++n) copy(n, far, q, last);
-            if (i == 0) put(far, last);
-            if (i == FI - 1) fetch(far + 1);
+            if (i == FI - 1) fetch(far + kFlight, q_units);
         });
         at = after;
+    };
+    for (int s = s0; s < s1; s += kFlight) {
+        step(s, units[0]);
+        if (kFlight == 2 && s + 1 < s1) step(s + 1, units[kFlight - 1]);
     }
     copies_done();   // none may land in the LDS of a workgroup that comes after
 #pragma unroll
@@ -389,18 +399,30 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
     }
 }
 
-// Adds the partial sums in the order of the splits and rounds once: four
-// columns a thread.
+// Adds the partial sums in the order of the splits and rounds once: four columns a
+// thread.  Bound by reading them: 16 splits of 1024 x 1024, 64 MiB, take 12 us (15 with
+// eight loads at once); 32 splits of 34 x 512, few enough for their waits to show, 4.2
+// with eight loads at once, 10.4 one by one.  (Where there are splits, the plan keeps ni
+// times nj below 2^28.)
 template <class Out>
-__global__ void __launch_bounds__(256) grad_sum(GradArgs a, int64_t first) {
-    const int64_t at = (first + blockIdx.x) * 256 + threadIdx.x;
-    const int64_t quads = a.ldpart / 4, row = at / quads;
-    if (row >= a.ni) return;
+__global__ void __launch_bounds__(256) grad_sum(GradArgs a) {
+    const uint32_t at = blockIdx.x * 256u + threadIdx.x, quads = (uint32_t)a.ldpart / 4, row = at / quads;
+    if (row >= (uint32_t)a.ni) return;
     const int col = (int)(at - row * quads) * 4;
-    const float *p = a.part + row * a.ldpart + col;
+    const float *p = a.part + (int64_t)row * a.ldpart + col;
+    const int64_t stride = (int64_t)a.ni * a.ldpart;
     f32x4 t = *reinterpret_cast<const f32x4 *>(p);
-    for (int s = 1; s < a.splits; ++s) t += *reinterpret_cast<const f32x4 *>(p + (int64_t)s * a.ni * a.ldpart);
-    Out *out = static_cast<Out *>(a.out) + row * a.ldo + col;
+    int s = 1;
+    if (a.splits > 16)   // few results
+        for (; s + 8 <= a.splits; s += 8) {
+            f32x4 v[8];
+#pragma unroll
+            for (int n = 0; n < 8; ++n) v[n] = *reinterpret_cast<const f32x4 *>(p + (s + n) * stride);
+#pragma unroll
+            for (int n = 0; n < 8; ++n) t += v[n];
+        }
+    for (; s < a.splits; ++s) t += *reinterpret_cast<const f32x4 *>(p + s * stride);
+    Out *out = static_cast<Out *>(a.out) + (int64_t)row * a.ldo + col;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
         if (col + e < a.nj) out[e] = (Out)t[e];

@@ -28,10 +28,8 @@ hipError_t product(const GradArgs &a, int size, hipStream_t stream) {
 
 template <class Out>
 hipError_t sum(const GradArgs &a, hipStream_t stream) {
-    const int64_t threads = (int64_t)a.ni * (a.ldpart / 4);
-    launch_slices((threads + 255) / 256, 256, [&](long long first, unsigned count) {
-        hipLaunchKernelGGL((grad_sum<Out>), dim3(count), dim3(256), 0, stream, a, (int64_t)first);
-    });
+    const unsigned threads = (unsigned)a.ni * (unsigned)(a.ldpart / 4);
+    hipLaunchKernelGGL((grad_sum<Out>), dim3((threads + 255) / 256), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 
