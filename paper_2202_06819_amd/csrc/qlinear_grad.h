@@ -17,7 +17,8 @@ namespace qconv {
 
 // Largest finite |scale| of a range, as a factor that brings it to 2^8: f16
 // products of code and scale are then normal numbers over 22 binary orders of
-// magnitude below the largest (bf16 has float's range and needs none).
+// magnitude below the largest (bf16 has float's range and needs none).  Each group of
+// THREADS threads finds it for itself, in LDS of its own.
 template <class T, int THREADS>
 __device__ __forceinline__ void scale_window(const float *scale, int begin, int end, uint32_t *lds, float &to,
                                              float &from) {
@@ -25,13 +26,13 @@ __device__ __forceinline__ void scale_window(const float *scale, int begin, int 
         to = from = 1.0f;
     } else {
         uint32_t m = 0;
-        for (int t = begin + (int)threadIdx.x; t < end; t += THREADS) {
+        for (int t = begin + (int)threadIdx.x % THREADS; t < end; t += THREADS) {
             const uint32_t b = __builtin_bit_cast(uint32_t, scale[t]) & 0x7fffffffu;
             if (b < 0x7f800000u) m = max(m, b);
         }
 #pragma unroll
         for (int d = 32; d; d >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d));
-        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = m;
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x % THREADS >> 6] = m;
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < THREADS / 64; ++w) m = max(m, lds[w]);
@@ -89,9 +90,13 @@ __device__ __forceinline__ uint32_t scaled_pair(uint32_t w, int half, float s0, 
     return pack2<T>((float)(int8_t)(w >> (16 * half)) * s0, (float)(int8_t)(w >> (16 * half + 8)) * s1);
 }
 
+//
+// KS groups of waves deal a tile's steps out among them, each with buffers of its own,
+// and their sums meet in LDS: with few tiles a CU's waves then still hide each other's
+// waits, without partial sums in memory.
 constexpr int kGradStages = 3;
-template <class T, int WB, bool TRANSPOSED, bool COPY, int TJ, int TI, int WJ, int WI>
-__global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
+template <class T, int WB, bool TRANSPOSED, bool COPY, int TJ, int TI, int WJ, int WI, int KS>
+__global__ void __launch_bounds__(KS *WJ *WI * 64) grad_tile(GradArgs a) {
     constexpr int FJ = TJ / (16 * WJ), FI = TI / (16 * WI), kThreads = WJ * WI * 64, kWaves = kThreads / 64;
     constexpr int kCodes = 64 * TJ, kP = TI * 128, kStage = kCodes + kP + 256;
     constexpr int kCodeCopies = WB == 8 ? kCodes / (1024 * kWaves) : 0, kPCopies = COPY ? kP / (1024 * kWaves) : 0;
@@ -99,14 +104,19 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
     constexpr int kCopies = kCodeCopies + kPCopies + 1;   // a wave's copies of a step
     using elem = typename T::elem;
     using v8 = typename T::v8;
-    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-    const int tid = (int)threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    extern __shared__ __attribute__((aligned(16))) uint8_t all_smem[];
+    const int group = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kThreads);
+    uint8_t *const smem = all_smem + group * (kGradStages * kStage);
+    const int tid = (int)threadIdx.x % kThreads, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int tiles = a.tiles_i * a.tiles_j;
     const int split = (int)blockIdx.x / tiles;
     int ti, tj;
     tile_at(xcd_run((int)blockIdx.x - split * tiles, tiles), a.tiles_i, a.tiles_j, ti, tj);
     const int i0 = ti * TI, j0 = tj * TJ;
-    const int s0 = split * a.steps_per_split, s1 = min(s0 + a.steps_per_split, a.steps);
+    // the split's steps, dealt to the groups in runs; past them every operand is zero
+    const int begin = split * a.steps_per_split, end = min(begin + a.steps_per_split, a.steps);
+    const int run = (end - begin + KS - 1) / KS, s0 = begin + group * run, s1 = s0 + run;
+    const int t_end = min(a.nt, end * 64);
     const elem *p = static_cast<const elem *>(a.p);
     float to, from;
     const u32x4_t rp_rows = range_words(p + (int64_t)i0 * a.ldp, ((int64_t)(a.ni - 1 - i0) * a.ldp + a.nt) * 2);
@@ -121,7 +131,7 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
     const int codes_step = 64 * (int)a.b.pitch, p_step = 64 * (int)a.ldp * 2;
     const int codes_last = a.b.used - j0, p_last = (a.ni - i0) * 2;   // bytes in reach of a step's last row
     Step place{(uint64_t)(a.b.codes + (int64_t)s0 * 64 * a.b.pitch + j0), (uint64_t)(p + (int64_t)s0 * 64 * a.ldp + i0),
-               (uint64_t)(a.b.scale + s0 * 64), a.nt - s0 * 64};
+               (uint64_t)(a.b.scale + s0 * 64), t_end - s0 * 64};
     const auto move_on = [&] {
         place.codes += codes_step;
         if (TRANSPOSED) place.p += p_step;
@@ -150,7 +160,7 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
             uint32_t off;
             if constexpr (!TRANSPOSED) {
                 const int row = (at0 >> 7) + (lane >> 3), at = s * 128 + (((lane & 7) ^ slot(row)) << 4);
-                off = at < a.nt * 2 ? (uint32_t)row * (uint32_t)a.ldp * 2u + (uint32_t)at : kNowhere;
+                off = at < t_end * 2 ? (uint32_t)row * (uint32_t)a.ldp * 2u + (uint32_t)at : kNowhere;
             } else {
                 const int at = at0 + lane * 16, t = at / (TI * 2), in = at % (TI * 2);
                 const int col = ((in >> 5) ^ unit_of<TI>(t)) * 32 + (in & 16);
@@ -171,7 +181,7 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
         uint2 code[kCodeUnits ? kCodeUnits : 1];
         u32x4_t p[kPUnits ? kPUnits : 1];
     };
-    const int p_rows = TRANSPOSED ? a.nt : a.ni, p_count = TRANSPOSED ? a.ni : a.nt;   // p as it lies in memory
+    const int p_rows = TRANSPOSED ? t_end : a.ni, p_count = TRANSPOSED ? a.ni : t_end;   // p as it lies in memory
     const bool narrow = !COPY && p_count < 8;   // rows shorter than a load: by elements
     auto p_place = [&](int s, int n, int &row, int &at) {
         const int unit = n * kThreads + tid;
@@ -211,7 +221,7 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
 #pragma unroll
             for (int n = 0; n < kCodeUnits; ++n) {
                 const int unit = n * kThreads + tid, t = unit / (TJ / 16), u = unit % (TJ / 16);
-                const bool in = s * 64 + t < a.nt && j0 + u * 16 < a.b.used * 2;
+                const bool in = s * 64 + t < t_end && j0 + u * 16 < a.b.used * 2;
                 const uint2 lo = widen8(in ? q.code[n].x : 0u), hi = widen8(in ? q.code[n].y : 0u);
                 *reinterpret_cast<uint4 *>(buf + t * TJ + ((u ^ code_unit_of<TJ>(t)) << 4)) = uint4{lo.x, lo.y, hi.x, hi.y};
             }
@@ -326,7 +336,7 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
 #pragma unroll
         for (int m = 0; m < kStages - 1; ++m) fetch(s0 + m, units[m]);
     // (found while those are on their way; the last buffer is free until the first step)
-    scale_window<T, kThreads>(a.b.scale, s0 * 64, min(s1 * 64, a.nt),
+    scale_window<T, kThreads>(a.b.scale, begin * 64, t_end,
                               reinterpret_cast<uint32_t *>(smem + (kStages - 1) * kStage), to, from);
     if constexpr (WB == 4) to *= 0.0625f;
     if constexpr (kFetches > 0) {
@@ -383,6 +393,26 @@ __global__ void __launch_bounds__(WJ *WI * 64) grad_tile(GradArgs a) {
         if (kFlight == 2 && s + 1 < s1) step(s + 1, units[kFlight - 1]);
     }
     copies_done();   // none may land in the LDS of a workgroup that comes after
+    if constexpr (KS > 1) {
+        static_assert(FJ * FI * kThreads * 16 <= kGradStages * kStage);
+        __syncthreads();   // nor where the groups' sums meet
+        auto part = [&](int from, int f) {
+            return reinterpret_cast<f32x4 *>(all_smem + from * (kGradStages * kStage)) + f * kThreads + tid;
+        };
+        if (group)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j)
+#pragma unroll
+                for (int i = 0; i < FI; ++i) *part(group, j * FI + i) = acc[j][i];
+        __syncthreads();
+        if (group) return;
+#pragma unroll
+        for (int from = 1; from < KS; ++from)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j)
+#pragma unroll
+                for (int i = 0; i < FI; ++i) acc[j][i] += *part(from, j * FI + i);
+    }
 #pragma unroll
     for (int i = 0; i < FI; ++i) {
         const int row = i0 + irow0 + i * 16 + r;

@@ -17,13 +17,16 @@ hipError_t tile(const GradArgs &a, hipStream_t stream) {
 // Steps in LDS: codes, p, scales.
 constexpr int lds_bytes(int size) { return kGradStages * (size * 64 + size * 128 + 256); }
 template <class T, int WB, bool TRANSPOSED, bool COPY>
-hipError_t product(const GradArgs &a, int size, hipStream_t stream) {
-    if (size == 256) return tile<grad_tile<T, WB, TRANSPOSED, COPY, 256, 256, 8, 1>, lds_bytes(256), 512>(a, stream);
-    if (size == 128) return tile<grad_tile<T, WB, TRANSPOSED, COPY, 128, 128, 4, 1>, lds_bytes(128), 256>(a, stream);
+hipError_t product(const GradArgs &a, int size, int groups, hipStream_t stream) {
+    if (size == 256) return tile<grad_tile<T, WB, TRANSPOSED, COPY, 256, 256, 8, 1, 1>, lds_bytes(256), 512>(a, stream);
+    if (size == 128) return tile<grad_tile<T, WB, TRANSPOSED, COPY, 128, 128, 4, 1, 1>, lds_bytes(128), 256>(a, stream);
     // (waves of 16 x 64 convert no code twice, waves of 32 x 32 read p from LDS less often:
     // a step takes 0.46 against 0.52 us transposed, 0.56 against 0.52 in rows)
-    if constexpr (TRANSPOSED) return tile<grad_tile<T, WB, TRANSPOSED, COPY, 64, 64, 4, 1>, lds_bytes(64), 256>(a, stream);
-    else return tile<grad_tile<T, WB, TRANSPOSED, COPY, 64, 64, 2, 2>, lds_bytes(64), 256>(a, stream);
+    constexpr int WJ = TRANSPOSED ? 4 : 2, WI = TRANSPOSED ? 1 : 2;
+    if (groups == 4)
+        return tile<grad_tile<T, WB, TRANSPOSED, COPY, 64, 64, WJ, WI, 4>, 4 * lds_bytes(64), 1024>(a, stream);
+    if (groups == 2) return tile<grad_tile<T, WB, TRANSPOSED, COPY, 64, 64, WJ, WI, 2>, 2 * lds_bytes(64), 512>(a, stream);
+    return tile<grad_tile<T, WB, TRANSPOSED, COPY, 64, 64, WJ, WI, 1>, lds_bytes(64), 256>(a, stream);
 }
 
 template <class Out>
@@ -45,11 +48,11 @@ hipError_t grad(GradArgs a, bool transposed, int w_bits, hipStream_t stream) {
     a.steps_per_split = plan.steps_per_split;
     hipError_t e;
     if (transposed)
-        e = copies ? product<T, 8, true, true>(a, plan.tile, stream) : product<T, 8, true, false>(a, plan.tile, stream);
+        e = copies ? product<T, 8, true, true>(a, plan.tile, plan.groups, stream) : product<T, 8, true, false>(a, plan.tile, plan.groups, stream);
     else if (w_bits == 8)
-        e = copies ? product<T, 8, false, true>(a, plan.tile, stream) : product<T, 8, false, false>(a, plan.tile, stream);
+        e = copies ? product<T, 8, false, true>(a, plan.tile, plan.groups, stream) : product<T, 8, false, false>(a, plan.tile, plan.groups, stream);
     else
-        e = copies ? product<T, 4, false, true>(a, plan.tile, stream) : product<T, 4, false, false>(a, plan.tile, stream);
+        e = copies ? product<T, 4, false, true>(a, plan.tile, plan.groups, stream) : product<T, 4, false, false>(a, plan.tile, plan.groups, stream);
     if (e != hipSuccess || a.splits == 1) return e;
     return transposed ? sum<float>(a, stream) : sum<typename T::elem>(a, stream);
 }
@@ -62,13 +65,16 @@ hipError_t grad(GradArgs a, bool transposed, int w_bits, hipStream_t stream) {
 // to 1.15 for one to four in one of 64; a split adds a launch and its partial sums'
 // way through memory.  E.g. 1024 x 1024 from 32768 rows: 80 us in 16 tiles of 256 split
 // 16 ways, 105 in 64 of 128 split 8 ways, 282 in 256 of 64; 1024 x 1024 from 1024: 12 in
-// tiles of 64, 20 in 128, 27 in 256.
+// tiles of 64, 20 in 128, 27 in 256.  Groups of waves dealing out the steps of a tile of
+// 64: 430 x 3104 from 1862 rows 25 us with two (35 without, in tiles of 128 split twice),
+// 333 x 2824 from 1001 17.2 (19.2); 941 x 384 from 512, too few steps for it, 11.8 (9.9).
 GradPlan plan_grad(int64_t ni, int64_t nj, int64_t nt) {
     static const struct {
-        int tile, resident;
+        int tile, groups, resident;
         double start, step[4];   // step[n]: n + 1 workgroups on a CU
-    } kKinds[] = {{256, 1, 10, {1.35}}, {128, 2, 7, {0.85, 1.2}}, {64, 4, 6, {0.52, 0.7, 0.92, 1.15}}};
-    GradPlan best{64, 1, 0, (int)((nt + 63) / 64)};
+    } kKinds[] = {{256, 1, 1, 10, {1.35}}, {128, 1, 2, 7, {0.85, 1.2}}, {64, 1, 4, 6, {0.52, 0.7, 0.92, 1.15}},
+                  {64, 2, 2, 7.5, {0.7, 1.15}}, {64, 4, 1, 9, {1.15}}};
+    GradPlan best{64, 1, 1, 0, (int)((nt + 63) / 64)};
     double best_us = 0;
     const int64_t steps = best.steps;
     for (const auto &k : kKinds) {
@@ -79,11 +85,12 @@ GradPlan plan_grad(int64_t ni, int64_t nj, int64_t nt) {
             const int64_t on_cu = (splits * tiles + 255) / 256;
             const int64_t rest = on_cu % k.resident;
             const double step = (on_cu / k.resident) * k.step[k.resident - 1] + (rest ? k.step[rest - 1] : 0.0);
-            double us = k.start + per * step;
+            double us = k.start + (per + k.groups - 1) / k.groups * step;
             if (splits > 1) us += 2.5 + 8e-6 * splits * ni * nj / 5.0;
             if (best_us == 0 || us < best_us) {
                 best_us = us;
                 best.tile = k.tile;
+                best.groups = k.groups;
                 best.splits = (int)splits;
                 best.steps_per_split = (int)per;
             }

@@ -71,7 +71,7 @@ hipError_t launch_grad(const GradArgs &a, bool transposed, int w_bits, int dtype
 // sizes and the launches.
 int linear_adapter_splits(int64_t m, int64_t c);
 struct GradPlan {
-    int tile;            // 64, 128 or 256
+    int tile, groups;    // 64, 128 or 256; groups of waves that deal its steps out
     int splits, steps_per_split, steps;
 };
 // Whether p's rows are whole 16-byte vectors, so that they can be copied to LDS.
