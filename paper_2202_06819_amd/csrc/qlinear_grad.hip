@@ -1,4 +1,6 @@
 // Launches of the products of the linear layer's backward pass.
+#include <algorithm>
+
 #include "qlinear_grad.h"
 
 namespace qconv {
@@ -59,21 +61,22 @@ hipError_t grad(GradArgs a, bool transposed, int w_bits, hipStream_t stream) {
 
 }  // namespace
 
-// The tile and the split that a model of the kernels' times (us) finds fastest.  The
-// constants are measured: a step of 64 of the summed axis takes 1.35 in a tile of
-// 256 (one workgroup fits a CU), 0.85 alone and 1.2 for two on a CU in one of 128, 0.52
-// to 1.15 for one to four in one of 64; a split adds a launch and its partial sums'
-// way through memory.  E.g. 1024 x 1024 from 32768 rows: 80 us in 16 tiles of 256 split
-// 16 ways, 105 in 64 of 128 split 8 ways, 282 in 256 of 64; 1024 x 1024 from 1024: 12 in
-// tiles of 64, 20 in 128, 27 in 256.  Groups of waves dealing out the steps of a tile of
-// 64: 430 x 3104 from 1862 rows 25 us with two (35 without, in tiles of 128 split twice),
-// 333 x 2824 from 1001 17.2 (19.2); 941 x 384 from 512, too few steps for it, 11.8 (9.9).
+// The tile, its groups of waves and the split that a model of the kernels' times (us)
+// finds fastest.  The constants are measured: a step of 64 of the summed axis takes 1.35
+// in a tile of 256 (one workgroup fits a CU), 0.83 alone and 1.25 for two on a CU in one
+// of 128, 0.5 to 1.1 for one to four in one of 64; two groups of a tile of 64 take a step
+// each in 0.57, four in 1.0; a split adds a launch and its partial sums' way through
+// memory.  E.g. 1024 x 1024 from 32768 rows: 79 us in 16 tiles of 256 split 16 ways, 101
+// in 64 of 128 split 8 ways, 133 in 256 of 64 split 8 ways, 141 of four groups; from 2560
+// rows: 14.2 in tiles of 64 with four groups, 14.7 with two, 21.6 with one, 22.4 in 128
+// split 4 ways, 28.4 in 256 split 8 ways; from 1024: 8.3 with two groups, 9.2 with four,
+// 10.6 with one, 18.6 in 128.  512 x 1024 from 4096: 17.2 with four groups split 2 ways.
 GradPlan plan_grad(int64_t ni, int64_t nj, int64_t nt) {
     static const struct {
         int tile, groups, resident;
         double start, step[4];   // step[n]: n + 1 workgroups on a CU
-    } kKinds[] = {{256, 1, 1, 10, {1.35}}, {128, 1, 2, 7, {0.85, 1.2}}, {64, 1, 4, 6, {0.52, 0.7, 0.92, 1.15}},
-                  {64, 2, 2, 7.5, {0.7, 1.15}}, {64, 4, 1, 9, {1.15}}};
+    } kKinds[] = {{256, 1, 1, 10, {1.35}}, {128, 1, 2, 6, {0.83, 1.25}}, {64, 1, 4, 3.7, {0.5, 0.75, 0.95, 1.1}},
+                  {64, 2, 2, 4.3, {0.57, 1.08}}, {64, 4, 1, 5, {1.0}}};
     GradPlan best{64, 1, 1, 0, (int)((nt + 63) / 64)};
     double best_us = 0;
     const int64_t steps = best.steps;
@@ -85,8 +88,9 @@ GradPlan plan_grad(int64_t ni, int64_t nj, int64_t nt) {
             const int64_t on_cu = (splits * tiles + 255) / 256;
             const int64_t rest = on_cu % k.resident;
             const double step = (on_cu / k.resident) * k.step[k.resident - 1] + (rest ? k.step[rest - 1] : 0.0);
-            double us = k.start + (per + k.groups - 1) / k.groups * step;
-            if (splits > 1) us += 2.5 + 8e-6 * splits * ni * nj / 5.0;
+            const int64_t turns = std::max<int64_t>((on_cu + k.resident - 1) / k.resident, 1);
+            double us = turns * k.start + (per + k.groups - 1) / k.groups * step;
+            if (splits > 1) us += 4 + 0.1 * splits + 8e-6 * splits * ni * nj / 5.0;
             if (best_us == 0 || us < best_us) {
                 best_us = us;
                 best.tile = k.tile;

@@ -389,6 +389,28 @@ def test_grads_large_tiles_of_any_alignment(L, bits, dtype):
     _near(L.linear_grad_weight(dy, x), want, size, m, torch.float32)
 
 
+@pytest.mark.parametrize("m,c,k", [(128, 1024, 700), (1000, 1010, 2630), (70, 4000, 1001), (500, 640, 90)])
+@pytest.mark.parametrize("odd", [0, 3])
+def test_an_infinity_in_the_gradient_stays_one(L, m, c, k, odd):
+    """An infinite value of dy reaches its row (of dw: its column's row) as that
+    infinity times the codes, wherever the summed axis was cut, and no other row."""
+    g = _gen(m + k)
+    dy, w, x = _dy(g, m, k, torch.bfloat16, k + odd), _rows8(L, g, k, c), _rows8(L, g, m, c)
+    for rows in (w, x):
+        rows.codes[:, :c][rows.codes[:, :c] == 0] = 1
+    clean = L.linear_grad_input(dy, w), L.linear_grad_weight(dy, x)
+    hits = ((5, 3), (m - 1, k - 1))
+    for i, j in hits:
+        dy[i, j] = math.inf
+    dx, dw = L.linear_grad_input(dy, w), L.linear_grad_weight(dy, x)
+    for i, j in hits:
+        assert torch.equal(dx[i].float(), math.inf * w.codes[j, :c].float())
+        assert torch.equal(dw[j], math.inf * x.codes[i, :c].float())
+    rest_x = [i for i in range(m) if i not in (5, m - 1)]
+    rest_w = [j for j in range(k) if j not in (3, k - 1)]
+    assert torch.equal(dx[rest_x], clean[0][rest_x]) and torch.equal(dw[rest_w], clean[1][rest_w])
+
+
 def test_f16_gradients_at_far_scales(L):
     """Row scales far from one, and far from each other: f16 products are formed
     about the largest scale."""
