@@ -19,7 +19,8 @@ hipError_t tile(const GradArgs &a, hipStream_t stream) {
 // Steps in LDS: codes, p, scales.
 constexpr int lds_bytes(int size) { return kGradStages * (size * 64 + size * 128 + 256); }
 template <class T, int WB, bool TRANSPOSED, bool COPY>
-hipError_t product(const GradArgs &a, int size, int groups, hipStream_t stream) {
+hipError_t product(const GradArgs &a, const GradPlan &plan, hipStream_t stream) {
+    const int size = plan.tile, groups = plan.groups;
     if (size == 256) return tile<grad_tile<T, WB, TRANSPOSED, COPY, 256, 256, 8, 1, 1>, lds_bytes(256), 512>(a, stream);
     if (size == 128) return tile<grad_tile<T, WB, TRANSPOSED, COPY, 128, 128, 4, 1, 1>, lds_bytes(128), 256>(a, stream);
     // (waves of 16 x 64 convert no code twice, waves of 32 x 32 read p from LDS less often:
@@ -50,11 +51,11 @@ hipError_t grad(GradArgs a, bool transposed, int w_bits, hipStream_t stream) {
     a.steps_per_split = plan.steps_per_split;
     hipError_t e;
     if (transposed)
-        e = copies ? product<T, 8, true, true>(a, plan.tile, plan.groups, stream) : product<T, 8, true, false>(a, plan.tile, plan.groups, stream);
+        e = copies ? product<T, 8, true, true>(a, plan, stream) : product<T, 8, true, false>(a, plan, stream);
     else if (w_bits == 8)
-        e = copies ? product<T, 8, false, true>(a, plan.tile, plan.groups, stream) : product<T, 8, false, false>(a, plan.tile, plan.groups, stream);
+        e = copies ? product<T, 8, false, true>(a, plan, stream) : product<T, 8, false, false>(a, plan, stream);
     else
-        e = copies ? product<T, 4, false, true>(a, plan.tile, plan.groups, stream) : product<T, 4, false, false>(a, plan.tile, plan.groups, stream);
+        e = copies ? product<T, 4, false, true>(a, plan, stream) : product<T, 4, false, false>(a, plan, stream);
     if (e != hipSuccess || a.splits == 1) return e;
     return transposed ? sum<float>(a, stream) : sum<typename T::elem>(a, stream);
 }
