@@ -561,9 +561,9 @@ int qconv_quantize_rows(const void *x, int32_t dtype, int64_t ldx, int32_t m, in
  *           count x k x rank values of y's type
  *   alpha   DEVICE, count floats;  row: DEVICE, int32 for each row of x
  *   rank    a multiple of 8 up to 128; c % 8 == 0
- * u is kept in 32 bits between the two products and rounded once to y's type
- * for the second (f16: after scaling its row by a power of two, so that only y
- * itself can overflow).
+ * u is kept in 32 bits between the two products and enters the second as the
+ * sum of two values of y's type, exact to 2^-16 (bf16) or 2^-22 (f16) of itself
+ * (f16: after scaling its row by a power of two, so that only y itself can overflow).
  */
 typedef struct qconv_adapters {
     const void *a, *b;

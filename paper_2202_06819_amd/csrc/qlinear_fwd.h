@@ -184,12 +184,26 @@ __device__ __forceinline__ void load_u(const LinearArgs &a, int row, int rank, f
 }
 
 // A power of two that brings a row's largest |u| (its float bits) into [1, 2), and its
-// inverse: u is rounded to 16 bits after it, so that the rounding is relative to the
-// row and no f16 overflows.  Within 2^-40 .. 2^40: results scaled by it stay finite.
+// inverse: u is split into 16-bit parts after it, so that their rounding is relative to
+// the row and no f16 overflows.  Within 2^-40 .. 2^40: results scaled by it stay finite.
 __device__ __forceinline__ void row_factor(uint32_t m, float &down, float &up) {
     const int e = min(max((int)(m >> 23), 127 - 40), 127 + 40);
     down = __builtin_bit_cast(float, (uint32_t)(254 - e) << 23);
     up = __builtin_bit_cast(float, (uint32_t)e << 23);
+}
+
+// Two values as a high and a low part in 16 bits, each rounded to nearest: what the two
+// leave out is a rounding of a rounding (2^-16 of a bf16 value, 2^-22 of an f16 one), so
+// that u's way through 16-bit products shows as little as the 32-bit sums' own order.
+// One part alone costs a product less and as much error as the result's own rounding
+// again (one row, 4096 channels: 0.0019 against 0.0017 of the result).
+template <class T>
+__device__ __forceinline__ void split_pair(float a, float b, uint32_t &high, uint32_t &low) {
+    high = pack2<T>(a, b);
+    const typename T::v2 h = __builtin_bit_cast(typename T::v2, high);
+    const float ha = (float)h[0], hb = (float)h[1];
+    // (an infinity has no rest)
+    low = pack2<T>(__builtin_isinf(ha) ? 0.0f : a - ha, __builtin_isinf(hb) ? 0.0f : b - hb);
 }
 
 // Adds the adapters' second products for 16 rows to FJ fragments of results: d[j] +=
@@ -240,7 +254,7 @@ __device__ __forceinline__ void add_adapters(const LinearArgs &a, int id, int ro
         };
         load_batch();
         if (ad[0] < 0) return;   // nothing for this wave
-        u32x4_t ub[RS];
+        u32x4_t high[RS], low[RS];
         float u[RS][8];
         uint32_t m = 0;
 #pragma unroll
@@ -256,7 +270,11 @@ __device__ __forceinline__ void add_adapters(const LinearArgs &a, int id, int ro
 #pragma unroll
         for (int s = 0; s < RS; ++s)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) ub[s][e] = pack2<T>(u[s][2 * e] * down, u[s][2 * e + 1] * down);
+            for (int e = 0; e < 4; ++e) {
+                uint32_t h, l;
+                split_pair<T>(u[s][2 * e] * down, u[s][2 * e + 1] * down, h, l);
+                high[s][e] = h, low[s][e] = l;
+            }
         const float scale = up * (row < a.m ? a.x.scale[row] : 0.0f);
         while (ad[0] >= 0) {
 #pragma unroll
@@ -265,8 +283,10 @@ __device__ __forceinline__ void add_adapters(const LinearArgs &a, int id, int ro
                 for (int j = 0; j < FJ; ++j) {
                     f32x4 t{0, 0, 0, 0};
 #pragma unroll
-                    for (int s = 0; s < RS; ++s)
-                        t = T::mma(__builtin_bit_cast(v8, w[b][j][s]), __builtin_bit_cast(v8, ub[s]), t);
+                    for (int s = 0; s < RS; ++s) {
+                        t = T::mma(__builtin_bit_cast(v8, w[b][j][s]), __builtin_bit_cast(v8, low[s]), t);
+                        t = T::mma(__builtin_bit_cast(v8, w[b][j][s]), __builtin_bit_cast(v8, high[s]), t);
+                    }
                     // (chosen, not by a zero factor: another adapter's product may not be finite)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
@@ -410,7 +430,7 @@ __global__ void __launch_bounds__(512) linear_few(LinearArgs a) {
 // --------------------------------------------------------------- many rows
 
 // The adapters' second products of a workgroup's tile: further steps of the same tile
-// product, in 16-bit floats.  u (64 ranks of it, scaled and rounded) stays in LDS;
+// product, in 16-bit floats.  u (64 ranks of it, scaled, as a high and a low part) stays in LDS;
 // each adapter that the tile's rows name has its B copied to one of two buffers and
 // takes a step, whose products go to the rows that named it.  So an adapter's B is
 // read once for a tile, however its rows lie.  KS groups of THREADS threads deal the
@@ -420,9 +440,10 @@ __global__ void __launch_bounds__(512) linear_few(LinearArgs a) {
 template <class T, int TJ, int TI, int THREADS, int KS>
 struct TileAdapters {
     const LinearArgs &a;
-    uint8_t *smem;   // after the main loop: adapters of the rows | factors | adapters named | u | two B of each group
+    uint8_t *smem;   // after the main loop: adapters of the rows | factors | adapters named | u, high and low | two B of each group
     int i0, j0;
-    static constexpr int kU = TI * 12 + 16, kB = TJ * kStepBytes;
+    static constexpr int kU = TI * 12 + 16, kPart = TI * kStepBytes, kB = TJ * kStepBytes;
+    static constexpr int kBytes = kU + 2 * kPart + KS * 2 * kB;
     static constexpr int kFill = THREADS * (KS < 2 ? KS : 2);   // threads that write u
     static constexpr bool kScaled = __is_same(T, F16);   // bf16 has float's range
 
@@ -430,11 +451,11 @@ struct TileAdapters {
     __device__ float *factors() const { return reinterpret_cast<float *>(smem + TI * 4); }
     __device__ int *named() const { return reinterpret_cast<int *>(smem + TI * 8); }
     __device__ int *count() const { return reinterpret_cast<int *>(smem + TI * 12); }
-    __device__ uint8_t *buffer(int group, int buf) const { return smem + kU + TI * kStepBytes + (group * 2 + buf) * kB; }
+    __device__ uint8_t *buffer(int group, int buf) const { return smem + kU + 2 * kPart + (group * 2 + buf) * kB; }
     __device__ float down(int row) const { return kScaled ? 1.0f / factors()[row] : 1.0f; }   // (a power of two: exact)
     __device__ float up(int row) const { return kScaled ? factors()[row] : 1.0f; }
 
-    // alpha xs u of the tile's rows: 64 ranks from rank0, as 16-bit floats in LDS.  The
+    // alpha xs u of the tile's rows: 64 ranks from rank0, in two 16-bit parts in LDS.  The
     // row's factor comes from all of its ranks.
     __device__ void fill_u(int rank0) const {
         if ((int)threadIdx.x >= kFill) return;
@@ -458,10 +479,16 @@ struct TileAdapters {
                 for (int b = 1; b < 8; b <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, b));
                 row_factor(m, down, up);
             }
-            u32x4_t w;
+            u32x4_t high, low;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = pack2<T>(u[2 * e] * s * down, u[2 * e + 1] * s * down);
-            *reinterpret_cast<u32x4_t *>(smem + kU + at * kStepBytes + ((v ^ slot(at)) << 4)) = w;
+            for (int e = 0; e < 4; ++e) {
+                uint32_t h, l;
+                split_pair<T>(u[2 * e] * s * down, u[2 * e + 1] * s * down, h, l);
+                high[e] = h, low[e] = l;
+            }
+            uint8_t *const to = smem + kU + at * kStepBytes + ((v ^ slot(at)) << 4);
+            *reinterpret_cast<u32x4_t *>(to) = high;
+            *reinterpret_cast<u32x4_t *>(to + kPart) = low;
             if (v == 0) ids()[at] = id, factors()[at] = up;
         }
     }
@@ -539,12 +566,13 @@ struct TileAdapters {
                         const bool mine = ids()[row] == ad;
                         const uint64_t who = __ballot(mine);
                         if (!who) continue;
-                        const v8 u = *reinterpret_cast<const v8 *>(smem + kU + row * kStepBytes + (((ks * 4 + g) ^ slot(row)) << 4));
+                        const uint8_t *const lu = smem + kU + row * kStepBytes + (((ks * 4 + g) ^ slot(row)) << 4);
+                        const v8 high = *reinterpret_cast<const v8 *>(lu), low = *reinterpret_cast<const v8 *>(lu + kPart);
                         // (results are chosen, not made zero by u: another adapter's
                         // product may not be finite)
 #pragma unroll
                         for (int j = 0; j < FJ; ++j) {
-                            const f32x4 t = T::mma(w[j], u, d[j][i]);
+                            const f32x4 t = T::mma(w[j], high, T::mma(w[j], low, d[j][i]));
 #pragma unroll
                             for (int e = 0; e < 4; ++e) d[j][i][e] = mine ? t[e] : d[j][i][e];
                         }
@@ -556,6 +584,13 @@ struct TileAdapters {
         }
     }
 };
+
+// LDS of a workgroup: its groups' buffers, and in their place afterwards the adapters'.
+template <class T, int TJ, int TI, int THREADS, int KS, bool AD>
+constexpr int tile_lds() {
+    const int steps = KS * 2 * (TJ + TI) * kStepBytes, adapters = AD ? TileAdapters<T, TJ, TI, THREADS, KS>::kBytes : 0;
+    return steps > adapters ? steps : adapters;
+}
 
 // TJ output channels by TI rows a workgroup of WJ x WI waves, each a tile of 64
 // by 16 FI.  Steps of 128 channels are staged in one of two LDS buffers while

@@ -23,11 +23,12 @@ hipError_t few(const LinearArgs &a, hipStream_t stream) {
     return start<linear_few<T, WB, FJ, FI, AD>, few_lds(FJ, FI, AD)>(a, grid, 512, stream);
 }
 
-template <auto Kernel, int TJ, int TI, int KS, int THREADS>
+template <class T, auto Kernel, int TJ, int TI, int KS, int THREADS, bool AD>
 hipError_t tile(LinearArgs a, hipStream_t stream) {
     a.tiles_j = (a.k + TJ - 1) / TJ;
     a.tiles_i = (a.m + TI - 1) / TI;
-    return start<Kernel, KS * 2 * (TJ + TI) * kStepBytes>(a, dim3((unsigned)a.tiles_i * (unsigned)a.tiles_j), THREADS, stream);
+    return start<Kernel, tile_lds<T, TJ, TI, THREADS / KS, KS, AD>()>(a, dim3((unsigned)a.tiles_i * (unsigned)a.tiles_j),
+                                                                      THREADS, stream);
 }
 
 // The kernels, and a model of their times (us), its constants measured.  A workgroup
@@ -90,11 +91,11 @@ hipError_t product(const LinearArgs &a, hipStream_t stream) {
         case Kind::FEW_2x1: return few<T, WB, 2, 1, AD>(a, stream);
         case Kind::FEW_2x2: return few<T, WB, 2, 2, AD>(a, stream);
         case Kind::FEW_2x4: return few<T, WB, 2, 4, AD>(a, stream);
-        case Kind::TILE_64x4: return tile<linear_tile<T, WB, 64, 64, 1, 4, 4, AD>, 64, 64, 4, 1024>(a, stream);
-        case Kind::TILE_64x2: return tile<linear_tile<T, WB, 64, 64, 1, 4, 2, AD>, 64, 64, 2, 512>(a, stream);
-        case Kind::TILE_64: return tile<linear_tile<T, WB, 64, 64, 1, 4, 1, AD>, 64, 64, 1, 256>(a, stream);
-        case Kind::TILE_128: return tile<linear_tile<T, WB, 128, 128, 2, 2, 1, AD>, 128, 128, 1, 256>(a, stream);
-        default: return tile<linear_tile<T, WB, 256, 256, 4, 2, 1, AD>, 256, 256, 1, 512>(a, stream);
+        case Kind::TILE_64x4: return tile<T, linear_tile<T, WB, 64, 64, 1, 4, 4, AD>, 64, 64, 4, 1024, AD>(a, stream);
+        case Kind::TILE_64x2: return tile<T, linear_tile<T, WB, 64, 64, 1, 4, 2, AD>, 64, 64, 2, 512, AD>(a, stream);
+        case Kind::TILE_64: return tile<T, linear_tile<T, WB, 64, 64, 1, 4, 1, AD>, 64, 64, 1, 256, AD>(a, stream);
+        case Kind::TILE_128: return tile<T, linear_tile<T, WB, 128, 128, 2, 2, 1, AD>, 128, 128, 1, 256, AD>(a, stream);
+        default: return tile<T, linear_tile<T, WB, 256, 256, 4, 2, 1, AD>, 256, 256, 1, 512, AD>(a, stream);
     }
 }
 

@@ -237,6 +237,30 @@ def test_linear_with_adapters(L, m, c, k, n, rank, bits, dtype):
     assert torch.equal(L.linear(x, w, dtype=dtype, adapters=ad, row_adapter=none), L.linear(x, w, dtype=dtype))
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,c,k,n,rank,bits", [
+    (1, 256, 40, 2, 16, 4), (5, 512, 33, 2, 24, 8), (40, 1000, 130, 7, 64, 8), (48, 512, 96, 1, 128, 8), (70, 264, 140, 5, 40, 4),
+    (200, 512, 300, 9, 16, 4), (250, 8200, 4000, 6, 72, 4), (250, 2056, 4000, 3, 128, 8), (385, 264, 8200, 12, 40, 4),
+    (1500, 264, 4100, 6, 128, 8), (3329, 200, 4100, 4, 72, 8)])
+def test_an_adapters_first_product_keeps_more_than_16_bits(L, m, c, k, n, rank, bits, dtype):
+    """u goes to the second product as two 16-bit parts: each rounding leaves half an
+    ulp of its part, so what both leave is the square of it, relative to the row's
+    largest u (f16: or half of its smallest subnormal, where that is more)."""
+    g = _gen(m + c + k + n + 1)
+    x = _rows8(L, g, m, c)
+    w, q = _rows4(L, g, k, c) if bits == 4 else (_rows8(L, g, k, c), None)
+    w.scale.mul_(2.0 ** -8)   # the adapters' part is the larger one
+    ad = _adapters(L, g, n, rank, c, k, dtype)
+    ids = torch.randint(0, n, (m,), generator=g, device="cuda", dtype=torch.int32)
+    base = _product(x, w, q)
+    part, size, coarse = _adapter_part(x, ad, ids)
+    want = base + part
+    y = L.linear(x, w, dtype=dtype, adapters=ad, row_adapter=ids)
+    tol = (coarse * (HALF_ULP[dtype] ** 2 + 2.0 ** -24) + size * (c + 2 * rank + 8) * 2.0 ** -24 + base.abs() * 2.0 ** -22) * 1.01
+    tol = tol + HALF_ULP[dtype] * want.abs() + (2.0 ** -25 if dtype == torch.float16 else 0.0)
+    assert ((y.double() - want).abs() <= tol).all()
+
+
 def test_linear_large_tiles_with_adapters(L):
     g = _gen(77)
     m, c, k, n, rank = 3329, 200, 4100, 4, 16
