@@ -15,10 +15,11 @@
 
 namespace qconv {
 
-// Largest finite |scale| of a range, as a factor that brings it to 2^8: f16
-// products of code and scale are then normal numbers over 22 binary orders of
-// magnitude below the largest (bf16 has float's range and needs none).  Each group of
-// THREADS threads finds it for itself, in LDS of its own.
+// A power of two that brings the largest finite |scale| of a range to at most 65504 /
+// 128, the largest f16 by the largest code, and above half of that: a code of -128 stays
+// finite, and f16 products of code and scale are normal numbers for scales down to 2^-21
+// of the largest (bf16 has float's range and needs none).  Each group of THREADS threads
+// finds it for itself, in LDS of its own.
 template <class T, int THREADS>
 __device__ __forceinline__ void scale_window(const float *scale, int begin, int end, uint32_t *lds, float &to,
                                              float &from) {
@@ -37,8 +38,9 @@ __device__ __forceinline__ void scale_window(const float *scale, int begin, int 
 #pragma unroll
         for (int w = 0; w < THREADS / 64; ++w) m = max(m, lds[w]);
         __syncthreads();
-        // exponents of to = 2^(8 - e) and its inverse, both normal
-        const int e = min(max((int)(m >> 23) - 127, -118), 126);
+        // exponents of to = 2^(8 - e) and its inverse, both normal (-118 <= e <= 128); a
+        // mantissa past 65504 / 32768 = 1 + 0x7fe000 / 2^23 takes the next e
+        const int e = max((int)(m >> 23) - 127 + ((m & 0x7fffffu) > 0x7fe000u), -118);
         to = __builtin_bit_cast(float, (uint32_t)(127 + 8 - e) << 23);
         from = __builtin_bit_cast(float, (uint32_t)(127 - 8 + e) << 23);
     }

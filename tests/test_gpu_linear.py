@@ -451,6 +451,42 @@ def test_f16_gradients_at_far_scales(L):
     assert not L.linear_grad_weight(dy, zero).any()
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("top", [1.0, 1.998, 1.999, 1.9995, 1.9998, 2.0 - 2.0 ** -23])
+@pytest.mark.parametrize("shift", [-100, -9, 110])
+@pytest.mark.parametrize("m", [70, 300])
+def test_gradients_of_the_largest_codes(L, m, shift, top, dtype):
+    """Codes of -128 under scales up to the next power of two: finite operands give
+    finite gradients.  The code times its scale is rounded once (half an ulp)."""
+    g = _gen(m + shift)
+    c, k = 48, 40
+    dy = _dy(g, m, k, dtype)
+    for rows in (_rows8(L, g, m, c), _rows8(L, g, k, c)):
+        rows.codes[:, :c][torch.rand(rows.codes.shape[0], c, generator=g, device="cuda") < 0.2] = -128
+        rows.scale.copy_(top * torch.exp2(shift - torch.randint(0, 3, (len(rows.scale),), generator=g, device="cuda").float()))
+        values = _values(rows)
+        if len(rows.scale) == m:
+            want, size = dy.double().t().contiguous() @ values, dy.double().abs().t().contiguous() @ values.abs()
+            _near(L.linear_grad_weight(dy, rows), want, size, m, torch.float32, extra=HALF_ULP[dtype] * 1.01 + 2.0 ** -23)
+        elif shift == -9:   # (a 16-bit result)
+            want, size = dy.double() @ values, dy.double().abs() @ values.abs()
+            _near(L.linear_grad_input(dy, rows), want, size, k, dtype, extra=HALF_ULP[dtype] * 1.01 + 2.0 ** -23)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** 127, 1.9999 * 2.0 ** 127])
+def test_f16_gradients_at_the_largest_scales(L, scale):
+    """A code times such a scale passes 32 bits, its product with a small gradient does not."""
+    g = _gen(8)
+    m, c, k = 20, 32, 24
+    x = _rows8(L, g, m, c)
+    x.scale.fill_(scale)
+    dy = (2.0 ** -14 * (1 + torch.rand(m, k, generator=g, device="cuda")) * torch.sign(_randn(g, m, k))).half()
+    want = dy.double().t().contiguous() @ _values(x)
+    size = dy.double().abs().t().contiguous() @ _values(x).abs()
+    assert size.max() < 2.0 ** 127
+    _near(L.linear_grad_weight(dy, x), want, size, m, torch.float32, extra=HALF_ULP[torch.float16] * 1.01)
+
+
 @pytest.mark.parametrize("k", [24, 25])
 def test_grad_weight_of_no_rows_is_zero(L, k):
     x = L.Rows(torch.empty((0, 48), dtype=torch.int8, device="cuda"), torch.empty(0, device="cuda"), 40)
