@@ -483,6 +483,22 @@ DevAttrCache g_attr;
 
 }  // namespace
 
+namespace qconv {
+
+hipError_t allow_lds(const void *kernel, int64_t lds) {
+    if (lds <= 64 * 1024) return hipSuccess;
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    std::lock_guard<std::mutex> g(g_attr.mu);
+    if (g_attr.done.count({dev, kernel})) return hipSuccess;
+    e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLdsBytes);
+    if (e == hipSuccess) g_attr.done.insert({dev, kernel});
+    return e;
+}
+
+}  // namespace qconv
+
 // ---- the device scratch of qconv2d_prepared_noalloc: the split-K workspace
 // for callers that cannot allocate.  One array per device (each GPU the
 // library runs on holds its own copy until the process ends).  Layout: the
@@ -738,7 +754,6 @@ FloatEpilogue float_epilogue(const qconv_desc *d, const qconv_layout_info &li, c
     return f;
 }
 
-// Kernels that stage more than 64 KiB of LDS must opt in, once per device.
 // Workgroups of `kernel` (threads, dynamic LDS bytes) that fit one CU, as the
 // runtime reports them; 0 if it cannot say.  Asked once per device and shape:
 // eager launches of persistent plans would otherwise query it every call.
@@ -759,16 +774,8 @@ int occupancy_per_cu(const void *kernel, int threads, int64_t lds) {
 }
 
 int ensure_lds_attribute(const void *kernel, int64_t lds) {
-    if (lds <= 64 * 1024) return QCONV_OK;
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess) return fail(QCONV_EHIP, "hipGetDevice failed");
-    std::lock_guard<std::mutex> g(g_attr.mu);
-    if (!g_attr.done.count({dev, kernel})) {
-        hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLdsBytes);
-        if (e != hipSuccess) return fail(QCONV_EHIP, "hipFuncSetAttribute: %s", hipGetErrorString(e));
-        g_attr.done.insert({dev, kernel});
-    }
-    return QCONV_OK;
+    const hipError_t e = allow_lds(kernel, lds);
+    return e == hipSuccess ? QCONV_OK : fail(QCONV_EHIP, "LDS limit of a kernel: %s", hipGetErrorString(e));
 }
 
 // The workgroup order of xcd_order -1 (the library's choice).  Each XCD has

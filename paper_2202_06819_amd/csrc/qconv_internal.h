@@ -45,6 +45,10 @@ void launch_slices(long long blocks, int threads, Launch go) {
         go(first, (unsigned)(blocks - first < most ? blocks - first : most));
 }
 
+// Lets `kernel` have `lds` bytes of dynamic LDS on the current device: more than 64 KiB
+// have to be asked for, once for each device.
+hipError_t allow_lds(const void *kernel, int64_t lds);
+
 // The f32 requantiser of an epilogue (EpiParams in qconv_device.h); kind 0: not
 // used (the clamp is not a whole output range, or an accumulator may pass 2^24).
 struct FloatEpilogue {

@@ -10,9 +10,8 @@ namespace {
 // A launch with LDS of any size up to the CU's.
 template <auto Kernel, int LDS>
 hipError_t start(const LinearArgs &a, dim3 grid, int threads, hipStream_t stream) {
-    static const hipError_t set =
-        hipFuncSetAttribute(reinterpret_cast<const void *>(Kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-    if (set != hipSuccess) return set;
+    const hipError_t e = allow_lds(reinterpret_cast<const void *>(Kernel), LDS);
+    if (e != hipSuccess) return e;
     hipLaunchKernelGGL(Kernel, grid, dim3((unsigned)threads), LDS, stream, a);
     return hipSuccess;
 }
@@ -102,9 +101,8 @@ hipError_t product(const LinearArgs &a, hipStream_t stream) {
 template <class T, int RF, int NI>
 hipError_t rows_of(const LinearArgs &a, hipStream_t stream) {
     constexpr auto kKernel = adapter_rows<T, RF, NI>;
-    static const hipError_t set = hipFuncSetAttribute(reinterpret_cast<const void *>(kKernel),
-                                                      hipFuncAttributeMaxDynamicSharedMemorySize, adapter_lds(RF, NI));
-    if (set != hipSuccess) return set;
+    const hipError_t e = allow_lds(reinterpret_cast<const void *>(kKernel), adapter_lds(RF, NI));
+    if (e != hipSuccess) return e;
     const int steps = (a.c + 31) / 32, per = (steps + a.ad.splits - 1) / a.ad.splits, tiles = (a.m + 16 * NI - 1) / (16 * NI);
     const int z = std::min({256 / (tiles * a.ad.splits) + 1, a.ad.count, 4});
     hipLaunchKernelGGL(kKernel, dim3((unsigned)tiles, (unsigned)a.ad.splits, (unsigned)z), dim3(adapter_waves(RF) * 64),

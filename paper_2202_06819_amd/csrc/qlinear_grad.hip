@@ -9,9 +9,8 @@ namespace {
 
 template <auto Kernel, int LDS, int THREADS>
 hipError_t tile(const GradArgs &a, hipStream_t stream) {
-    static const hipError_t set =
-        hipFuncSetAttribute(reinterpret_cast<const void *>(Kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-    if (set != hipSuccess) return set;
+    const hipError_t e = allow_lds(reinterpret_cast<const void *>(Kernel), LDS);
+    if (e != hipSuccess) return e;
     hipLaunchKernelGGL(Kernel, dim3((unsigned)(a.tiles_i * a.tiles_j * a.splits)), dim3(THREADS), LDS, stream, a);
     return hipGetLastError();
 }

@@ -1,0 +1,40 @@
+"""What the linear layer's entry points launch, recorded without a GPU."""
+import pytest
+
+from _launches import record
+
+
+@pytest.fixture(scope="module")
+def tmp(tmp_path_factory):
+    return tmp_path_factory.mktemp("recorder")
+
+
+# one call of each kernel that stages more than 64 KiB
+LARGE = [dict(op="linear", m=8192, c=4096, k=4096), dict(op="linear", m=198, c=8192, k=4096, bits=4),
+         dict(op="linear", m=2003, c=2048, k=8192, adapters=5, rank=128),
+         dict(op="grad_input", m=8192, c=4096, k=4096), dict(op="grad_weight", m=777, c=1411, k=1003)]
+
+
+def test_lds_limits_are_raised_on_every_device(tmp):
+    """A kernel with more than 64 KiB of LDS asks for it on each device before its first
+    launch there, and not again."""
+    there = [{"device": 0}, *LARGE, *LARGE, {"device": 3}, *LARGE, {"device": 0}, *LARGE]
+    raised = set()
+    for step, (status, events) in zip(there, record(tmp, there)["events"]):
+        assert status == 0
+        assert ("op" in step) == any(e[0] == "launch" for e in events)
+        for kind, device, name, *rest in events:
+            if kind == "attribute":
+                assert (device, name) not in raised
+                raised.add((device, name))
+            elif int(rest[2]) > 64 * 1024:
+                assert (device, name) in raised, f"{name} on device {device}"
+    assert {d for d, _ in raised} == {"0", "3"} and len(raised) >= 8
+
+
+def test_a_refused_lds_limit_is_asked_for_again(tmp):
+    """The call that could not raise it says so and launches nothing; the next one tries anew."""
+    for call in (LARGE[0], LARGE[3]):
+        (_, _), (status, events), (again, then) = record(tmp, [{"refuse": 1}, call, call])["events"]
+        assert status == -4 and not events
+        assert again == 0 and [e[0] for e in then] == ["attribute", "launch"]
