@@ -20,7 +20,8 @@ weights are rows of the same form (8-bit, or 4-bit from :func:`pack_rows4`) in
 :func:`linear_layer` is those calls as one differentiable function; with
 ``adapters`` the forward product serves many requests, each with its own
 low-rank adapter.  Tensors may live on any GPU: a call runs on their device's
-current stream, or on ``stream``.
+current stream, or on ``stream`` (a torch stream or a raw handle), after that
+stream's earlier work and no other's; what it allocates is that stream's memory.
 """
 from __future__ import annotations
 
@@ -121,19 +122,30 @@ def _rows_arg(r: Rows, name: str, device: torch.device) -> QConvRows:
     return QConvRows(codes.data_ptr(), scale.data_ptr(), pitch, m, channels, bits)
 
 
-def _used_on(t: torch.Tensor, stream) -> torch.Tensor:
-    """A tensor that the call made on the current stream's pool and uses on ``stream``."""
-    if stream is not None:
-        t.record_stream(stream if isinstance(stream, torch.cuda.Stream)
-                        else torch.cuda.ExternalStream(int(stream), device=t.device))
+def _empty(shape, dtype: torch.dtype, device: torch.device, stream) -> torch.Tensor:
+    """Memory that the call writes on ``stream``: that stream's own, since what was freed
+    on another one may still be in use by work queued there.  It is kept for the current
+    stream too, where the caller may read it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(_as_stream(stream, device)):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
     return t
+
+
+def _as_stream(stream, device: torch.device) -> torch.cuda.Stream:
+    """``stream``, or torch's view of a raw handle."""
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    return torch.cuda.ExternalStream(_stream(stream, device), device=device)
 
 
 def _on(device: torch.device, out: torch.Tensor | None, shape: tuple, dtype: torch.dtype, name: str,
         stream) -> torch.Tensor:
     """The output: new, or the caller's after a check."""
     if out is None:
-        return _used_on(torch.empty(shape, dtype=dtype, device=device), stream)
+        return _empty(shape, dtype, device, stream)
     if out.shape != shape or out.dtype is not dtype or out.device != device:
         raise QConvError(EINVAL, f"{name} must be {shape} of {dtype} on {device}")
     if shape[1] > 1 and out.stride(1) != 1:
@@ -150,7 +162,7 @@ def _workspace(need: int, workspace: torch.Tensor | None, device: torch.device, 
         return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
     if not need:
         return None, None, 0
-    t = _used_on(torch.empty(need, dtype=torch.uint8, device=device), stream)
+    t = _empty(need, torch.uint8, device, stream)
     return t, t.data_ptr(), need
 
 
@@ -180,8 +192,8 @@ def quantize_rows(x: torch.Tensor, out: Rows | None = None, stream=None) -> Rows
     device = x.device
     if out is None:
         pitch = rows_pitch(c)
-        codes = _used_on(torch.empty((m, pitch), dtype=torch.int8, device=device), stream)
-        scale = _used_on(torch.empty(m, dtype=torch.float32, device=device), stream)
+        codes = _empty((m, pitch), torch.int8, device, stream)
+        scale = _empty(m, torch.float32, device, stream)
         out = Rows(codes, scale, c)
         to = (codes.data_ptr(), pitch, scale.data_ptr())
     else:

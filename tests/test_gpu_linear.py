@@ -564,6 +564,63 @@ def test_other_streams_and_graphs(L):
         (x.float() @ x.float().t()).sum().item()
 
 
+@pytest.mark.parametrize("op", ["quantize_rows", "linear", "linear_grad_input", "linear_grad_weight", "split"])
+def test_a_given_streams_results_do_not_meet_the_current_streams_memory(L, op):
+    """A call on another stream is not ordered after the current one: what it makes must
+    not lie in memory that was freed there while work on it is still queued, nor the
+    other way round, when a result that the current stream still reads is given back."""
+    g = _gen(61)
+    m, c, k = (4096, 1024, 1024) if op != "split" else (16384, 512, 512)
+    x, w = _rows8(L, g, m, c), _rows8(L, g, k, c)
+    v = _randn(g, m, c).bfloat16()
+    dy = _dy(g, m, k, torch.bfloat16)
+    call = {"quantize_rows": lambda **on: L.quantize_rows(v, **on).codes,
+            "linear": lambda **on: L.linear(x, w, **on),
+            "linear_grad_input": lambda **on: L.linear_grad_input(dy, w, **on),
+            "linear_grad_weight": lambda **on: L.linear_grad_weight(dy, x, **on),
+            "split": lambda **on: L.linear_grad_weight(dy, x, **on)}[op]
+    assert op != "split" or L.grad_workspace_bytes(k, c, m) > 0
+    want = call()
+    held = L.grad_workspace_bytes(k, c, m) if op == "split" else want.numel() * want.element_size()
+    s, current = torch.cuda.Stream(), torch.cuda.current_stream()
+    call(stream=s)
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    # freed on the current stream, read there later
+    old = torch.full((held,), 77, dtype=torch.uint8, device="cuda")
+    read = torch.empty_like(old)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)
+    read.copy_(old)
+    del old
+    got = call(stream=s)
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and (read == 77).all()
+    # a result read on the current stream, and given back
+    again = call(stream=s)
+    current.wait_stream(s)
+    torch.cuda._sleep(200_000_000)
+    copy = again.clone()
+    del again, got
+    with torch.cuda.stream(s):
+        other = torch.full((want.numel() * want.element_size(),), 99, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    assert torch.equal(copy, want) and (other == 99).all()
+
+
+def test_a_stream_as_a_raw_handle(L):
+    g = _gen(62)
+    x, w = _rows8(L, g, 70, 256), _rows8(L, g, 40, 256)
+    want = L.linear(x, w)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for stream in (s, s.cuda_stream, torch.cuda.default_stream().cuda_stream):
+        got = L.linear(x, w, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_layer_trains(L, dtype):
     """The differentiable layer: gradients of the rounded product, and a few
