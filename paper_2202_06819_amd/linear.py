@@ -211,12 +211,19 @@ def pack_rows4(codes: torch.Tensor, scale: torch.Tensor, stream=None) -> Rows:
     scales as 4-bit rows: qconv_pack of rows of whole 16-byte vectors."""
     if codes.dim() != 2 or codes.dtype != torch.int8:
         raise QConvError(EINVAL, "codes must be an int8 matrix")
+    if not codes.is_cuda:
+        raise QConvError(EINVAL, "codes must be a device tensor")
     k, c = codes.shape
     if c % 8:
         raise QConvError(EINVAL, f"4-bit rows need channels % 8 == 0 (got {c})")
-    if c % 32:
-        codes = torch.nn.functional.pad(codes, (0, 32 - c % 32))
-    words = qconv.pack(codes.contiguous().reshape(k, -1, 1, 1), 4, True, stream=stream)
+    device = codes.device
+    current = torch.cuda.current_stream(device)
+    # (the copies too: they are made and given back on the stream that reads them)
+    with torch.cuda.stream(current if stream is None else _as_stream(stream, device)):
+        if c % 32:
+            codes = torch.nn.functional.pad(codes, (0, 32 - c % 32))
+        words = qconv.pack(codes.contiguous().reshape(k, -1, 1, 1), 4, True)
+    words.record_stream(current)
     return Rows(words.reshape(k, -1), scale, c, 4)
 
 

@@ -621,6 +621,37 @@ def test_a_stream_as_a_raw_handle(L):
         assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("c", [256, 264])
+@pytest.mark.parametrize("contiguous", [True, False])
+def test_pack_rows4_on_a_given_stream(L, c, contiguous):
+    """All of the packing runs on the stream that was given, whatever the current one
+    is busy with, and its result is not memory that is still in use there."""
+    g = _gen(c)
+    k = 3000
+    codes = torch.randint(-8, 8, (k, c + 8), generator=g, device="cuda").to(torch.int8)[:, :c]
+    codes = codes.contiguous() if contiguous else codes
+    scale = torch.ones(k, device="cuda")
+    want = L.pack_rows4(codes, scale)
+    s = torch.cuda.Stream()
+    L.pack_rows4(codes, scale, stream=s)
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    old = torch.full((want.codes.numel() * 4,), 77, dtype=torch.uint8, device="cuda")
+    read = torch.empty_like(old)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)
+    read.copy_(old)
+    del old
+    got = L.pack_rows4(codes, scale, stream=s)
+    with torch.cuda.stream(s):
+        copy = got.codes.clone()
+        torch.full((k * 288,), 99, dtype=torch.uint8, device="cuda")   # (the padded codes' size: theirs, if given back)
+    s.synchronize()
+    assert torch.equal(copy, want.codes)
+    torch.cuda.synchronize()
+    assert (read == 77).all()
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_layer_trains(L, dtype):
     """The differentiable layer: gradients of the rounded product, and a few
