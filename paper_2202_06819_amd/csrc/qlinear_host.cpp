@@ -91,16 +91,16 @@ int check_tiles(int64_t rows, int64_t cols) {
     return QCONV_OK;
 }
 
-int check_adapters(const qconv_adapters *ad, const qconv_rows *x, const qconv_rows *w) {
+int check_adapters(const qconv_adapters *ad, const qconv_rows *x) {
     if (ad->count < 0) return fail(QCONV_EINVAL, "adapters: count must be >= 0");
     if (ad->count == 0) return QCONV_OK;
     if (ad->rank < 8 || ad->rank > 128 || ad->rank % 8)
         return fail(QCONV_EUNSUPPORTED, "adapters: rank must be a multiple of 8 up to 128 (got %d)", ad->rank);
     if (x->channels % 8) return fail(QCONV_EUNSUPPORTED, "adapters need channels %% 8 == 0 (got %d)", x->channels);
-    if (!ad->a || !ad->b || !ad->alpha || !ad->row) return fail(QCONV_EINVAL, "adapters: a, b, alpha and row must be non-NULL");
+    if (!ad->a || !ad->b || !ad->alpha || (x->rows > 0 && !ad->row))
+        return fail(QCONV_EINVAL, "adapters: a, b, alpha and row must be non-NULL");
     if (!aligned(ad->a, 16) || !aligned(ad->b, 16) || !aligned(ad->alpha, 4) || !aligned(ad->row, 4))
         return fail(QCONV_EINVAL, "adapters: a and b must be 16-byte, alpha and row 4-byte aligned");
-    (void)w;
     return QCONV_OK;
 }
 
@@ -182,7 +182,7 @@ int qconv_linear(const qconv_rows *x, const qconv_rows *w, const qconv_adapters 
     if (x->channels != w->channels)
         return fail(QCONV_EINVAL, "x has %d channels, w %d", x->channels, w->channels);
     if (w->rows < 1) return fail(QCONV_EINVAL, "w has no rows");
-    if (adapters && (rc = check_adapters(adapters, x, w)) != QCONV_OK) return rc;
+    if (adapters && (rc = check_adapters(adapters, x)) != QCONV_OK) return rc;
     if ((rc = check_matrix(y, x->rows, w->rows, ldy, 2, "y")) != QCONV_OK ||
         (rc = check_tiles(x->rows, w->rows)) != QCONV_OK)
         return rc;

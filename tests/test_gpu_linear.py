@@ -320,6 +320,15 @@ def test_one_rows_fault_stays_in_its_row(L, m):
     assert torch.equal(y[~hit], clean[~hit]) and not torch.isfinite(y[hit]).any()
 
 
+def test_no_rows_with_adapters(L):
+    g = _gen(3)
+    x, w = _rows8(L, g, 4, 64), _rows8(L, g, 24, 64)
+    ad = _adapters(L, g, 2, 8, 64, 24, torch.bfloat16)
+    none = L.Rows(x.codes[:0], x.scale[:0], 64)
+    y = L.linear(none, w, adapters=ad, row_adapter=torch.empty(0, dtype=torch.int32, device="cuda"))
+    assert y.shape == (0, 24)
+
+
 def test_linear_into_a_strided_view(L):
     g = _gen(3)
     for m, k in ((5, 20), (90, 150)):

@@ -51,6 +51,15 @@ def test_nothing_to_do(L):
     assert _status(L, "qconv_linear_grad_input", None, 0, 32, 0, _rows(L), None, 256, None, 0, None) == 0
 
 
+def test_nothing_to_do_with_adapters(L):
+    """An empty tensor's pointer is NULL: of no rows none is asked for.  What is wrong
+    with the adapters themselves is refused all the same."""
+    none, w = _rows(L, None, None, rows=0), _rows(L, C, D)
+    assert _status(L, "qconv_linear", none, w, _adapters(L, row=None), None, 0, 32, None, 0, None) == 0
+    assert _status(L, "qconv_linear", none, w, _adapters(L, a=None), None, 0, 32, None, 0, None) == EINVAL
+    assert _status(L, "qconv_linear", none, w, _adapters(L, rank=12), None, 0, 32, None, 0, None) == EUNSUPPORTED
+
+
 BAD_ROWS = [
     (dict(rows=-1), EINVAL), (dict(channels=0), EINVAL), (dict(bits=16), EUNSUPPORTED), (dict(bits=0), EUNSUPPORTED),
     (dict(channels=131072, pitch=131072), EUNSUPPORTED), (dict(pitch=240), EINVAL), (dict(pitch=264), EINVAL),
