@@ -326,13 +326,23 @@ def linear_grad_weight(dy: torch.Tensor, x: Rows, *, out: torch.Tensor | None = 
     return dw
 
 
+def _readable(t: torch.Tensor) -> torch.Tensor:
+    """The matrix, or a copy where the operators do not read it in place: columns apart,
+    rows that overlap (a broadcast one), rows more than 2^21 elements apart."""
+    if t.dim() != 2:
+        return t   # (refused by the operator)
+    m, n = t.shape
+    apart = n > 1 and t.stride(1) != 1
+    return t.contiguous() if apart or (m > 1 and not n <= t.stride(0) <= 1 << 21) else t
+
+
 class _LinearLayer(torch.autograd.Function):
     """Rounding to 8 bits is taken as the identity in the backward pass: the
     gradients are those of the product of the rounded values."""
 
     @staticmethod
     def forward(ctx, x, w):
-        x8, w8 = quantize_rows(x), quantize_rows(w)
+        x8, w8 = quantize_rows(_readable(x)), quantize_rows(_readable(w))
         ctx.save_for_backward(x8.codes, x8.scale, w8.codes, w8.scale)
         ctx.channels, ctx.x_dtype, ctx.w_dtype = x8.channels, x.dtype, w.dtype
         return linear(x8, w8, dtype=x.dtype)
@@ -341,8 +351,7 @@ class _LinearLayer(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         x_codes, x_scale, w_codes, w_scale = ctx.saved_tensors
-        if dy.shape[1] > 1 and dy.stride(1) != 1 or dy.stride(0) < dy.shape[1]:
-            dy = dy.contiguous()
+        dy = _readable(dy)
         dx = dw = None
         if ctx.needs_input_grad[0]:
             dx = linear_grad_input(dy, Rows(w_codes, w_scale, ctx.channels))
@@ -353,7 +362,7 @@ class _LinearLayer(torch.autograd.Function):
 
 def linear_layer(x: torch.Tensor, w: torch.Tensor) -> torch.Tensor:
     """x (... x c, bfloat16 or float16) times the k x c weights' transpose, both
-    rounded to 8-bit rows, differentiable in both.  Between the passes only the
-    8-bit rows are kept: 1 byte a value of x instead of 2."""
+    rounded to 8-bit rows, differentiable in both.  Either may be any view.  Between
+    the passes only the 8-bit rows are kept: 1 byte a value of x instead of 2."""
     y = _LinearLayer.apply(x.reshape(-1, x.shape[-1]), w)
     return y.reshape(*x.shape[:-1], w.shape[0])

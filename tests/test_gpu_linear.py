@@ -687,6 +687,32 @@ def test_layer_trains(L, dtype):
     assert losses[-1] < losses[0] * 0.8
 
 
+@pytest.mark.parametrize("form", ["broadcast", "columns", "far rows", "weights"])
+def test_layer_takes_any_view(L, form):
+    """Views whose rows the operators do not read in place are copied by the layer: the
+    same results and gradients as of the tensors themselves."""
+    g = _gen(43)
+    w = (_randn(g, 72, 96) * 0.1).bfloat16()
+    if form == "broadcast":
+        x = _randn(g, 1, 96).bfloat16().expand(40, 96)
+    elif form == "columns":
+        x = _randn(g, 96, 40).bfloat16().t()
+    elif form == "far rows":
+        x = torch.as_strided(_randn(g, (1 << 22) + 96).bfloat16(), (2, 96), (1 << 22, 1))
+    else:
+        x, w = _randn(g, 40, 96).bfloat16(), w.t().contiguous().t()
+    dy = _randn(g, x.shape[0], 72).bfloat16()
+    x, w = x.detach().requires_grad_(), w.detach().requires_grad_()
+    plain = [t.detach().clone(memory_format=torch.contiguous_format).requires_grad_() for t in (x, w)]
+    y, want = L.linear_layer(x, w), L.linear_layer(*plain)
+    assert torch.equal(y, want)
+    y.backward(dy)
+    want.backward(dy)
+    assert torch.equal(x.grad, plain[0].grad) and torch.equal(w.grad, plain[1].grad)
+    with pytest.raises(L.QConvError):
+        L.linear_layer(plain[0], plain[1][0])
+
+
 def test_layer_keeps_only_bytes(L):
     x = torch.randn(64, 128, device="cuda").bfloat16().requires_grad_()
     w = torch.randn(32, 128, device="cuda").requires_grad_()
