@@ -20,7 +20,7 @@ int64_t round16(int64_t n) { return (n + 15) & ~(int64_t)15; }
 struct Span {
     uintptr_t begin, end;
     Span(const void *p, int64_t bytes) : begin((uintptr_t)p), end((uintptr_t)p + (bytes > 0 ? bytes : 0)) {}
-    bool meets(const Span &o) const { return begin < o.end && o.begin < end; }
+    bool meets(const Span &o) const { return begin < end && o.begin < o.end && begin < o.end && o.begin < end; }
 };
 
 // Bytes of rows x cols elements, `ld` from row to row.

@@ -28,10 +28,12 @@ def _rows(at: int, rows: int, channels: int, bits: int = 8) -> Rows:
 
 
 def _call(lib, op: str, m: int = 0, c: int = 0, k: int = 0, bits: int = 8, dtype: int = 0, adapters: int = 0, rank: int = 0,
-          stride: int = 0) -> int:
-    """One call of m rows, c channels and k outputs; stride: the gradient's, 0 for tight rows."""
+          stride: int = 0, dy: int = POINTERS[0], workspace: int = POINTERS[9]) -> int:
+    """One call of m rows, c channels and k outputs; stride: the gradient's, 0 for tight rows.
+    Operands lie at POINTERS 0 to 7 (rows: codes, then scales), results at POINTERS[8]."""
     i32, i64, vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p
     size, need, P = ctypes.c_size_t, ctypes.c_size_t(0), POINTERS
+    dy, workspace = vp(dy), vp(workspace)
     if op == "rows":
         return lib.qconv_quantize_rows(vp(P[0]), i32(dtype), i64(c), i32(m), i32(c), vp(P[1]), i64((c + 15) // 16 * 16),
                                        vp(P[2]), None)
@@ -40,14 +42,14 @@ def _call(lib, op: str, m: int = 0, c: int = 0, k: int = 0, bits: int = 8, dtype
         with_ad = ctypes.byref(ad) if adapters else None
         lib.qconv_linear_workspace_bytes(i32(m), i32(c), with_ad, ctypes.byref(need))
         return lib.qconv_linear(ctypes.byref(_rows(0, m, c)), ctypes.byref(_rows(2, k, c, bits)), with_ad, vp(P[8]),
-                                i32(dtype), i64(k), vp(P[9]), size(need.value), None)
+                                i32(dtype), i64(k), workspace, size(need.value), None)
     sizes = (m, c, k) if op == "grad_input" else (k, c, m)
     lib.qconv_linear_grad_workspace_bytes(*map(i32, sizes), ctypes.byref(need))
     if op == "grad_input":
-        return lib.qconv_linear_grad_input(vp(P[0]), i32(dtype), i64(stride or k), i32(m), ctypes.byref(_rows(2, k, c, bits)),
-                                           vp(P[8]), i64(c), vp(P[9]), size(need.value), None)
-    return lib.qconv_linear_grad_weight(vp(P[0]), i32(dtype), i64(stride or k), i32(k), ctypes.byref(_rows(2, m, c)),
-                                        vp(P[8]), i64(c), vp(P[9]), size(need.value), None)
+        return lib.qconv_linear_grad_input(dy, i32(dtype), i64(stride or k), i32(m), ctypes.byref(_rows(2, k, c, bits)),
+                                           vp(P[8]), i64(c), workspace, size(need.value), None)
+    return lib.qconv_linear_grad_weight(dy, i32(dtype), i64(stride or k), i32(k), ctypes.byref(_rows(2, m, c)),
+                                        vp(P[8]), i64(c), workspace, size(need.value), None)
 
 
 def record(tmp, steps: list) -> dict:

@@ -1,7 +1,7 @@
 """What the linear layer's entry points launch, recorded without a GPU."""
 import pytest
 
-from _launches import record
+from _launches import POINTERS, record
 
 
 @pytest.fixture(scope="module")
@@ -38,3 +38,13 @@ def test_a_refused_lds_limit_is_asked_for_again(tmp):
         (_, _), (status, events), (again, then) = record(tmp, [{"refuse": 1}, call, call])["events"]
         assert status == -4 and not events
         assert again == 0 and [e[0] for e in then] == ["attribute", "launch"]
+
+
+def test_what_holds_nothing_overlaps_nothing(tmp):
+    """A gradient of no rows, or a workspace that the call does not need, may point
+    anywhere: within an output or an input too."""
+    steps = [dict(op="grad_weight", m=0, c=64, k=32, dy=POINTERS[8] + 64),
+             dict(op="linear", m=32, c=256, k=32, workspace=POINTERS[0] + 64),
+             dict(op="linear", m=32, c=256, k=32, workspace=POINTERS[8] + 64),
+             dict(op="grad_input", m=32, c=64, k=32, workspace=POINTERS[0] + 64)]
+    assert [status for status, _ in record(tmp, steps)["events"]] == [0] * len(steps)
