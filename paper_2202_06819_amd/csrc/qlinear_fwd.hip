@@ -65,9 +65,13 @@ Kind plan_linear(const LinearArgs &a, int w_bits) {
     const auto consider = [&](Kind kind, double us) {
         if (best_us == 0 || us < best_us) best = kind, best_us = us;
     };
-    for (const auto &f : kFew)
+    for (const auto &f : kFew) {
+        // (without adapters tiles of 64 are as fast wherever 64 rows a workgroup could be
+        // chosen: never with 8-bit weights, within 1 % with 4-bit ones of 5700 channels)
+        if (f.kind == Kind::FEW_2x4 && !a.ad.count) continue;
         consider(f.kind, 1.5 + on_cu(f.channels, f.rows) * (f.start + f.step * (w_bits == 8 ? 1.2 : 1.0) * a.c / 1024.0 +
                                                             (a.ad.count ? f.adapters : 0.0)));
+    }
     for (const auto &t : kTiles) {
         const int64_t n = on_cu(t.size, t.size), rest = n % t.resident;
         const double *steps = w_bits == 8 ? t.steps8 : t.steps4;
@@ -89,7 +93,9 @@ hipError_t product(const LinearArgs &a, hipStream_t stream) {
         case Kind::FEW_1x1: return few<T, WB, 1, 1, AD>(a, stream);
         case Kind::FEW_2x1: return few<T, WB, 2, 1, AD>(a, stream);
         case Kind::FEW_2x2: return few<T, WB, 2, 2, AD>(a, stream);
-        case Kind::FEW_2x4: return few<T, WB, 2, 4, AD>(a, stream);
+        case Kind::FEW_2x4:
+            if constexpr (AD) return few<T, WB, 2, 4, AD>(a, stream);
+            [[fallthrough]];
         case Kind::TILE_64x4: return tile<T, linear_tile<T, WB, 64, 64, 1, 4, 4, AD>, 64, 64, 4, 1024, AD>(a, stream);
         case Kind::TILE_64x2: return tile<T, linear_tile<T, WB, 64, 64, 1, 4, 2, AD>, 64, 64, 2, 512, AD>(a, stream);
         case Kind::TILE_64: return tile<T, linear_tile<T, WB, 64, 64, 1, 4, 1, AD>, 64, 64, 1, 256, AD>(a, stream);

@@ -1,6 +1,7 @@
 """What the linear layer's entry points launch, recorded without a GPU."""
 import pytest
 
+import linear_sizes as sizes
 from _launches import POINTERS, record
 
 
@@ -48,3 +49,50 @@ def test_what_holds_nothing_overlaps_nothing(tmp):
              dict(op="linear", m=32, c=256, k=32, workspace=POINTERS[8] + 64),
              dict(op="grad_input", m=32, c=64, k=32, workspace=POINTERS[0] + 64)]
     assert [status for status, _ in record(tmp, steps)["events"]] == [0] * len(steps)
+
+
+OURS = ("quantize_rows", "linear_few", "linear_tile", "adapter_rows", "grad_tile", "grad_sum")
+
+
+def _forms(step, events):
+    """Each kernel that the call launched, in the form that its results take there."""
+    names = [e[2] for e in events if e[0] == "launch"]
+    split = any("grad_sum" in n for n in names)
+    for kind, _, name, *rest in events:
+        if kind != "launch":
+            continue
+        if "grad_tile" in name:
+            yield name, "split" if split else "whole"
+        elif "adapter_rows" in name:
+            yield name, "whole" if rest[0].split()[1] == "1" else "split"
+        elif "linear_tile" in name and step["adapters"]:
+            yield name, "64 ranks" if step["rank"] <= 64 else "more ranks"
+        else:
+            yield name, ""
+
+
+def test_the_parity_tests_sizes_launch_every_kernel(tmp):
+    """The sizes that the GPU tests compare reach every kernel that the library holds, in
+    every form; a model of times that changes may not take one from them, or leave one
+    that no call reaches."""
+    steps = [dict(op="rows", m=m, c=c, dtype=t) for m, c in sizes.ROWS for t in range(3)]
+    for t in (0, 1):
+        steps += [dict(op="linear", m=m, c=c, k=k, bits=bits, adapters=n, rank=rank, dtype=t)
+                  for m, c, k, bits, n, rank in sizes.LINEAR]
+        steps += [dict(op="grad_input", m=m, c=c, k=k, bits=bits, dtype=t) for m, c, k, bits in sizes.GRAD_INPUT]
+        steps += [dict(op="grad_weight", m=m, c=c, k=k, dtype=t) for m, c, k in sizes.GRAD_WEIGHT]
+    done = record(tmp, steps)
+    reached = set()
+    for step, (status, events) in zip(steps, done["events"]):
+        assert status == 0, step
+        reached.update(_forms(step, events))
+    want = set()
+    for name in done["kernels"]:
+        if any(o in name for o in OURS):
+            if "grad_tile" in name or "adapter_rows" in name:
+                want.update({(name, "whole"), (name, "split")})
+            elif "linear_tile" in name and "true" in name:
+                want.update({(name, "64 ranks"), (name, "more ranks")})
+            else:
+                want.add((name, ""))
+    assert len(want) > 200 and not want - reached, "\n".join(map(str, sorted(want - reached)))
