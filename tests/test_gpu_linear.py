@@ -13,6 +13,8 @@ import math
 import pytest
 import torch
 
+import linear_sizes as sizes
+
 pytestmark = pytest.mark.gpu
 
 HALF_ULP = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
@@ -531,6 +533,52 @@ def test_grads_are_the_forward_products_differences(L):
             diff = loss(*args[0]) - loss(*args[1])
             scale = float((dy.double().abs() @ wv.abs())[i, j] if which == 0 else (dy.double().abs().t() @ xv.abs())[i, j])
             assert abs(diff - float(grad[i, j])) <= scale * 2.0 ** -8
+
+
+# --------------------------------------------------- every kernel, in every form
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,c,k,bits,n,rank", sizes.LINEAR)
+def test_every_kernel_of_the_projection(L, m, c, k, bits, n, rank, dtype):
+    g = _gen(m + c + k + rank)
+    x = _rows8(L, g, m, c)
+    w, q = _rows4(L, g, k, c) if bits == 4 else (_rows8(L, g, k, c), None)
+    base = _product(x, w, q)
+    if not n:
+        _near(L.linear(x, w, dtype=dtype), base, base.abs(), 4, dtype)
+        return
+    ad = _adapters(L, g, n, rank, c, k, dtype)
+    ids = torch.randint(-1, n, (m,), generator=g, device="cuda", dtype=torch.int32)
+    part, size, coarse = _adapter_part(x, ad, ids)
+    want = base + part
+    y = L.linear(x, w, dtype=dtype, adapters=ad, row_adapter=ids)
+    tol = (coarse * (HALF_ULP[dtype] ** 2 + 2.0 ** -24) + size * (c + 2 * rank + 8) * 2.0 ** -24 + base.abs() * 2.0 ** -22) * 1.01
+    tol = tol + HALF_ULP[dtype] * want.abs() + (2.0 ** -25 if dtype == torch.float16 else 0.0)
+    assert ((y.double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,c,k,bits", sizes.GRAD_INPUT)
+def test_every_kernel_of_the_input_gradient(L, m, c, k, bits, dtype):
+    g = _gen(m + c + k + bits)
+    dy = _dy(g, m, k, dtype, k + 8)
+    if bits == 4:
+        w, q = _rows4(L, g, k, c)
+        values, extra = _values(w, q), HALF_ULP[dtype] * 1.01
+    else:
+        w = _rows8(L, g, k, c)
+        values, extra = _values(w), 0.0
+    want, size = dy.double().contiguous() @ values, dy.double().abs().contiguous() @ values.abs()
+    _near(L.linear_grad_input(dy, w), want, size, k, dtype, extra=extra)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,c,k", sizes.GRAD_WEIGHT)
+def test_every_kernel_of_the_weight_gradient(L, m, c, k, dtype):
+    g = _gen(m + c + k)
+    dy, x = _dy(g, m, k, dtype, k + 8), _rows8(L, g, m, c)
+    want, size = dy.double().t().contiguous() @ _values(x), dy.double().abs().t().contiguous() @ _values(x).abs()
+    _near(L.linear_grad_weight(dy, x), want, size, m, torch.float32)
 
 
 # ----------------------------------------------------- streams, graphs, layer
