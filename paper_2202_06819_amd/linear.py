@@ -21,7 +21,8 @@ weights are rows of the same form (8-bit, or 4-bit from :func:`pack_rows4`) in
 ``adapters`` the forward product serves many requests, each with its own
 low-rank adapter.  Tensors may live on any GPU: a call runs on their device's
 current stream, or on ``stream`` (a torch stream or a raw handle), after that
-stream's earlier work and no other's; what it allocates is that stream's memory.
+stream's earlier work and no other's; what it allocates is that stream's memory, and
+what it reads is kept until it has run.
 """
 from __future__ import annotations
 
@@ -141,6 +142,15 @@ def _as_stream(stream, device: torch.device) -> torch.cuda.Stream:
     return torch.cuda.ExternalStream(_stream(stream, device), device=device)
 
 
+def _hold(stream, *tensors) -> None:
+    """Keeps the memory of what a call on ``stream`` reads or writes until it has run,
+    should the caller give it back before."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(_as_stream(stream, t.device))
+
+
 def _on(device: torch.device, out: torch.Tensor | None, shape: tuple, dtype: torch.dtype, name: str,
         stream) -> torch.Tensor:
     """The output: new, or the caller's after a check."""
@@ -203,6 +213,7 @@ def quantize_rows(x: torch.Tensor, out: Rows | None = None, stream=None) -> Rows
         to = (r.codes, r.pitch, r.scale)
     _check(_call(device, _lib().qconv_quantize_rows, x.data_ptr(), DTYPES[x.dtype], _ld(x), m, c, *to,
                  _stream(stream, device)), "qconv_quantize_rows")
+    _hold(stream, x, out.codes, out.scale)
     return out
 
 
@@ -220,6 +231,7 @@ def pack_rows4(codes: torch.Tensor, scale: torch.Tensor, stream=None) -> Rows:
     current = torch.cuda.current_stream(device)
     # (the copies too: they are made and given back on the stream that reads them)
     with torch.cuda.stream(current if stream is None else _as_stream(stream, device)):
+        _hold(stream, codes)
         if c % 32:
             codes = torch.nn.functional.pad(codes, (0, 32 - c % 32))
         words = qconv.pack(codes.contiguous().reshape(k, -1, 1, 1), 4, True)
@@ -270,6 +282,7 @@ def linear(x: Rows, w: Rows, *, dtype: torch.dtype = torch.bfloat16, adapters: A
     keep, ws, ws_bytes = _workspace(need, workspace, device, stream)
     _check(_call(device, L.qconv_linear, ctypes.byref(rx), ctypes.byref(rw), ad, y.data_ptr(), DTYPES[dtype], _ld(y), ws,
                  ws_bytes, _stream(stream, device)), "qconv_linear")
+    _hold(stream, *x[:2], *w[:2], *(adapters or ()), row_adapter, out, workspace)
     return y
 
 
@@ -306,6 +319,7 @@ def linear_grad_input(dy: torch.Tensor, w: Rows, *, out: torch.Tensor | None = N
     keep, ws, ws_bytes = _workspace(grad_workspace_bytes(m, rw.channels, rw.rows), workspace, device, stream)
     _check(_call(device, _lib().qconv_linear_grad_input, dy.data_ptr(), DTYPES[dy.dtype], _ld(dy), m, ctypes.byref(rw),
                  dx.data_ptr(), _ld(dx), ws, ws_bytes, _stream(stream, device)), "qconv_linear_grad_input")
+    _hold(stream, dy, *w[:2], out, workspace)
     return dx
 
 
@@ -323,6 +337,7 @@ def linear_grad_weight(dy: torch.Tensor, x: Rows, *, out: torch.Tensor | None = 
     keep, ws, ws_bytes = _workspace(grad_workspace_bytes(k, rx.channels, m), workspace, device, stream)
     _check(_call(device, _lib().qconv_linear_grad_weight, dy.data_ptr(), DTYPES[dy.dtype], _ld(dy), k, ctypes.byref(rx),
                  dw.data_ptr(), _ld(dw), ws, ws_bytes, _stream(stream, device)), "qconv_linear_grad_weight")
+    _hold(stream, dy, *x[:2], out, workspace)
     return dw
 
 

@@ -709,6 +709,40 @@ def test_pack_rows4_on_a_given_stream(L, c, contiguous):
     assert (read == 77).all()
 
 
+@pytest.mark.parametrize("op", ["quantize_rows", "linear", "linear_grad_input", "linear_grad_weight", "pack_rows4"])
+def test_operands_are_kept_until_a_given_stream_has_read_them(L, op):
+    """What a call on another stream reads may be given back on the current one right
+    after the call: its memory is not used again before the call has run."""
+    g = _gen(63)
+    m, c, k = 2048, 512, 512
+    x, w, v, dy = _rows8(L, g, m, c), _rows8(L, g, k, c), _randn(g, m, c).bfloat16(), _dy(g, m, k, torch.bfloat16)
+    ad = _adapters(L, g, 2, 16, c, k, torch.bfloat16)
+    ids = torch.randint(-1, 2, (m,), generator=g, device="cuda", dtype=torch.int32)
+    calls = {"quantize_rows": ([v], lambda t, **on: L.quantize_rows(*t, **on).codes),
+             "linear": ([x.codes, x.scale, w.codes, w.scale, *ad, ids],
+                        lambda t, **on: L.linear(L.Rows(t[0], t[1], c), L.Rows(t[2], t[3], c),
+                                                 adapters=L.Adapters(*t[4:7]), row_adapter=t[7], **on)),
+             "linear_grad_input": ([dy, w.codes, w.scale],
+                                   lambda t, **on: L.linear_grad_input(t[0], L.Rows(*t[1:], c), **on)),
+             "linear_grad_weight": ([dy, x.codes, x.scale],
+                                    lambda t, **on: L.linear_grad_weight(t[0], L.Rows(*t[1:], c), **on)),
+             "pack_rows4": ([x.codes, x.scale], lambda t, **on: L.pack_rows4(*t, **on).codes)}
+    operands, call = calls[op]
+    want = call(operands)
+    s = torch.cuda.Stream()
+    call(operands, stream=s)
+    mine = [t.clone() for t in operands]
+    sizes_of = [t.numel() * t.element_size() for t in mine]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(200_000_000)
+    got = call(mine, stream=s)
+    del mine
+    new = [torch.full((n,), 99, dtype=torch.uint8, device="cuda") for n in sizes_of * 2]
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and all((t == 99).all() for t in new)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_layer_trains(L, dtype):
     """The differentiable layer: gradients of the rounded product, and a few
