@@ -743,6 +743,39 @@ def test_operands_are_kept_until_a_given_stream_has_read_them(L, op):
     assert torch.equal(got, want) and all((t == 99).all() for t in new)
 
 
+def test_a_given_stream_within_a_capture(L):
+    """A captured step whose calls are given a stream that forks from the capturing one
+    and joins it again: replays, with other work between them, equal the eager results."""
+    g = _gen(64)
+    m, c, k = 70, 256, 96
+    v, w, dy = _randn(g, m, c).bfloat16(), _rows8(L, g, k, c), _dy(g, m, k, torch.bfloat16)
+    q = torch.randint(-8, 8, (k, 264), generator=g, device="cuda").to(torch.int8)
+    ad = _adapters(L, g, 3, 16, c, k, torch.bfloat16)
+    ids = torch.randint(-1, 3, (m,), generator=g, device="cuda", dtype=torch.int32)
+
+    def step(**on):
+        x = L.quantize_rows(v, **on)
+        return (x.codes, L.linear(x, w, adapters=ad, row_adapter=ids, **on), L.linear_grad_input(dy, w, **on),
+                L.linear_grad_weight(dy, x, **on), L.pack_rows4(q, w.scale, **on).codes)
+
+    eager = [t.clone() for t in step()]
+    side = torch.cuda.Stream()
+    step(stream=side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        outs = step(stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+    for _ in range(4):
+        for t in outs:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(eager, outs))
+        (v.float() @ v.float().t()).sum().item()
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_layer_trains(L, dtype):
     """The differentiable layer: gradients of the rounded product, and a few
