@@ -506,9 +506,12 @@ int qconv2d_scheduled(const qconv_desc *d, const void *x, const void *w_prepared
  *   weight gradient   dw[k][c] = sum_m dy[m][k] x[m][c]
  * Conventions as above: device pointers, nothing allocated or kept, work
  * enqueued on `stream`, arguments checked before anything is enqueued.
- * Views are allowed throughout (row strides in elements), and no alignment
- * beyond the element's is asked of x, y, dy, dx and dw; a dy whose rows start on
- * 16-byte boundaries and hold a multiple of 8 values is read the fastest way.
+ * Views are allowed throughout (row strides in elements, at most 2^21), and no
+ * alignment beyond the element's is asked of x, y, dy, dx and dw; a dy whose rows
+ * start on 16-byte boundaries and hold a multiple of 8 values is read the fastest
+ * way.  "Must not overlap" is meant of whole ranges, from an operand's first byte
+ * to its last, gaps between its rows included.  A result of more than 2^22 tiles
+ * of 64 x 64 is refused (QCONV_EUNSUPPORTED).
  */
 #define QCONV_BF16 0
 #define QCONV_F16 1
@@ -541,8 +544,8 @@ typedef struct qconv_rows {
  * A row of zeros has scale 0.  A row with an infinity or a NaN has scale NaN
  * and codes 0: all that is computed from it is NaN.  Scales are powers of two
  * so that the quotient, and later code * scale in 16-bit floats, are exact.
- *   x       DEVICE, m x c of `dtype` (QCONV_BF16, _F16 or _F32), ldx >= c
- *           elements from row to row
+ *   x       DEVICE, m x c of `dtype` (QCONV_BF16, _F16 or _F32), ldx elements
+ *           from row to row, c to 2^21
  *   codes   DEVICE, 16-byte aligned, m rows of `pitch` bytes (a multiple of 16,
  *           >= c rounded up to 16); written up to c rounded up to 16
  *   scale   DEVICE, m floats
@@ -574,11 +577,12 @@ typedef struct qconv_adapters {
 
 /*
  * qconv_linear -- y[m][k] = sum_c x[m][c] w[k][c], plus the adapters' part, as
- * floats of `dtype` (QCONV_BF16 or QCONV_F16), rounded once.
+ * floats of `dtype` (QCONV_BF16 or QCONV_F16), rounded once.  The sum of codes is
+ * a whole number, exact; x's scale and then w's multiply it in 32 bits.
  *   x   8-bit rows;  w   8-bit or 4-bit rows with the same channels
  *   adapters  NULL, or as above (count == 0: none)
- *   y   DEVICE, x->rows x w->rows, ldy >= w->rows elements from row to row; must
- *       not overlap an input or the workspace
+ *   y   DEVICE, x->rows x w->rows, ldy elements from row to row, w->rows to 2^21;
+ *       must not overlap an input or the workspace
  *   workspace  DEVICE, 16-byte aligned, qconv_linear_workspace_bytes (0 without
  *       adapters); its contents need no preparation and mean nothing afterwards.
  *       Calls that share one must not overlap in time.

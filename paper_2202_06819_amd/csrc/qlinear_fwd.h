@@ -436,7 +436,7 @@ __global__ void __launch_bounds__(512) linear_few(LinearArgs a) {
 // read once for a tile, however its rows lie.  KS groups of THREADS threads deal the
 // adapters out among them; a row's products are in the group that had its adapter.
 // Bound by the wait for an adapter's B, one step ahead: 2003 rows, 2048 to 8192 channels,
-// 5 adapters of rank 64 take 47 us, 43 without them.
+// 5 adapters of rank 64 take 49 us, 42 without them.
 template <class T, int TJ, int TI, int THREADS, int KS>
 struct TileAdapters {
     const LinearArgs &a;
@@ -601,7 +601,7 @@ constexpr int tile_lds() {
 // hide each other's waits (256 rows of 8192 channels, 4096 outputs of 4 bits: 32 us with
 // one group, 21.6 with two, 19.5 with four).  The largest tile is bound by the matrix
 // cores, which its random operands hold to what power allows: 8192 x 4096 x 4096 takes
-// 119 us, 2.31 POP/s of the 3.1 that products of registers alone reach.
+// 118 to 124 us, 2.2 to 2.3 POP/s of the 3.1 that products of registers alone reach.
 template <class T, int WB, int TJ, int TI, int WJ, int WI, int KS, bool AD>
 __global__ void __launch_bounds__(KS *WJ *WI * 64, TJ == 64 ? 4 : 2) linear_tile(LinearArgs a) {
     constexpr int FJ = 4, FI = TI / (16 * WI), kThreads = WJ * WI * 64, kBuffer = (TJ + TI) * kStepBytes;

@@ -8,7 +8,11 @@
 // operand that has t outermost is read by transposing loads.  A code times its scale
 // is formed in 32 bits and rounded to the 16-bit type: exact for scales that are
 // powers of two (as the quantiser gives them); for others it is one rounding of each
-// operand to the gradient's own precision.  Sums are 32-bit.
+// operand to the gradient's own precision, which adds about as much error as the result's
+// own rounding: relative to the results 0.0024 instead of 0.0017 in bf16 (4-bit weights,
+// 4096 of them summed), 0.0003 instead of 0.0002 in f16.  (What the rounding leaves, as a
+// second product, takes that away and doubles the matrix instructions: tried, 19 -> 40 us
+// for 333 rows of 2824 by 1001, 235 -> 589 for 8192 x 4096 x 4096.)  Sums are 32-bit.
 #pragma once
 
 #include "qlinear_device.h"
@@ -77,7 +81,7 @@ __device__ __forceinline__ typename T::v8 read_transposed(const uint8_t *lds, in
 // can give.  Where loads go through registers, the smaller tiles keep those of two steps
 // on their way (777 rows, 1411 x 1003 in f16: 18.1 us, with one 19.8; the largest tile
 // has no registers left for it).  The largest tile is bound by the matrix cores and the
-// conversions beside them: 8192 x 4096 x 4096 takes 215 to 221 us, 1.25 PFLOP/s of the
+// conversions beside them: 8192 x 4096 x 4096 takes 219 to 229 us, 1.2 PFLOP/s of the
 // 1.53 that products of registers alone reach.
 template <int TJ>
 __device__ __forceinline__ int code_unit_of(int t) {

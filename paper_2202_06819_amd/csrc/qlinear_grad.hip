@@ -66,8 +66,9 @@ hipError_t grad(GradArgs a, bool transposed, int w_bits, hipStream_t stream) {
 // in a tile of 256 (one workgroup fits a CU), 0.83 alone and 1.25 for two on a CU in one
 // of 128, 0.5 to 1.1 for one to four in one of 64; two groups of a tile of 64 take a step
 // each in 0.57, four in 1.0; a split adds a launch and its partial sums' way through
-// memory.  E.g. 1024 x 1024 from 32768 rows: 79 us in 16 tiles of 256 split 16 ways, 101
-// in 64 of 128 split 8 ways, 133 in 256 of 64 split 8 ways, 141 of four groups; from 2560
+// memory.  E.g. (the fastest of some replays; calls one by one take a few percent
+// longer) 1024 x 1024 from 32768 rows: 79 us in 16 tiles of 256 split 16 ways, 101 in 64
+// of 128 split 8 ways, 133 in 256 of 64 split 8 ways, 141 of four groups; from 2560
 // rows: 14.2 in tiles of 64 with four groups, 14.7 with two, 21.6 with one, 22.4 in 128
 // split 4 ways, 28.4 in 256 split 8 ways; from 1024: 8.3 with two groups, 9.2 with four,
 // 10.6 with one, 18.6 in 128.  512 x 1024 from 4096: 17.2 with four groups split 2 ways.

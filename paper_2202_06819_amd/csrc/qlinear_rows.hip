@@ -18,7 +18,7 @@ namespace {
 
 // Eight values of a row from element `at`, zero from c on.  Whole ones are loaded in
 // 16-byte accesses whatever the row's alignment (1021 x 5003 floats of rows that start
-// on 8-byte boundaries: 12.4 us by single elements, 5.7 so).
+// on 8-byte boundaries: 12.6 us by single elements, 5.0 so, in a graph).
 template <class In>
 __device__ __forceinline__ void load8(const In *row, int at, int c, float (&v)[8]) {
     typedef In whole __attribute__((ext_vector_type(16 / sizeof(In))));
