@@ -619,6 +619,52 @@ int qconv_linear_grad_input(const void *dy, int32_t dtype, int64_t lddy, int32_t
 int qconv_linear_grad_weight(const void *dy, int32_t dtype, int64_t lddy, int32_t k, const qconv_rows *x, float *dw,
                              int64_t lddw, void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * Around the linear layer: the norm that makes its 8-bit rows.
+ *
+ * qconv_norm_rows -- root-mean-square norm with the residual's addition, to 8-bit rows:
+ *   h[m][c] = x[m][c] + residual[m][c], rounded to their type   (x itself without one)
+ *   r[m]    = (mean_c h[m][c]^2 + eps)^(-1/2)
+ *   y[m][c] = h[m][c] r[m] gain[c]
+ *   codes, scale: y as qconv_quantize_rows quantises its rows
+ * The mean and r are formed in 64 bits and a code is the rounding of the 64-bit y (ties
+ * to even), so it does not depend on the order of a sum.  A row in which an h or a y is
+ * not a finite 32-bit float has scale NaN and codes 0; a row of zeros with eps == 0 is one.
+ *   x, residual   DEVICE, m x c of `dtype`; ldx, ldr elements from row to row, to 2^21.
+ *                 residual NULL: none
+ *   sum           DEVICE, h: m x c of `dtype`, lds from row to row; NULL exactly if
+ *                 residual is.  May be the whole of x or of the residual.
+ *   gain          DEVICE, c of `gain_dtype` (QCONV_BF16, _F16 or _F32, whatever dtype is)
+ *   eps           from 0 to 1e30
+ *   codes, pitch, scale   as of qconv_quantize_rows
+ *   rstd          DEVICE, m floats: r, for the gradient; may be NULL
+ * m == 0 is a no-op.  One launch.  Other rules, and limits, as above.
+ */
+int qconv_norm_rows(const void *x, int64_t ldx, const void *residual, int64_t ldr, void *sum, int64_t lds, int32_t dtype,
+                    const void *gain, int32_t gain_dtype, double eps, int32_t m, int32_t c, void *codes, int64_t pitch,
+                    float *scale, float *rstd, void *stream);
+
+/*
+ * qconv_norm_rows_grad -- its gradient, the rounding to codes taken as the identity:
+ *   n[m][c]  = h[m][c] rstd[m];   t[m][c] = dy[m][c] gain[c]
+ *   dx[m][c] = rstd[m] (t[m][c] - n[m][c] mean_c' t[m][c'] n[m][c'])  (+ dsum[m][c])
+ *   dgain[c] = sum_m dy[m][c] n[m][c]
+ * dx is the gradient of x and of the residual alike.  Sums are 32-bit, in an order that
+ * does not change from call to call.
+ *   dy, h, dx  DEVICE, m x c of `dtype` (any of the three), lddy, ldh, lddx from row to row;
+ *              h: what qconv_norm_rows gave as sum (without a residual: its x)
+ *   dsum       DEVICE, m x c: the gradient that arrives at h by other ways; NULL: none.
+ *              dx may be the whole of it.
+ *   rstd       DEVICE, m floats;  dgain  DEVICE, c floats (of m == 0: zeros)
+ *   workspace  DEVICE, 16-byte aligned, qconv_norm_rows_grad_workspace_bytes; rules as
+ *              of qconv_linear
+ * Two launches.
+ */
+int qconv_norm_rows_grad_workspace_bytes(int32_t m, int32_t c, size_t *bytes);
+int qconv_norm_rows_grad(const void *dy, int64_t lddy, const void *h, int64_t ldh, const void *dsum, int64_t ldds,
+                         int32_t dtype, const void *gain, int32_t gain_dtype, const float *rstd, int32_t m, int32_t c,
+                         void *dx, int64_t lddx, float *dgain, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Number of compiled tile configurations; ids are 0 .. count-1. */
 int qconv_tile_count(void);
 

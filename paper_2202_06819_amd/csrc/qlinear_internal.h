@@ -28,6 +28,29 @@ struct QuantizeArgs {
     int32_t m, c;
 };
 
+struct NormArgs {
+    const void *x, *residual;    // residual: may be NULL, then sum is too
+    void *sum;
+    int64_t ldx, ldr, lds;       // elements from row to row
+    const void *gain;
+    uint8_t *codes;
+    int64_t pitch;
+    float *scale, *rstd;         // rstd: may be NULL
+    double eps;
+    int32_t gain_dtype, m, c;
+};
+
+struct NormGradArgs {
+    const void *dy, *h, *dsum;   // dsum: may be NULL
+    void *dx;
+    int64_t lddy, ldh, ldds, lddx;
+    const void *gain;
+    const float *rstd;
+    float *dgain, *part;         // part: `parts` rows of partial sums of dgain
+    int64_t ldpart;
+    int32_t gain_dtype, m, c, parts;
+};
+
 struct AdapterArgs {
     const void *a;       // adapters x rank x c
     const void *b;       // adapters x k x rank
@@ -64,6 +87,9 @@ struct GradArgs {
 };
 
 hipError_t launch_quantize_rows(const QuantizeArgs &a, int dtype, hipStream_t stream);
+hipError_t launch_norm_rows(const NormArgs &a, int dtype, hipStream_t stream);
+hipError_t launch_norm_grad(const NormGradArgs &a, int dtype, hipStream_t stream);
+int norm_grad_parts(int64_t m);   // workgroups of the norm's gradient: rows of its workspace
 hipError_t launch_linear(const LinearArgs &a, int w_bits, int dtype, hipStream_t stream);
 hipError_t launch_grad(const GradArgs &a, bool transposed, int w_bits, int dtype, hipStream_t stream);
 

@@ -10,29 +10,11 @@
 // One pass: a row's values stay in registers between its maximum and its
 // codes.  Bound by memory (2 or 4 bytes read and 1 written a value): 8192 x 4096 bf16
 // take 16.6 us, 6.05 TB/s.
-#include "qlinear_device.h"
+#include "qlinear_rows.h"
 
 namespace qconv {
 
 namespace {
-
-// Eight values of a row from element `at`, zero from c on.  Whole ones are loaded in
-// 16-byte accesses whatever the row's alignment (1021 x 5003 floats of rows that start
-// on 8-byte boundaries: 12.6 us by single elements, 5.0 so, in a graph).
-template <class In>
-__device__ __forceinline__ void load8(const In *row, int at, int c, float (&v)[8]) {
-    typedef In whole __attribute__((ext_vector_type(16 / sizeof(In))));
-    if (at + 8 <= c) {
-        whole w[sizeof(In) / 2];
-#pragma unroll
-        for (int h = 0; h < (int)sizeof(In) / 2; ++h) __builtin_memcpy(&w[h], row + at + 16 / sizeof(In) * h, 16);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)w[i * sizeof(In) / 16][i % (16 / sizeof(In))];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = at + i < c ? (float)row[at + i] : 0.0f;
-    }
-}
 
 __device__ __forceinline__ uint32_t abs_max8(const float (&v)[8], uint32_t m) {
 #pragma unroll

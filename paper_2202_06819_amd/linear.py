@@ -36,7 +36,7 @@ from .qconv import EINVAL, QConvError, _check
 
 DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
-_i32, _i64, _vp, _size = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t
+_i32, _i64, _vp, _size, _f64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_double
 
 
 class Rows(NamedTuple):
@@ -56,6 +56,13 @@ class Adapters(NamedTuple):
     a: torch.Tensor          # adapters x rank x c
     b: torch.Tensor          # adapters x k x rank
     alpha: torch.Tensor      # float32, one factor for each adapter
+
+
+class Normed(NamedTuple):
+    """What :func:`norm_rows` gives: the 8-bit rows, and what its gradient reads."""
+    rows: Rows
+    sum: torch.Tensor        # x plus the residual, or x itself
+    rstd: torch.Tensor       # float32, one for each row
 
 
 class QConvRows(ctypes.Structure):
@@ -80,7 +87,12 @@ def _lib():
         L.qconv_linear_grad_workspace_bytes.argtypes = [_i32, _i32, _i32, P(_size)]
         L.qconv_linear_grad_input.argtypes = [_vp, _i32, _i64, _i32, P(QConvRows), _vp, _i64, _vp, _size, _vp]
         L.qconv_linear_grad_weight.argtypes = [_vp, _i32, _i64, _i32, P(QConvRows), _vp, _i64, _vp, _size, _vp]
-        for f in ("qconv_quantize_rows", "qconv_linear_workspace_bytes", "qconv_linear",
+        L.qconv_norm_rows.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _i32, _f64, _i32, _i32, _vp, _i64, _vp, _vp,
+                                      _vp]
+        L.qconv_norm_rows_grad_workspace_bytes.argtypes = [_i32, _i32, P(_size)]
+        L.qconv_norm_rows_grad.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _i32, _vp, _i32, _i32, _vp, _i64, _vp,
+                                           _vp, _size, _vp]
+        for f in ("qconv_quantize_rows", "qconv_norm_rows", "qconv_norm_rows_grad_workspace_bytes", "qconv_norm_rows_grad", "qconv_linear_workspace_bytes", "qconv_linear",
                   "qconv_linear_grad_workspace_bytes", "qconv_linear_grad_input", "qconv_linear_grad_weight"):
             getattr(L, f).restype = ctypes.c_int
         _calls = L
@@ -215,6 +227,87 @@ def quantize_rows(x: torch.Tensor, out: Rows | None = None, stream=None) -> Rows
                  _stream(stream, device)), "qconv_quantize_rows")
     _hold(stream, x, out.codes, out.scale)
     return out
+
+
+def _gain(t: torch.Tensor, c: int, device: torch.device) -> None:
+    if t.dtype not in DTYPES or t.shape != (c,) or not t.is_contiguous() or t.device != device:
+        raise QConvError(EINVAL, f"gain must be {c} contiguous bfloat16, float16 or float32 on {device}")
+
+
+def _like(t: torch.Tensor, x: torch.Tensor, name: str) -> None:
+    if t.dtype is not x.dtype or t.shape != x.shape or t.device != x.device:
+        raise QConvError(EINVAL, f"{name} must be {tuple(x.shape)} of {x.dtype} on {x.device}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise QConvError(EINVAL, f"{name}: the columns of a row must be contiguous")
+
+
+def _rows_out(out: Rows | None, m: int, c: int, device: torch.device, stream) -> Rows:
+    """8-bit rows to write: new, or the caller's after a check."""
+    if out is None:
+        return Rows(_empty((m, rows_pitch(c)), torch.int8, device, stream), _empty(m, torch.float32, device, stream), c)
+    if out.bits != 8 or out.channels != c or out.codes.shape[0] != m:
+        raise QConvError(EINVAL, f"out must be 8-bit rows, {m} of {c} channels")
+    return out
+
+
+def norm_rows(x: torch.Tensor, gain: torch.Tensor, *, residual: torch.Tensor | None = None, eps: float = 1e-6,
+              out: Rows | None = None, sum_out: torch.Tensor | None = None, stream=None) -> Normed:
+    """Root-mean-square norm of the rows of x plus the residual, as 8-bit rows
+    (qconv_norm_rows).  ``sum_out``: where x + residual goes; the whole of x or of the
+    residual may be given, new memory otherwise."""
+    _matrix(x, "x", tuple(DTYPES))
+    m, c = x.shape
+    device = x.device
+    _gain(gain, c, device)
+    total = x
+    if residual is not None:
+        _like(residual, x, "residual")
+        total = _on(device, sum_out, (m, c), x.dtype, "sum_out", stream)
+    elif sum_out is not None:
+        raise QConvError(EINVAL, "sum_out without a residual")
+    rows = _rows_out(out, m, c, device, stream)
+    rstd = _empty(m, torch.float32, device, stream)
+    to = _rows_arg(rows, "out", device)
+    add = (None, 0, None, 0) if residual is None else (residual.data_ptr(), _ld(residual), total.data_ptr(), _ld(total))
+    _check(_call(device, _lib().qconv_norm_rows, x.data_ptr(), _ld(x), *add, DTYPES[x.dtype], gain.data_ptr(),
+                 DTYPES[gain.dtype], float(eps), m, c, to.codes, to.pitch, to.scale, rstd.data_ptr(), _stream(stream, device)),
+           "qconv_norm_rows")
+    _hold(stream, x, gain, residual, rows.codes, rows.scale, sum_out)
+    return Normed(rows, total, rstd)
+
+
+def norm_grad_workspace_bytes(rows: int, channels: int) -> int:
+    """Scratch of :func:`norm_rows_grad`."""
+    n = _size(0)
+    _check(_lib().qconv_norm_rows_grad_workspace_bytes(int(rows), int(channels), ctypes.byref(n)),
+           "qconv_norm_rows_grad_workspace_bytes")
+    return n.value
+
+
+def norm_rows_grad(dy: torch.Tensor, h: torch.Tensor, gain: torch.Tensor, rstd: torch.Tensor, *,
+                   dsum: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                   workspace: torch.Tensor | None = None, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
+    """Gradients (of x and the residual alike, of dy's type; of the gain, float32) from
+    the gradient dy of the norm's values and dsum of h, the norm's ``sum``
+    (qconv_norm_rows_grad).  ``out`` may be dsum itself."""
+    _matrix(dy, "dy", tuple(DTYPES))
+    _like(h, dy, "h")
+    m, c = dy.shape
+    device = dy.device
+    _gain(gain, c, device)
+    if rstd.dtype is not torch.float32 or rstd.shape != (m,) or not rstd.is_contiguous() or rstd.device != device:
+        raise QConvError(EINVAL, f"rstd must be one float32 for each row, on {device}")
+    if dsum is not None:
+        _like(dsum, dy, "dsum")
+    dx = _on(device, out, (m, c), dy.dtype, "out", stream)
+    dgain = _empty(c, torch.float32, device, stream)
+    keep, ws, ws_bytes = _workspace(norm_grad_workspace_bytes(m, c), workspace, device, stream)
+    _check(_call(device, _lib().qconv_norm_rows_grad, dy.data_ptr(), _ld(dy), h.data_ptr(), _ld(h),
+                 None if dsum is None else dsum.data_ptr(), 0 if dsum is None else _ld(dsum), DTYPES[dy.dtype],
+                 gain.data_ptr(), DTYPES[gain.dtype], rstd.data_ptr(), m, c, dx.data_ptr(), _ld(dx), dgain.data_ptr(), ws,
+                 ws_bytes, _stream(stream, device)), "qconv_norm_rows_grad")
+    _hold(stream, dy, h, gain, rstd, dsum, out, workspace)
+    return dx, dgain
 
 
 def pack_rows4(codes: torch.Tensor, scale: torch.Tensor, stream=None) -> Rows:
