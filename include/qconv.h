@@ -620,6 +620,64 @@ int qconv_linear_grad_weight(const void *dy, int32_t dtype, int64_t lddy, int32_
                              int64_t lddw, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * 4-bit weights with a scale for each group of channels of each row:
+ *   w[k][c] = scale[k * scale_pitch + c / group] * code[k][c]
+ *   codes, pitch, rows, channels   as of 4-bit qconv_rows
+ *   scale        DEVICE, rows x ceil(channels / group) of scale_dtype (QCONV_BF16, _F16 or
+ *                _F32), scale_pitch elements from row to row (at most 2^17), any values
+ *   group        channels of a scale: a multiple of 32 up to 4096 (more than channels: one
+ *                scale a row; the last group may be short)
+ *
+ * qconv_linear_groups -- qconv_linear by such weights (without adapters).  A group's sum
+ * of codes is a whole number, exact; times its scale, in 32 bits, it is added to the sum
+ * of the groups, and x's scale multiplies that.
+ * qconv_linear_groups_grad_input -- qconv_linear_grad_input by such weights; workspace
+ * as there (qconv_linear_grad_workspace_bytes of m, w->channels, w->rows).
+ * Rules, limits and errors as of qconv_linear and qconv_linear_grad_input.
+ */
+typedef struct qconv_group_rows {
+    const void *codes;
+    const void *scale;
+    int64_t pitch, scale_pitch;
+    int32_t rows, channels;
+    int32_t group, scale_dtype;
+} qconv_group_rows;
+int qconv_linear_groups(const qconv_rows *x, const qconv_group_rows *w, void *y, int32_t dtype, int64_t ldy, void *stream);
+int qconv_linear_groups_grad_input(const void *dy, int32_t dtype, int64_t lddy, int32_t m, const qconv_group_rows *w, void *dx,
+                                   int64_t lddx, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Experts: rows sorted by the expert that they go to, each expert with k x c weights of
+ * its own.  Expert e has rows offsets[e] .. offsets[e + 1] - 1, none of them possibly:
+ *   offsets   DEVICE, experts + 1 int32 that do not fall, from 0 to the number of rows
+ *             (larger or smaller ones are taken as that or 0).  They are read when the
+ *             call runs, so a captured call follows them.  Rows before offsets[0] and
+ *             from offsets[experts] on belong to no expert: what is computed for rows
+ *             leaves theirs as it was.
+ *   experts   1 to 4096
+ *   w         experts * k rows, expert e's from row e * k on
+ * qconv_linear_experts, qconv_linear_experts_groups -- y[i] = w_e x[i] for every row i of
+ *   expert e, as qconv_linear and qconv_linear_groups (y: x->rows x k).
+ * qconv_linear_experts_grad_input, qconv_linear_experts_groups_grad_input --
+ *   dx[i] = dy[i] w_e, as qconv_linear_grad_input, for m rows (dy: m x k, dx: m x w->channels).
+ * qconv_linear_experts_grad_weight -- dw[e * k + j][c] = sum over e's rows i of dy[i][j]
+ *   x[i][c], 32-bit floats (dy: x->rows x k; dw: experts * k x x->channels, all of it
+ *   written: zeros for an expert without rows).
+ * One launch each, no workspace.  Rules, limits and errors as of those without experts; a
+ * result of more than 2^22 tiles of 64 x 64, one more counted for each expert, is refused.
+ */
+int qconv_linear_experts(const qconv_rows *x, const qconv_rows *w, const int32_t *offsets, int32_t experts, void *y,
+                         int32_t dtype, int64_t ldy, void *stream);
+int qconv_linear_experts_groups(const qconv_rows *x, const qconv_group_rows *w, const int32_t *offsets, int32_t experts,
+                                void *y, int32_t dtype, int64_t ldy, void *stream);
+int qconv_linear_experts_grad_input(const void *dy, int32_t dtype, int64_t lddy, int32_t m, const qconv_rows *w,
+                                    const int32_t *offsets, int32_t experts, void *dx, int64_t lddx, void *stream);
+int qconv_linear_experts_groups_grad_input(const void *dy, int32_t dtype, int64_t lddy, int32_t m, const qconv_group_rows *w,
+                                           const int32_t *offsets, int32_t experts, void *dx, int64_t lddx, void *stream);
+int qconv_linear_experts_grad_weight(const void *dy, int32_t dtype, int64_t lddy, int32_t k, const qconv_rows *x,
+                                     const int32_t *offsets, int32_t experts, float *dw, int64_t lddw, void *stream);
+
+/*
  * Around the linear layer: the norm that makes its 8-bit rows.
  *
  * qconv_norm_rows -- root-mean-square norm with the residual's addition, to 8-bit rows:

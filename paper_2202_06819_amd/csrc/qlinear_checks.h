@@ -89,4 +89,10 @@ inline int check_tiles(int64_t rows, int64_t cols) {
     return QCONV_OK;
 }
 
+// Partial sums of a gradient whose sum is split.
+inline size_t grad_workspace(int64_t ni, int64_t nj, int64_t nt) {
+    const int splits = plan_grad(ni, nj, nt).splits;
+    return splits > 1 ? (size_t)splits * (size_t)ni * (size_t)((nj + 3) / 4 * 4) * 4 : 0;
+}
+
 }  // namespace qconv

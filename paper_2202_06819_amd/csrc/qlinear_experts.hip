@@ -1,0 +1,70 @@
+// Products of rows sorted by expert with each expert's weights: the projection's kernels
+// (qlinear_fwd.h), each workgroup on the rows and weights of one expert.
+#include <algorithm>
+
+#include "qlinear_experts.h"
+#include "qlinear_fwd.h"
+#include "qlinear_plan.h"
+
+namespace qconv {
+
+namespace {
+
+template <class T, int WB, int FJ, int FI>
+__global__ void __launch_bounds__(512) experts_rows(LinearArgs a, ExpertArg ex) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    if ((int)blockIdx.y >= expert_tiles<16 * FI>(ex)) return;
+    const ExpertRows p = expert_tile<16 * FI>(ex, (int)blockIdx.y);
+    few_product<T, WB, FJ, FI, false>(of_expert(a, p), (int)blockIdx.x, p.tile, smem);
+}
+template <class T, int WB, int TJ, int TI, int WJ, int WI, int KS>
+__global__ void __launch_bounds__(KS *WJ *WI * 64, TJ == 64 ? 4 : 2) experts_tiles(LinearArgs a, ExpertArg ex) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    ExpertRows p;
+    int tj;
+    if (!expert_place<TI>(ex, a.tiles_j, p, tj)) return;
+    tile_product<T, WB, TJ, TI, WJ, WI, KS, false>(of_expert(a, p), tj, p.tile, smem);
+}
+
+template <auto Kernel, int LDS>
+hipError_t start(const LinearArgs &a, const ExpertArg &ex, dim3 grid, int threads, hipStream_t stream) {
+    const hipError_t e = allow_lds(reinterpret_cast<const void *>(Kernel), LDS);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(Kernel, grid, dim3((unsigned)threads), LDS, stream, a, ex);
+    return hipGetLastError();
+}
+template <class T, int WB, int FJ, int FI>
+hipError_t few(const LinearArgs &a, const ExpertArg &ex, hipStream_t stream) {
+    const dim3 grid((unsigned)((a.k + 16 * FJ - 1) / (16 * FJ)), (unsigned)most_tiles(a.m, ex.count, 16 * FI));
+    return start<experts_rows<T, WB, FJ, FI>, few_lds(FJ, FI, false)>(a, ex, grid, 512, stream);
+}
+template <class T, int WB, int SIZE, int WJ, int WI, int KS>
+hipError_t tile(LinearArgs a, const ExpertArg &ex, hipStream_t stream) {
+    a.tiles_j = (a.k + SIZE - 1) / SIZE;
+    const dim3 grid((unsigned)most_tiles(a.m, ex.count, SIZE) * (unsigned)a.tiles_j);
+    return start<experts_tiles<T, WB, SIZE, SIZE, WJ, WI, KS>, tile_lds<T, SIZE, SIZE, WJ * WI * 64, KS, false>()>(
+        a, ex, grid, KS * WJ * WI * 64, stream);
+}
+
+template <class T, int WB>
+hipError_t product(const LinearArgs &a, const ExpertArg &ex, hipStream_t stream) {
+    switch (plan_linear(a, WB, [&](int size) { return expected_tiles(a.m, ex.count, size); })) {
+        case Kind::FEW_1x1: return few<T, WB, 1, 1>(a, ex, stream);
+        case Kind::FEW_2x1: return few<T, WB, 2, 1>(a, ex, stream);
+        case Kind::FEW_2x2: return few<T, WB, 2, 2>(a, ex, stream);
+        case Kind::TILE_64x4: return tile<T, WB, 64, 1, 4, 4>(a, ex, stream);
+        case Kind::TILE_64x2: return tile<T, WB, 64, 1, 4, 2>(a, ex, stream);
+        case Kind::TILE_128: return tile<T, WB, 128, 2, 2, 1>(a, ex, stream);
+        case Kind::TILE_256: return tile<T, WB, 256, 4, 2, 1>(a, ex, stream);
+        default: return tile<T, WB, 64, 1, 4, 1>(a, ex, stream);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_experts(const LinearArgs &a, const ExpertArg &ex, int w_bits, int dtype, hipStream_t stream) {
+    if (dtype == QCONV_BF16) return w_bits == 4 ? product<BF16, 4>(a, ex, stream) : product<BF16, 8>(a, ex, stream);
+    return w_bits == 4 ? product<F16, 4>(a, ex, stream) : product<F16, 8>(a, ex, stream);
+}
+
+}  // namespace qconv

@@ -308,15 +308,14 @@ __device__ __forceinline__ void add_adapters(const LinearArgs &a, int id, int ro
 // bits: 4.4 us without adapters (8.4 MB, 1.9 TB/s).
 constexpr int few_lds(int fj, int fi, bool ad) { return 8 * 64 * 16 * (fj * fi + (ad ? fj : 0)); }
 template <class T, int WB, int FJ, int FI, bool AD>
-__global__ void __launch_bounds__(512) linear_few(LinearArgs a) {
+__device__ __forceinline__ void few_product(const LinearArgs &a, int tile_j, int tile_i, uint8_t *smem) {
     constexpr int kWaves = 8, kParts = kWaves / FI;
     constexpr int kWide = WB == 8 ? 2 : 1;   // 16-byte vectors of weights a lane and step
-    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     auto part = reinterpret_cast<i32x4(*)[FJ * FI][64]>(smem);                                // waves' sums
     auto extra = reinterpret_cast<f32x4(*)[FJ][64]>(smem + kWaves * FJ * FI * 64 * 16);   // the adapters' part
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int r = lane & 15, g = lane >> 4;
-    const int ch0 = (int)blockIdx.x * 16 * FJ, row0 = (int)blockIdx.y * 16 * FI;
+    const int ch0 = tile_j * 16 * FJ, row0 = tile_i * 16 * FI;
     const __amdgpu_buffer_rsrc_t rx = range_of(a.x.codes + (int64_t)row0 * a.x.pitch,
                                                (int64_t)(a.m - 1 - row0) * a.x.pitch + a.x.used);
     const __amdgpu_buffer_rsrc_t rw = range_of(a.w.codes + (int64_t)ch0 * a.w.pitch,
@@ -425,6 +424,11 @@ __global__ void __launch_bounds__(512) linear_few(LinearArgs a) {
             for (int p = 0; p < kParts; ++p) y += extra[p * FI + f][j][lane];
         store4<T>(static_cast<typename T::elem *>(a.y) + (int64_t)row * a.ldy + ch, y, a.k - ch);
     }
+}
+template <class T, int WB, int FJ, int FI, bool AD>
+__global__ void __launch_bounds__(512) linear_few(LinearArgs a) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    few_product<T, WB, FJ, FI, AD>(a, (int)blockIdx.x, (int)blockIdx.y, smem);
 }
 
 // --------------------------------------------------------------- many rows
@@ -603,15 +607,12 @@ constexpr int tile_lds() {
 // cores, which its random operands hold to what power allows: 8192 x 4096 x 4096 takes
 // 118 to 124 us, 2.2 to 2.3 POP/s of the 3.1 that products of registers alone reach.
 template <class T, int WB, int TJ, int TI, int WJ, int WI, int KS, bool AD>
-__global__ void __launch_bounds__(KS *WJ *WI * 64, TJ == 64 ? 4 : 2) linear_tile(LinearArgs a) {
+__device__ __forceinline__ void tile_product(const LinearArgs &a, int tj, int ti, uint8_t *smem) {
     constexpr int FJ = 4, FI = TI / (16 * WI), kThreads = WJ * WI * 64, kBuffer = (TJ + TI) * kStepBytes;
     static_assert(TJ == WJ * 64);
     static_assert(KS == 1 || FI == 1);
-    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     const int group = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kThreads), thread = (int)threadIdx.x % kThreads;
     const int wave = __builtin_amdgcn_readfirstlane(thread >> 6), lane = threadIdx.x & 63;
-    int ti, tj;
-    tile_at(xcd_run((int)blockIdx.x, a.tiles_i * a.tiles_j), a.tiles_i, a.tiles_j, ti, tj);
     const int i0 = ti * TI, j0 = tj * TJ;
     const u32x4_t rx = range_words(a.x.codes + (int64_t)i0 * a.x.pitch, (int64_t)(a.m - 1 - i0) * a.x.pitch + a.x.used);
     const uint8_t *wbase = a.w.codes + (int64_t)j0 * a.w.pitch;
@@ -742,6 +743,13 @@ __global__ void __launch_bounds__(KS *WJ *WI * 64, TJ == 64 ? 4 : 2) linear_tile
             }
         }
     }
+}
+template <class T, int WB, int TJ, int TI, int WJ, int WI, int KS, bool AD>
+__global__ void __launch_bounds__(KS *WJ *WI * 64, TJ == 64 ? 4 : 2) linear_tile(LinearArgs a) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    int ti, tj;
+    tile_at(xcd_run((int)blockIdx.x, a.tiles_i * a.tiles_j), a.tiles_i, a.tiles_j, ti, tj);
+    tile_product<T, WB, TJ, TI, WJ, WI, KS, AD>(a, tj, ti, smem);
 }
 
 }  // namespace qconv

@@ -2,6 +2,7 @@
 #include <algorithm>
 
 #include "qlinear_fwd.h"
+#include "qlinear_plan.h"
 
 namespace qconv {
 
@@ -30,66 +31,9 @@ hipError_t tile(LinearArgs a, hipStream_t stream) {
                                                                       THREADS, stream);
 }
 
-// The kernels, and a model of their times (us), its constants measured.  A workgroup
-// of the few-row kernel takes `start` and `step` for each 1024 channels in its turn on
-// a CU; a tile takes `steps[n]` for a step of 128 channels (of each of its groups of
-// waves) with n + 1 on a CU, where `resident` fit.  E.g. 4-bit weights of 2048 channels,
-// 4096 outputs: 16 rows 3.6 (16 channels and rows a workgroup; a tile of 64 with two
-// groups 7.1); 64 rows 5.3 (32 x 32; tile 7.3); 160 rows 7.6 (tile of 64, two groups; with
-// one 9.6, four 8.1, few-row kernel 11.8); 2048 rows 24 (tile of 128; of 64 33, of 256 38).
-// Of 8192 channels, 256 rows: 19.5 (tile of 64, four groups; two 21.6, one 32, tile of
-// 128 48).  8-bit, 4096 x 4096, 8192 rows: 119 (tile of 256).
-enum class Kind { FEW_1x1, FEW_2x1, FEW_2x2, FEW_2x4, TILE_64x4, TILE_64x2, TILE_64, TILE_128, TILE_256 };
-
-Kind plan_linear(const LinearArgs &a, int w_bits) {
-    static const struct {
-        Kind kind;
-        int channels, rows;
-        double start, step, adapters;
-    } kFew[] = {{Kind::FEW_1x1, 16, 16, 0.9, 0.55, 2.5}, {Kind::FEW_2x1, 32, 16, 0.85, 0.8, 3.0},
-                {Kind::FEW_2x2, 32, 32, 1.4, 1.15, 4.0}, {Kind::FEW_2x4, 32, 64, 3.2, 1.95, 6.0}};
-    static const struct {
-        Kind kind;
-        int size, groups, resident;
-        double start, steps8[4], steps4[4], adapters;
-    } kTiles[] = {{Kind::TILE_64x4, 64, 4, 1, 4.2, {0.85}, {0.95}, 2.0},
-                  {Kind::TILE_64x2, 64, 2, 2, 3.4, {0.5, 0.82}, {0.53, 0.89}, 2.0},
-                  {Kind::TILE_64, 64, 1, 4, 2.9, {0.38, 0.5, 0.68, 0.82}, {0.44, 0.58, 0.72, 0.88}, 2.0},
-                  {Kind::TILE_128, 128, 1, 2, 4.2, {0.7, 1.1}, {0.74, 1.17}, 4.0},
-                  {Kind::TILE_256, 256, 1, 1, 6.0, {1.7}, {2.2}, 6.0}};
-    const auto on_cu = [&](int64_t channels, int64_t rows) {
-        return (((a.k + channels - 1) / channels) * ((a.m + rows - 1) / rows) + 255) / 256;
-    };
-    Kind best = Kind::TILE_64;
-    double best_us = 0;
-    const auto consider = [&](Kind kind, double us) {
-        if (best_us == 0 || us < best_us) best = kind, best_us = us;
-    };
-    for (const auto &f : kFew) {
-        // (without adapters tiles of 64 are as fast wherever 64 rows a workgroup could be
-        // chosen: never with 8-bit weights, within 1 % with 4-bit ones of 5700 channels)
-        if (f.kind == Kind::FEW_2x4 && !a.ad.count) continue;
-        consider(f.kind, 1.5 + on_cu(f.channels, f.rows) * (f.start + f.step * (w_bits == 8 ? 1.2 : 1.0) * a.c / 1024.0 +
-                                                            (a.ad.count ? f.adapters : 0.0)));
-    }
-    for (const auto &t : kTiles) {
-        const int64_t n = on_cu(t.size, t.size), rest = n % t.resident;
-        const double *steps = w_bits == 8 ? t.steps8 : t.steps4;
-        const double step = (n / t.resident) * steps[t.resident - 1] + (rest ? steps[rest - 1] : 0.0);
-        const int64_t turns = (n + t.resident - 1) / t.resident;
-        // each adapter that a tile's rows name is a step of one of its groups: few rows are
-        // taken to name any, many to lie in runs of one
-        const int64_t most = std::min<int64_t>(a.ad.count, a.m < t.size ? a.m : t.size);
-        const int64_t named = a.m <= 256 ? most : std::min(most, (int64_t)a.ad.count * t.size / a.m + 1);
-        const double adapters = a.ad.count ? t.adapters + 1.2 * (double)((named + t.groups - 1) / t.groups) : 0.0;
-        consider(t.kind, t.start + (a.steps + t.groups - 1) / t.groups * step + turns * adapters);
-    }
-    return best;
-}
-
 template <class T, int WB, bool AD>
 hipError_t product(const LinearArgs &a, hipStream_t stream) {
-    switch (plan_linear(a, WB)) {
+    switch (plan_linear(a, WB, [&](int rows) { return (a.m + rows - 1) / rows; })) {
         case Kind::FEW_1x1: return few<T, WB, 1, 1, AD>(a, stream);
         case Kind::FEW_2x1: return few<T, WB, 2, 1, AD>(a, stream);
         case Kind::FEW_2x2: return few<T, WB, 2, 2, AD>(a, stream);

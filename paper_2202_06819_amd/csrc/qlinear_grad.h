@@ -16,25 +16,31 @@
 #pragma once
 
 #include "qlinear_device.h"
+#include "qlinear_scales.h"
 
 namespace qconv {
+
+// LDS of a step's scales: one for each t, or for each t and 32 columns.
+constexpr int grad_scale_bytes(int scale_bytes, int tile) { return scale_bytes ? tile / 32 * 256 : 256; }
+constexpr int kGradStages = 3;
+// Of a group of waves: its steps' codes, p and scales.
+constexpr int grad_lds(int tile, int scale_bytes = 0) {
+    return kGradStages * (tile * 64 + tile * 128 + grad_scale_bytes(scale_bytes, tile));
+}
 
 // A power of two that brings the largest finite |scale| of a range to at most 65504 /
 // 128, the largest f16 by the largest code, and above half of that: a code of -128 stays
 // finite, and f16 products of code and scale are normal numbers for scales down to 2^-21
 // of the largest (bf16 has float's range and needs none).  Each group of THREADS threads
 // finds it for itself, in LDS of its own.
-template <class T, int THREADS>
-__device__ __forceinline__ void scale_window(const float *scale, int begin, int end, uint32_t *lds, float &to,
+template <class T, int THREADS, class Scales>
+__device__ __forceinline__ void scale_window(Scales largest, int begin, int end, uint32_t *lds, float &to,
                                              float &from) {
     if constexpr (sizeof(typename T::elem) != 2 || __is_same(T, BF16)) {
         to = from = 1.0f;
     } else {
         uint32_t m = 0;
-        for (int t = begin + (int)threadIdx.x % THREADS; t < end; t += THREADS) {
-            const uint32_t b = __builtin_bit_cast(uint32_t, scale[t]) & 0x7fffffffu;
-            if (b < 0x7f800000u) m = max(m, b);
-        }
+        for (int t = begin + (int)threadIdx.x % THREADS; t < end; t += THREADS) m = max(m, largest(t));
 #pragma unroll
         for (int d = 32; d; d >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d));
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x % THREADS >> 6] = m;
@@ -100,24 +106,23 @@ __device__ __forceinline__ uint32_t scaled_pair(uint32_t w, int half, float s0, 
 // KS groups of waves deal a tile's steps out among them, each with buffers of its own,
 // and their sums meet in LDS: with few tiles a CU's waves then still hide each other's
 // waits, without partial sums in memory.
-constexpr int kGradStages = 3;
-template <class T, int WB, bool TRANSPOSED, bool COPY, int TJ, int TI, int WJ, int WI, int KS>
-__global__ void __launch_bounds__(KS *WJ *WI * 64) grad_tile(GradArgs a) {
+// GS: 0, or the bytes of a scale of a group of channels (4-bit codes); a wave's columns
+// lie within 32 channels, so it reads one scale for each t as it does without groups.
+template <class T, int WB, bool TRANSPOSED, bool COPY, int GS, int TJ, int TI, int WJ, int WI, int KS>
+__device__ __forceinline__ void grad_product(const GradArgs &a, const GroupArg &groups, int split, int ti, int tj,
+                                             uint8_t *all_smem) {
     constexpr int FJ = TJ / (16 * WJ), FI = TI / (16 * WI), kThreads = WJ * WI * 64, kWaves = kThreads / 64;
-    constexpr int kCodes = 64 * TJ, kP = TI * 128, kStage = kCodes + kP + 256;
+    constexpr int kCodes = 64 * TJ, kP = TI * 128, kStage = kCodes + kP + grad_scale_bytes(GS, TJ);
     constexpr int kCodeCopies = WB == 8 ? kCodes / (1024 * kWaves) : 0, kPCopies = COPY ? kP / (1024 * kWaves) : 0;
     constexpr int kCodeUnits = WB == 4 ? kCodes / (16 * kThreads) : 0, kPUnits = COPY ? 0 : kP / (16 * kThreads);
-    constexpr int kCopies = kCodeCopies + kPCopies + 1;   // a wave's copies of a step
+    constexpr int kCopies = kCodeCopies + kPCopies + (GS ? 0 : 1);   // a wave's copies of a step
+    constexpr int kSlots = TJ / 32, kScaleUnits = GS ? (64 * kSlots + kThreads - 1) / kThreads : 0;
+    static_assert(!GS || (WB == 4 && !TRANSPOSED && FJ == 2));
     using elem = typename T::elem;
     using v8 = typename T::v8;
-    extern __shared__ __attribute__((aligned(16))) uint8_t all_smem[];
     const int group = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kThreads);
     uint8_t *const smem = all_smem + group * (kGradStages * kStage);
     const int tid = (int)threadIdx.x % kThreads, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-    const int tiles = a.tiles_i * a.tiles_j;
-    const int split = (int)blockIdx.x / tiles;
-    int ti, tj;
-    tile_at(xcd_run((int)blockIdx.x - split * tiles, tiles), a.tiles_i, a.tiles_j, ti, tj);
     const int i0 = ti * TI, j0 = tj * TJ;
     // the split's steps, dealt to the groups in runs; past them every operand is zero
     const int begin = split * a.steps_per_split, end = min(begin + a.steps_per_split, a.steps);
@@ -173,7 +178,7 @@ __global__ void __launch_bounds__(KS *WJ *WI * 64) grad_tile(GradArgs a) {
                 off = col < (a.ni - i0) * 2 ? (uint32_t)t * (uint32_t)a.ldp * 2u + (uint32_t)col : kNowhere;
             }
             copy16(buf + kCodes + at0, off, q.p);
-        } else {
+        } else if (n < kCopies) {
             copy4(buf + kCodes + kP, (uint32_t)lane * 4u, q.scale);
         }
     };
@@ -181,11 +186,17 @@ __global__ void __launch_bounds__(KS *WJ *WI * 64) grad_tile(GradArgs a) {
     // What goes through registers: units of 16 bytes of LDS, each from one load (p's of
     // any alignment).  A unit past the matrix is loaded from within it and put right
     // when it is stored, so that the loads of a step are always as many.
-    constexpr int kFetches = kCodeUnits + kPUnits, kStages = kGradStages;
+    constexpr int kFetches = kCodeUnits + kPUnits + kScaleUnits, kStages = kGradStages;
     constexpr int kFlight = TJ < 256 && kFetches > 0 ? 2 : 1;   // steps whose loads are on their way
     struct Units {
         uint2 code[kCodeUnits ? kCodeUnits : 1];
         u32x4_t p[kPUnits ? kPUnits : 1];
+        uint32_t scale[kScaleUnits ? kScaleUnits : 1];
+    };
+    // The scale of row t for the columns of slot `slot` (32 each) of the tile.
+    const auto group_scale = [&](int t, int slot) {
+        const int64_t at = (int64_t)t * groups.pitch + group_of(groups, min(j0 / 32 + slot, (a.nj - 1) / 32));
+        return load_scale<GS ? GS : 4>(groups, at);
     };
     const int p_rows = TRANSPOSED ? t_end : a.ni, p_count = TRANSPOSED ? a.ni : t_end;   // p as it lies in memory
     const bool narrow = !COPY && p_count < 8;   // rows shorter than a load: by elements
@@ -201,6 +212,13 @@ __global__ void __launch_bounds__(KS *WJ *WI * 64) grad_tile(GradArgs a) {
                 const int unit = n * kThreads + tid, t = min(s * 64 + unit / (TJ / 16), a.nt - 1);
                 const int at = min((j0 + unit % (TJ / 16) * 16) / 2, a.b.used - 8);
                 q.code[n] = *reinterpret_cast<const uint2 *>(a.b.codes + (int64_t)t * a.b.pitch + at);
+            }
+        }
+        if constexpr (GS > 0) {   // (where there are more threads than scales, some load one again)
+#pragma unroll
+            for (int n = 0; n < kScaleUnits; ++n) {
+                const int unit = n * kThreads + tid;
+                q.scale[n] = group_scale(min(s * 64 + (unit & 63), a.nt - 1), unit / 64 % kSlots);
             }
         }
         if constexpr (!COPY) {
@@ -230,6 +248,14 @@ __global__ void __launch_bounds__(KS *WJ *WI * 64) grad_tile(GradArgs a) {
                 const bool in = s * 64 + t < t_end && j0 + u * 16 < a.b.used * 2;
                 const uint2 lo = widen8(in ? q.code[n].x : 0u), hi = widen8(in ? q.code[n].y : 0u);
                 *reinterpret_cast<uint4 *>(buf + t * TJ + ((u ^ code_unit_of<TJ>(t)) << 4)) = uint4{lo.x, lo.y, hi.x, hi.y};
+            }
+        }
+        if constexpr (GS > 0) {
+#pragma unroll
+            for (int n = 0; n < kScaleUnits; ++n) {
+                const int unit = n * kThreads + tid, t = unit & 63;
+                *reinterpret_cast<float *>(buf + kCodes + kP + unit / 64 % kSlots * 256 + t * 4) =
+                    s * 64 + t < t_end ? scale_value<GS ? GS : 4>(groups, q.scale[n]) : 0.0f;
             }
         }
         if constexpr (!COPY) {
@@ -283,7 +309,7 @@ __global__ void __launch_bounds__(KS *WJ *WI * 64) grad_tile(GradArgs a) {
     };
     auto read_codes = [&](const uint8_t *buf, int ks) {
         Codes c;
-        const float *sc = reinterpret_cast<const float *>(buf + kCodes + kP) + ks * 32 + g * 8;
+        const float *sc = reinterpret_cast<const float *>(buf + kCodes + kP + (GS ? (jrow0 >> 5) * 256 : 0)) + ks * 32 + g * 8;
         c.scale[0] = *reinterpret_cast<const f32x4 *>(sc);
         c.scale[1] = *reinterpret_cast<const f32x4 *>(sc + 4);
         const int t = ks * 32 + g * 8 + (r >> 1);
@@ -342,8 +368,18 @@ __global__ void __launch_bounds__(KS *WJ *WI * 64) grad_tile(GradArgs a) {
 #pragma unroll
         for (int m = 0; m < kStages - 1; ++m) fetch(s0 + m, units[m]);
     // (found while those are on their way; the last buffer is free until the first step)
-    scale_window<T, kThreads>(a.b.scale, begin * 64, t_end,
-                              reinterpret_cast<uint32_t *>(smem + (kStages - 1) * kStage), to, from);
+    const auto largest = [&](int t) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int n = 0; n < (GS ? kSlots : 1); ++n) {
+            const float v = GS ? scale_value<GS ? GS : 4>(groups, group_scale(t, n)) : a.b.scale[t];
+            const uint32_t b = __builtin_bit_cast(uint32_t, v) & 0x7fffffffu;
+            if (b < 0x7f800000u) m = max(m, b);
+        }
+        return m;
+    };
+    scale_window<T, kThreads>(largest, begin * 64, t_end, reinterpret_cast<uint32_t *>(smem + (kStages - 1) * kStage), to,
+                              from);
     if constexpr (WB == 4) to *= 0.0625f;
     if constexpr (kFetches > 0) {
 #pragma unroll
@@ -437,6 +473,25 @@ __global__ void __launch_bounds__(KS *WJ *WI * 64) grad_tile(GradArgs a) {
             }
         }
     }
+}
+
+// Tile and split of a workgroup of tiles_i * tiles_j * splits.
+struct GradPlace {
+    int split, ti, tj;
+};
+__device__ __forceinline__ GradPlace grad_place(const GradArgs &a) {
+    const int tiles = a.tiles_i * a.tiles_j;
+    GradPlace p;
+    p.split = (int)blockIdx.x / tiles;
+    tile_at(xcd_run((int)blockIdx.x - p.split * tiles, tiles), a.tiles_i, a.tiles_j, p.ti, p.tj);
+    return p;
+}
+
+template <class T, int WB, bool TRANSPOSED, bool COPY, int TJ, int TI, int WJ, int WI, int KS>
+__global__ void __launch_bounds__(KS *WJ *WI * 64) grad_tile(GradArgs a) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t all_smem[];
+    const GradPlace p = grad_place(a);
+    grad_product<T, WB, TRANSPOSED, COPY, 0, TJ, TI, WJ, WI, KS>(a, GroupArg{}, p.split, p.ti, p.tj, all_smem);
 }
 
 // Adds the partial sums in the order of the splits and rounds once: four columns a

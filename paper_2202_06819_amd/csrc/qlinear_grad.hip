@@ -2,6 +2,7 @@
 #include <algorithm>
 
 #include "qlinear_grad.h"
+#include "qlinear_plan.h"
 
 namespace qconv {
 
@@ -15,20 +16,18 @@ hipError_t tile(const GradArgs &a, hipStream_t stream) {
     return hipGetLastError();
 }
 
-// Steps in LDS: codes, p, scales.
-constexpr int lds_bytes(int size) { return kGradStages * (size * 64 + size * 128 + 256); }
 template <class T, int WB, bool TRANSPOSED, bool COPY>
 hipError_t product(const GradArgs &a, const GradPlan &plan, hipStream_t stream) {
     const int size = plan.tile, groups = plan.groups;
-    if (size == 256) return tile<grad_tile<T, WB, TRANSPOSED, COPY, 256, 256, 8, 1, 1>, lds_bytes(256), 512>(a, stream);
-    if (size == 128) return tile<grad_tile<T, WB, TRANSPOSED, COPY, 128, 128, 4, 1, 1>, lds_bytes(128), 256>(a, stream);
+    if (size == 256) return tile<grad_tile<T, WB, TRANSPOSED, COPY, 256, 256, 8, 1, 1>, grad_lds(256), 512>(a, stream);
+    if (size == 128) return tile<grad_tile<T, WB, TRANSPOSED, COPY, 128, 128, 4, 1, 1>, grad_lds(128), 256>(a, stream);
     // (waves of 16 x 64 convert no code twice, waves of 32 x 32 read p from LDS less often:
     // a step takes 0.46 against 0.52 us transposed, 0.56 against 0.52 in rows)
     constexpr int WJ = TRANSPOSED ? 4 : 2, WI = TRANSPOSED ? 1 : 2;
     if (groups == 4)
-        return tile<grad_tile<T, WB, TRANSPOSED, COPY, 64, 64, WJ, WI, 4>, 4 * lds_bytes(64), 1024>(a, stream);
-    if (groups == 2) return tile<grad_tile<T, WB, TRANSPOSED, COPY, 64, 64, WJ, WI, 2>, 2 * lds_bytes(64), 512>(a, stream);
-    return tile<grad_tile<T, WB, TRANSPOSED, COPY, 64, 64, WJ, WI, 1>, lds_bytes(64), 256>(a, stream);
+        return tile<grad_tile<T, WB, TRANSPOSED, COPY, 64, 64, WJ, WI, 4>, 4 * grad_lds(64), 1024>(a, stream);
+    if (groups == 2) return tile<grad_tile<T, WB, TRANSPOSED, COPY, 64, 64, WJ, WI, 2>, 2 * grad_lds(64), 512>(a, stream);
+    return tile<grad_tile<T, WB, TRANSPOSED, COPY, 64, 64, WJ, WI, 1>, grad_lds(64), 256>(a, stream);
 }
 
 template <class Out>
@@ -56,10 +55,15 @@ hipError_t grad(GradArgs a, bool transposed, int w_bits, hipStream_t stream) {
     else
         e = copies ? product<T, 4, false, true>(a, plan, stream) : product<T, 4, false, false>(a, plan, stream);
     if (e != hipSuccess || a.splits == 1) return e;
-    return transposed ? sum<float>(a, stream) : sum<typename T::elem>(a, stream);
+    return launch_grad_sum(a, transposed, __is_same(T, BF16) ? QCONV_BF16 : QCONV_F16, stream);
 }
 
 }  // namespace
+
+hipError_t launch_grad_sum(const GradArgs &a, bool to_float, int dtype, hipStream_t stream) {
+    if (to_float) return sum<float>(a, stream);
+    return dtype == QCONV_BF16 ? sum<BF16::elem>(a, stream) : sum<F16::elem>(a, stream);
+}
 
 // The tile, its groups of waves and the split that a model of the kernels' times (us)
 // finds fastest.  The constants are measured: a step of 64 of the summed axis takes 1.35
@@ -73,24 +77,15 @@ hipError_t grad(GradArgs a, bool transposed, int w_bits, hipStream_t stream) {
 // split 4 ways, 28.4 in 256 split 8 ways; from 1024: 8.3 with two groups, 9.2 with four,
 // 10.6 with one, 18.6 in 128.  512 x 1024 from 4096: 17.2 with four groups split 2 ways.
 GradPlan plan_grad(int64_t ni, int64_t nj, int64_t nt) {
-    static const struct {
-        int tile, groups, resident;
-        double start, step[4];   // step[n]: n + 1 workgroups on a CU
-    } kKinds[] = {{256, 1, 1, 10, {1.35}}, {128, 1, 2, 6, {0.83, 1.25}}, {64, 1, 4, 3.7, {0.5, 0.75, 0.95, 1.1}},
-                  {64, 2, 2, 4.3, {0.57, 1.08}}, {64, 4, 1, 5, {1.0}}};
     GradPlan best{64, 1, 1, 0, (int)((nt + 63) / 64)};
     double best_us = 0;
     const int64_t steps = best.steps;
-    for (const auto &k : kKinds) {
+    for (const auto &k : kGradKinds) {
         const int64_t tiles = ((ni + k.tile - 1) / k.tile) * ((nj + k.tile - 1) / k.tile);
         for (int64_t want = 1; want <= 32; want *= 2) {
             const int64_t per = (steps + want - 1) / want, splits = per ? (steps + per - 1) / per : 1;
             if (want > 1 && (splits < want || splits * tiles > 4096)) break;
-            const int64_t on_cu = (splits * tiles + 255) / 256;
-            const int64_t rest = on_cu % k.resident;
-            const double step = (on_cu / k.resident) * k.step[k.resident - 1] + (rest ? k.step[rest - 1] : 0.0);
-            const int64_t turns = std::max<int64_t>((on_cu + k.resident - 1) / k.resident, 1);
-            double us = turns * k.start + (per + k.groups - 1) / k.groups * step;
+            double us = grad_time(k, splits * tiles, per);
             if (splits > 1) us += 4 + 0.1 * splits + 8e-6 * splits * ni * nj / 5.0;
             if (best_us == 0 || us < best_us) {
                 best_us = us;

@@ -27,11 +27,6 @@ size_t adapter_workspace(int64_t m, int64_t c, const qconv_adapters *ad) {
     return (size_t)linear_adapter_splits(m, c) * (size_t)m * (size_t)ad->rank * 4;
 }
 
-size_t grad_workspace(int64_t ni, int64_t nj, int64_t nt) {
-    const int splits = plan_grad(ni, nj, nt).splits;
-    return splits > 1 ? (size_t)splits * (size_t)ni * (size_t)((nj + 3) / 4 * 4) * 4 : 0;
-}
-
 int run_grad(GradArgs &a, bool transposed, int w_bits, int dtype, int64_t out_size, const qconv_rows *b, void *workspace,
              size_t workspace_bytes, void *stream) {
     int rc = check_tiles(a.ni, a.nj);

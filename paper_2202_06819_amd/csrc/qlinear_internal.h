@@ -19,6 +19,22 @@ struct RowsArg {
     int32_t rows;
 };
 
+// Scales of groups of channels, in place of one for each row.
+struct GroupArg {
+    const void *scale;   // rows x groups, 16-bit or 32-bit floats
+    int64_t pitch;       // elements from row to row
+    uint32_t per32;      // n * per32 >> 20 is the group of the row's n-th 32 channels
+    int32_t bf16;        // of 16-bit scales: bfloat16, else float16
+};
+
+// Rows sorted by expert: expert e has rows offsets[e] .. offsets[e + 1] - 1, and its
+// weights come after those of expert e - 1.
+struct ExpertArg {
+    const int32_t *offsets;
+    int32_t count;
+    int32_t rows;        // of all experts: offsets are held within it
+};
+
 struct QuantizeArgs {
     const void *x;
     int64_t ldx;         // elements from row to row
@@ -92,6 +108,18 @@ hipError_t launch_norm_grad(const NormGradArgs &a, int dtype, hipStream_t stream
 int norm_grad_parts(int64_t m);   // workgroups of the norm's gradient: rows of its workspace
 hipError_t launch_linear(const LinearArgs &a, int w_bits, int dtype, hipStream_t stream);
 hipError_t launch_grad(const GradArgs &a, bool transposed, int w_bits, int dtype, hipStream_t stream);
+// Adds the partial sums of a.splits (to 32-bit floats, or to dtype).
+hipError_t launch_grad_sum(const GradArgs &a, bool to_float, int dtype, hipStream_t stream);
+// The same with scales of groups (of scale_bytes each; 4-bit weights), and the products of experts
+// (scale_bytes 0: one scale a row).
+hipError_t launch_groups(const LinearArgs &a, const GroupArg &g, int scale_bytes, int group, int dtype, hipStream_t stream);
+hipError_t launch_group_grad(const GradArgs &a, const GroupArg &g, int scale_bytes, int dtype, hipStream_t stream);
+hipError_t launch_experts(const LinearArgs &a, const ExpertArg &ex, int w_bits, int dtype, hipStream_t stream);
+hipError_t launch_expert_groups(const LinearArgs &a, const GroupArg &g, const ExpertArg &ex, int scale_bytes, int group,
+                                int dtype, hipStream_t stream);
+hipError_t launch_expert_grad_input(const GradArgs &a, const GroupArg &g, const ExpertArg &ex, int w_bits, int scale_bytes,
+                                    int dtype, hipStream_t stream);
+hipError_t launch_expert_grad_weight(const GradArgs &a, const ExpertArg &ex, int dtype, hipStream_t stream);
 
 // Workgroup tiles (square), and how a product is cut: shared by the workspace
 // sizes and the launches.

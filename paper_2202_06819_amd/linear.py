@@ -32,7 +32,7 @@ from typing import NamedTuple
 import torch
 
 from . import qconv
-from .qconv import EINVAL, QConvError, _check
+from .qconv import EINVAL, EUNSUPPORTED, QConvError, _check
 
 DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
@@ -51,6 +51,19 @@ class Rows(NamedTuple):
     bits: int = 8
 
 
+class GroupRows(NamedTuple):
+    """4-bit rows with a scale for each group of channels: value = code * scale of its
+    row and group.
+
+    ``codes``: int32, rows x pitch / 4 words as of 4-bit :class:`Rows`.  ``scale``: rows
+    x ceil(channels / group) of bfloat16, float16 or float32, the last axis contiguous.
+    ``group``: a multiple of 32."""
+    codes: torch.Tensor
+    scale: torch.Tensor
+    channels: int
+    group: int
+
+
 class Adapters(NamedTuple):
     """Low-rank adapters over one projection (see qconv_adapters)."""
     a: torch.Tensor          # adapters x rank x c
@@ -67,6 +80,11 @@ class Normed(NamedTuple):
 
 class QConvRows(ctypes.Structure):
     _fields_ = [("codes", _vp), ("scale", _vp), ("pitch", _i64), ("rows", _i32), ("channels", _i32), ("bits", _i32)]
+
+
+class QConvGroupRows(ctypes.Structure):
+    _fields_ = [("codes", _vp), ("scale", _vp), ("pitch", _i64), ("scale_pitch", _i64), ("rows", _i32), ("channels", _i32),
+                ("group", _i32), ("scale_dtype", _i32)]
 
 
 class QConvAdapters(ctypes.Structure):
@@ -92,6 +110,16 @@ def _lib():
         L.qconv_norm_rows_grad_workspace_bytes.argtypes = [_i32, _i32, P(_size)]
         L.qconv_norm_rows_grad.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _i32, _vp, _i32, _i32, _vp, _i64, _vp,
                                            _vp, _size, _vp]
+        L.qconv_linear_groups.argtypes = [P(QConvRows), P(QConvGroupRows), _vp, _i32, _i64, _vp]
+        L.qconv_linear_groups_grad_input.argtypes = [_vp, _i32, _i64, _i32, P(QConvGroupRows), _vp, _i64, _vp, _size, _vp]
+        for f, w in (("", QConvRows), ("_groups", QConvGroupRows)):
+            getattr(L, f"qconv_linear_experts{f}").argtypes = [P(QConvRows), P(w), _vp, _i32, _vp, _i32, _i64, _vp]
+            getattr(L, f"qconv_linear_experts{f}_grad_input").argtypes = [_vp, _i32, _i64, _i32, P(w), _vp, _i32, _vp, _i64, _vp]
+        L.qconv_linear_experts_grad_weight.argtypes = [_vp, _i32, _i64, _i32, P(QConvRows), _vp, _i32, _vp, _i64, _vp]
+        for f in ("qconv_linear_groups", "qconv_linear_groups_grad_input", "qconv_linear_experts",
+                  "qconv_linear_experts_groups", "qconv_linear_experts_grad_input", "qconv_linear_experts_groups_grad_input",
+                  "qconv_linear_experts_grad_weight"):
+            getattr(L, f).restype = ctypes.c_int
         for f in ("qconv_quantize_rows", "qconv_norm_rows", "qconv_norm_rows_grad_workspace_bytes", "qconv_norm_rows_grad", "qconv_linear_workspace_bytes", "qconv_linear",
                   "qconv_linear_grad_workspace_bytes", "qconv_linear_grad_input", "qconv_linear_grad_weight"):
             getattr(L, f).restype = ctypes.c_int
@@ -113,8 +141,8 @@ def _ld(t: torch.Tensor) -> int:
     return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
 
 
-def _rows_arg(r: Rows, name: str, device: torch.device) -> QConvRows:
-    codes, scale, channels, bits = r
+def _codes_arg(codes: torch.Tensor, channels: int, bits: int, name: str, device: torch.device) -> QConvRows:
+    """Rows of codes without their scales."""
     if codes.dim() != 2 or codes.dtype is not (torch.int32 if bits == 4 else torch.int8):
         raise QConvError(EINVAL, f"{name}.codes must be a matrix of {'int32 words' if bits == 4 else 'int8'}")
     m, width = codes.shape
@@ -128,11 +156,42 @@ def _rows_arg(r: Rows, name: str, device: torch.device) -> QConvRows:
     if width < (channels * bits // 8 + 15) // 16 * 16:
         raise QConvError(EINVAL, f"{name}.codes: rows of {width} bytes do not hold {channels} channels in whole "
                                  "16-byte vectors")
-    if scale.dtype is not torch.float32 or scale.shape != (m,) or not scale.is_contiguous():
-        raise QConvError(EINVAL, f"{name}.scale must be one float32 for each row")
-    if codes.get_device() != device.index or scale.get_device() != device.index:
+    if codes.get_device() != device.index:
         raise QConvError(EINVAL, f"{name} must be on {device}")
-    return QConvRows(codes.data_ptr(), scale.data_ptr(), pitch, m, channels, bits)
+    return QConvRows(codes.data_ptr(), None, pitch, m, channels, bits)
+
+
+def _rows_arg(r: Rows, name: str, device: torch.device) -> QConvRows:
+    codes, scale, channels, bits = r
+    a = _codes_arg(codes, channels, bits, name, device)
+    if scale.dtype is not torch.float32 or scale.shape != (a.rows,) or not scale.is_contiguous():
+        raise QConvError(EINVAL, f"{name}.scale must be one float32 for each row")
+    if scale.get_device() != device.index:
+        raise QConvError(EINVAL, f"{name} must be on {device}")
+    a.scale = scale.data_ptr()
+    return a
+
+
+def _group_rows_arg(r: GroupRows, name: str, device: torch.device) -> QConvGroupRows:
+    codes, scale, channels, group = r
+    if scale.dtype not in DTYPES or scale.dim() != 2 or scale.shape[0] != codes.shape[0]:
+        raise QConvError(EINVAL, f"{name}.scale must be one row of bfloat16, float16 or float32 for each row of codes")
+    if group < 1 or scale.shape[1] != -(-channels // group):
+        raise QConvError(EINVAL, f"{name}.scale must have one column for each {group} of {channels} channels")
+    if scale.shape[1] > 1 and scale.stride(1) != 1:
+        raise QConvError(EINVAL, f"{name}.scale: the scales of a row must be contiguous")
+    if scale.get_device() != device.index:
+        raise QConvError(EINVAL, f"{name} must be on {device}")
+    # (the codes as those of 4-bit rows)
+    a = _codes_arg(codes, channels, 4, name, device)
+    return QConvGroupRows(a.codes, scale.data_ptr(), a.pitch, _ld(scale), a.rows, channels, group, DTYPES[scale.dtype])
+
+
+def _weights_arg(w: Rows | GroupRows, device: torch.device):
+    """The weights for a call, and the part of the entry points' names that says their form."""
+    if isinstance(w, GroupRows):
+        return _group_rows_arg(w, "w", device), "_groups"
+    return _rows_arg(w, "w", device), ""
 
 
 def _empty(shape, dtype: torch.dtype, device: torch.device, stream) -> torch.Tensor:
@@ -332,6 +391,13 @@ def pack_rows4(codes: torch.Tensor, scale: torch.Tensor, stream=None) -> Rows:
     return Rows(words.reshape(k, -1), scale, c, 4)
 
 
+def pack_groups4(codes: torch.Tensor, scale: torch.Tensor, group: int, stream=None) -> GroupRows:
+    """int8 codes (rows x channels, saturated into [-8, 7]) and the scales of their
+    groups of channels as 4-bit rows (see :func:`pack_rows4`)."""
+    words, _, channels, _ = pack_rows4(codes, scale, stream)
+    return GroupRows(words, scale, channels, group)
+
+
 def _adapters_arg(ad: Adapters, row_adapter, m: int, c: int, k: int, dtype, device) -> QConvAdapters:
     a, b, alpha = ad
     n, rank = a.shape[:2] if a.dim() == 3 else (0, 0)
@@ -350,20 +416,29 @@ def _adapters_arg(ad: Adapters, row_adapter, m: int, c: int, k: int, dtype, devi
     return QConvAdapters(a.data_ptr(), b.data_ptr(), alpha.data_ptr(), row_adapter.data_ptr(), n, rank)
 
 
-def linear(x: Rows, w: Rows, *, dtype: torch.dtype = torch.bfloat16, adapters: Adapters | None = None,
+def linear(x: Rows, w: Rows | GroupRows, *, dtype: torch.dtype = torch.bfloat16, adapters: Adapters | None = None,
            row_adapter: torch.Tensor | None = None, out: torch.Tensor | None = None,
            workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """rows x k products of 8-bit rows with k x c weights, plus each row's
     adapter's part (qconv_linear).  ``row_adapter``: int32 for each row, -1 for
     none.  ``workspace``: any contiguous device tensor of
-    :func:`linear_workspace_bytes`; made by the call if not given."""
+    :func:`linear_workspace_bytes`; made by the call if not given.  Weights with scales
+    of groups (qconv_linear_groups) need none, and take no adapters."""
     if dtype not in (torch.bfloat16, torch.float16):
         raise QConvError(EINVAL, "dtype must be torch.bfloat16 or torch.float16")
     device = x.codes.device
     if device.type != "cuda":
         raise QConvError(EINVAL, "x must be on a GPU")
-    rx, rw = _rows_arg(x, "x", device), _rows_arg(w, "w", device)
+    rx, (rw, form) = _rows_arg(x, "x", device), _weights_arg(w, device)
     L = _lib()
+    if form:
+        if adapters is not None or row_adapter is not None:
+            raise QConvError(EUNSUPPORTED, "adapters need weights with one scale a row")
+        y = _on(device, out, (rx.rows, rw.rows), dtype, "out", stream)
+        _check(_call(device, L.qconv_linear_groups, ctypes.byref(rx), ctypes.byref(rw), y.data_ptr(), DTYPES[dtype], _ld(y),
+                     _stream(stream, device)), "qconv_linear_groups")
+        _hold(stream, *x[:2], *w[:2], out)
+        return y
     ad, need = None, 0
     if adapters is not None:
         ad = _adapters_arg(adapters, row_adapter, rx.rows, rx.channels, rw.rows, dtype, device)
@@ -399,19 +474,21 @@ def grad_workspace_bytes(rows: int, cols: int, depth: int) -> int:
     return n.value
 
 
-def linear_grad_input(dy: torch.Tensor, w: Rows, *, out: torch.Tensor | None = None,
+def linear_grad_input(dy: torch.Tensor, w: Rows | GroupRows, *, out: torch.Tensor | None = None,
                       workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
-    """dy (rows x k) times the weights (k x c), of dy's type (qconv_linear_grad_input)."""
+    """dy (rows x k) times the weights (k x c), of dy's type (qconv_linear_grad_input, or
+    qconv_linear_groups_grad_input by weights with scales of groups)."""
     _matrix(dy, "dy")
     device = dy.device
-    rw = _rows_arg(w, "w", device)
+    rw, form = _weights_arg(w, device)
+    name = f"qconv_linear{form}_grad_input"
     m = dy.shape[0]
     if dy.shape[1] != rw.rows:
         raise QConvError(EINVAL, f"dy has {dy.shape[1]} columns, w {rw.rows} rows")
     dx = _on(device, out, (m, rw.channels), dy.dtype, "out", stream)
     keep, ws, ws_bytes = _workspace(grad_workspace_bytes(m, rw.channels, rw.rows), workspace, device, stream)
-    _check(_call(device, _lib().qconv_linear_grad_input, dy.data_ptr(), DTYPES[dy.dtype], _ld(dy), m, ctypes.byref(rw),
-                 dx.data_ptr(), _ld(dx), ws, ws_bytes, _stream(stream, device)), "qconv_linear_grad_input")
+    _check(_call(device, getattr(_lib(), name), dy.data_ptr(), DTYPES[dy.dtype], _ld(dy), m, ctypes.byref(rw),
+                 dx.data_ptr(), _ld(dx), ws, ws_bytes, _stream(stream, device)), name)
     _hold(stream, dy, *w[:2], out, workspace)
     return dx
 
@@ -431,6 +508,87 @@ def linear_grad_weight(dy: torch.Tensor, x: Rows, *, out: torch.Tensor | None = 
     _check(_call(device, _lib().qconv_linear_grad_weight, dy.data_ptr(), DTYPES[dy.dtype], _ld(dy), k, ctypes.byref(rx),
                  dw.data_ptr(), _ld(dw), ws, ws_bytes, _stream(stream, device)), "qconv_linear_grad_weight")
     _hold(stream, dy, *x[:2], out, workspace)
+    return dw
+
+
+def _experts_arg(offsets: torch.Tensor, device: torch.device) -> tuple[int, int]:
+    """(pointer, experts)."""
+    if offsets.dtype is not torch.int32 or offsets.dim() != 1 or offsets.shape[0] < 2 or not offsets.is_contiguous():
+        raise QConvError(EINVAL, "offsets must be int32: the first row of each expert, and the end of the last one's")
+    if offsets.get_device() != device.index:
+        raise QConvError(EINVAL, f"offsets must be on {device}")
+    return offsets.data_ptr(), offsets.shape[0] - 1
+
+
+def _of_experts(rows: int, experts: int) -> int:
+    if rows % experts:
+        raise QConvError(EINVAL, f"w has {rows} rows, not those of {experts} experts")
+    return rows // experts
+
+
+def linear_experts(x: Rows, w: Rows | GroupRows, offsets: torch.Tensor, *, dtype: torch.dtype = torch.bfloat16,
+                   out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Rows sorted by expert, each times its expert's k x c weights (qconv_linear_experts):
+    expert e has rows ``offsets[e]`` to ``offsets[e + 1] - 1`` of x, and rows e k to
+    e k + k - 1 of w.  ``offsets`` is int32 on the device and read there.  Rows of no
+    expert keep what ``out`` holds."""
+    if dtype not in (torch.bfloat16, torch.float16):
+        raise QConvError(EINVAL, "dtype must be torch.bfloat16 or torch.float16")
+    device = x.codes.device
+    if device.type != "cuda":
+        raise QConvError(EINVAL, "x must be on a GPU")
+    rx, (rw, form) = _rows_arg(x, "x", device), _weights_arg(w, device)
+    at, experts = _experts_arg(offsets, device)
+    y = _on(device, out, (rx.rows, _of_experts(rw.rows, experts)), dtype, "out", stream)
+    name = f"qconv_linear_experts{form}"
+    _check(_call(device, getattr(_lib(), name), ctypes.byref(rx), ctypes.byref(rw), at, experts, y.data_ptr(), DTYPES[dtype],
+                 _ld(y), _stream(stream, device)), name)
+    _hold(stream, *x[:2], *w[:2], offsets, out)
+    return y
+
+
+def linear_experts_grad_input(dy: torch.Tensor, w: Rows | GroupRows, offsets: torch.Tensor, *,
+                              out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Each row of dy (rows x k) times its expert's weights (k x c), of dy's type
+    (qconv_linear_experts_grad_input).  Rows of no expert keep what ``out`` holds."""
+    _matrix(dy, "dy")
+    device = dy.device
+    rw, form = _weights_arg(w, device)
+    at, experts = _experts_arg(offsets, device)
+    m, k = dy.shape
+    if k != _of_experts(rw.rows, experts):
+        raise QConvError(EINVAL, f"dy has {k} columns, an expert {rw.rows // experts} rows")
+    dx = _on(device, out, (m, rw.channels), dy.dtype, "out", stream)
+    name = f"qconv_linear_experts{form}_grad_input"
+    _check(_call(device, getattr(_lib(), name), dy.data_ptr(), DTYPES[dy.dtype], _ld(dy), m, ctypes.byref(rw), at, experts,
+                 dx.data_ptr(), _ld(dx), _stream(stream, device)), name)
+    _hold(stream, dy, *w[:2], offsets, out)
+    return dx
+
+
+def linear_experts_grad_weight(dy: torch.Tensor, x: Rows, offsets: torch.Tensor, *, out: torch.Tensor | None = None,
+                               stream=None) -> torch.Tensor:
+    """For each expert, its rows of dy transposed (k x rows) times its rows of x: float32,
+    experts x k x c, zeros for an expert without rows (qconv_linear_experts_grad_weight).
+    ``out``: contiguous."""
+    _matrix(dy, "dy")
+    device = dy.device
+    rx = _rows_arg(x, "x", device)
+    at, experts = _experts_arg(offsets, device)
+    m, k = dy.shape
+    if m != rx.rows:
+        raise QConvError(EINVAL, f"dy has {m} rows, x {rx.rows}")
+    shape = (experts, k, rx.channels)
+    if out is None:
+        dw = _empty(shape, torch.float32, device, stream)
+    elif out.shape != shape or out.dtype is not torch.float32 or out.device != device or not out.is_contiguous():
+        raise QConvError(EINVAL, f"out must be {shape} of torch.float32, contiguous and on {device}")
+    else:
+        dw = out
+    _check(_call(device, _lib().qconv_linear_experts_grad_weight, dy.data_ptr(), DTYPES[dy.dtype], _ld(dy), k,
+                 ctypes.byref(rx), at, experts, dw.data_ptr(), rx.channels, _stream(stream, device)),
+           "qconv_linear_experts_grad_weight")
+    _hold(stream, dy, *x[:2], offsets, out)
     return dw
 
 
