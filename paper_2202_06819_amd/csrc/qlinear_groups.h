@@ -137,71 +137,71 @@ __device__ __forceinline__ void groups_few(const LinearArgs &a, const GroupArg &
 
 // --------------------------------------------------------------- many rows
 
-// A step's products for FJ x FI fragments, each slice's scaled and added to d: the whole
-// numbers live for one fragment at a time.  `scales`: NG x TJ floats.
+// The products of a slice: 64 channels deep, or 32.
+template <int NG>
+struct GroupsMma : MmaI8 {};
+template <>
+struct GroupsMma<4> {
+    using frag = long;
+    static __device__ __forceinline__ i32x4 mma(frag a, frag b, i32x4 c) {
+        return __builtin_amdgcn_mfma_i32_16x16x32_i8(a, b, c, 0, 0, 0);
+    }
+};
+
+// A step's products for FJ x FI fragments, each slice's scaled and added to d.  While two
+// fragments are multiplied the two before them are converted, scaled and added, so that
+// the vector instructions (two a result and slice) run beside the matrix cores; the units
+// are fenced off from each other, or the scheduler brings forth all whole numbers first
+// and has no registers for them.  `scales`: NG x TJ floats.
 template <int NG, int TJ, int FJ, int FI>
 __device__ __forceinline__ void groups_step(const uint8_t *lj, const uint8_t *li, const float *scales, int jrow0, int irow0,
                                             int lane, f32x4 (&d)[FJ][FI]) {
     static_assert(FJ == 4, "a lane holds 16 consecutive rows of the product");
+    constexpr int kHalves = NG == 1 ? 2 : 1;   // products of a slice
+    typedef typename GroupsMma<NG>::frag frag;
     const int r = lane & 15, g = lane >> 4;
-    const auto fold = [&](const i32x4 (&t)[FJ], const f32x4 (&ws)[FJ], int i) {
-#pragma unroll
-        for (int j = 0; j < FJ; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) d[j][i][e] = __builtin_fmaf((float)t[j][e], ws[j][e], d[j][i][e]);
+    // the lane's part of row `row`, product h of a slice
+    const auto read = [&](const uint8_t *l, int row, int slice, int h) {
+        if constexpr (NG < 4)
+            return *reinterpret_cast<const frag *>(l + row * kStepBytes + ((((slice + h) * 4 + g) ^ slot(row)) << 4));
+        else   // 32 channels: eight a lane
+            return *reinterpret_cast<const frag *>(l + row * kStepBytes + (((slice * 2 + (g >> 1)) ^ slot(row)) << 4) + (g & 1) * 8);
     };
-    const auto read_scales = [&](int slice, f32x4 (&ws)[FJ]) {
+#pragma unroll
+    for (int slice = 0; slice < NG; ++slice) {
+        frag w[kHalves][FJ], x[kHalves];
+        f32x4 ws[FJ];
 #pragma unroll
         for (int j = 0; j < FJ; ++j) ws[j] = *reinterpret_cast<const f32x4 *>(scales + slice * TJ + jrow0 + g * 16 + 4 * j);
-    };
-    const auto vector = [&](const uint8_t *l, int row, int v) {
-        return *reinterpret_cast<const i32x4 *>(l + row * kStepBytes + ((v ^ slot(row)) << 4));
-    };
-    if constexpr (NG < 4) {
 #pragma unroll
-        for (int part = 0; part < NG; ++part) {
-            constexpr int kHalves = 2 / NG;
-            i32x4 w[kHalves][FJ];
-            f32x4 ws[FJ];
-            read_scales(part, ws);
+        for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j) w[h][j] = read(lj, jrow0 + j_row(j, r), slice, h);
+        i32x4 t[2][2];
+        // unit u: fragments 2 (u % 2) and the one after it of row fragment u / 2
+        const auto fold = [&](int u) {
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const int j = u % 2 * 2 + n;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) d[j][u / 2][e] = __builtin_fmaf((float)t[u & 1][n][e], ws[j][e], d[j][u / 2][e]);
+                asm volatile("" : "+v"(d[j][u / 2]));   // here, not where the sum is next used
+            }
+        };
+#pragma unroll
+        for (int u = 0; u < 2 * FI; ++u) {
+            if (u % 2 == 0)
+#pragma unroll
+                for (int h = 0; h < kHalves; ++h) x[h] = read(li, irow0 + u / 2 * 16 + r, slice, h);
 #pragma unroll
             for (int h = 0; h < kHalves; ++h)
 #pragma unroll
-                for (int j = 0; j < FJ; ++j) w[h][j] = vector(lj, jrow0 + j_row(j, r), (part + h) * 4 + g);
-#pragma unroll
-            for (int i = 0; i < FI; ++i) {
-                i32x4 t[FJ];
-#pragma unroll
-                for (int h = 0; h < kHalves; ++h) {
-                    const i32x4 x = vector(li, irow0 + i * 16 + r, (part + h) * 4 + g);
-#pragma unroll
-                    for (int j = 0; j < FJ; ++j) t[j] = MmaI8::mma(w[h][j], x, h ? t[j] : i32x4{0, 0, 0, 0});
-                }
-                fold(t, ws, i);
-            }
+                for (int n = 0; n < 2; ++n)
+                    t[u & 1][n] = GroupsMma<NG>::mma(w[h][u % 2 * 2 + n], x[h], h ? t[u & 1][n] : i32x4{0, 0, 0, 0});
+            if (u) fold(u - 1);
+            __builtin_amdgcn_sched_barrier(0);
         }
-    } else {
-        // 32 channels: eight a lane
-        const auto eight = [&](const uint8_t *l, int row, int part) {
-            return *reinterpret_cast<const long *>(l + row * kStepBytes + (((part * 2 + (g >> 1)) ^ slot(row)) << 4) + (g & 1) * 8);
-        };
-#pragma unroll
-        for (int part = 0; part < NG; ++part) {
-            long w[FJ];
-            f32x4 ws[FJ];
-            read_scales(part, ws);
-#pragma unroll
-            for (int j = 0; j < FJ; ++j) w[j] = eight(lj, jrow0 + j_row(j, r), part);
-#pragma unroll
-            for (int i = 0; i < FI; ++i) {
-                const long x = eight(li, irow0 + i * 16 + r, part);
-                i32x4 t[FJ];
-#pragma unroll
-                for (int j = 0; j < FJ; ++j)
-                    t[j] = __builtin_amdgcn_mfma_i32_16x16x32_i8(w[j], x, i32x4{0, 0, 0, 0}, 0, 0, 0);
-                fold(t, ws, i);
-            }
-        }
+        fold(2 * FI - 1);
     }
 }
 
