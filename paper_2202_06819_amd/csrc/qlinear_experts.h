@@ -36,8 +36,7 @@ __device__ __forceinline__ void lane_expert(const ExpertArg &ex, int e, int &row
     }
 }
 
-// Tiles of SIZE rows of all experts, and which rows the `which`-th of them holds
-// (0 <= which < the tiles of all).
+// Tiles of SIZE rows of all experts.
 template <int SIZE>
 __device__ __forceinline__ int expert_tiles(const ExpertArg &ex) {
     int total = 0;
@@ -48,19 +47,22 @@ __device__ __forceinline__ int expert_tiles(const ExpertArg &ex) {
     }
     return total;
 }
+// Which rows the `which`-th of them holds; false: there are not so many.
 template <int SIZE>
-__device__ __forceinline__ ExpertRows expert_tile(const ExpertArg &ex, int which) {
-    for (int e0 = 0;; e0 += 64) {
+__device__ __forceinline__ bool expert_tile(const ExpertArg &ex, int which, ExpertRows &p) {
+    for (int e0 = 0; e0 < ex.count; e0 += 64) {
         int row0, rows, tiles, sum;
         lane_expert<SIZE>(ex, e0 + ((int)threadIdx.x & 63), row0, rows, tiles, sum);
         const uint64_t past = __ballot(sum > which);
-        if (past || e0 + 64 >= ex.count) {
-            const int lane = past ? __builtin_ctzll(past) : 63;
-            return {e0 + lane, __builtin_amdgcn_readlane(row0, lane), __builtin_amdgcn_readlane(rows, lane),
-                    which - (__builtin_amdgcn_readlane(sum, lane) - __builtin_amdgcn_readlane(tiles, lane))};
+        if (past) {
+            const int lane = __builtin_ctzll(past);
+            p = {e0 + lane, __builtin_amdgcn_readlane(row0, lane), __builtin_amdgcn_readlane(rows, lane),
+                 which - (__builtin_amdgcn_readlane(sum, lane) - __builtin_amdgcn_readlane(tiles, lane))};
+            return true;
         }
         which -= __builtin_amdgcn_readlane(sum, 63);
     }
+    return false;
 }
 
 // The rows of expert e alone.
@@ -77,8 +79,7 @@ __device__ __forceinline__ bool expert_place(const ExpertArg &ex, int tiles_j, E
     if (id >= total * tiles_j) return false;
     int ti;
     tile_at(xcd_run(id, total * tiles_j), total, tiles_j, ti, tj);
-    rows = expert_tile<SIZE>(ex, ti);
-    return true;
+    return expert_tile<SIZE>(ex, ti, rows);
 }
 
 // A product's operands for those rows.

@@ -13,8 +13,8 @@ namespace {
 template <class T, int WB, int FJ, int FI>
 __global__ void __launch_bounds__(512) experts_rows(LinearArgs a, ExpertArg ex) {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-    if ((int)blockIdx.y >= expert_tiles<16 * FI>(ex)) return;
-    const ExpertRows p = expert_tile<16 * FI>(ex, (int)blockIdx.y);
+    ExpertRows p;
+    if (!expert_tile<16 * FI>(ex, (int)blockIdx.y, p)) return;
     few_product<T, WB, FJ, FI, false>(of_expert(a, p), (int)blockIdx.x, p.tile, smem);
 }
 template <class T, int WB, int TJ, int TI, int WJ, int WI, int KS>

@@ -308,7 +308,7 @@ __device__ __forceinline__ void add_adapters(const LinearArgs &a, int id, int ro
 // bits: 4.4 us without adapters (8.4 MB, 1.9 TB/s).
 constexpr int few_lds(int fj, int fi, bool ad) { return 8 * 64 * 16 * (fj * fi + (ad ? fj : 0)); }
 template <class T, int WB, int FJ, int FI, bool AD>
-__device__ __forceinline__ void few_product(const LinearArgs &a, int tile_j, int tile_i, uint8_t *smem) {
+__device__ __forceinline__ void few_product(LinearArgs a, int tile_j, int tile_i, uint8_t *smem) {
     constexpr int kWaves = 8, kParts = kWaves / FI;
     constexpr int kWide = WB == 8 ? 2 : 1;   // 16-byte vectors of weights a lane and step
     auto part = reinterpret_cast<i32x4(*)[FJ * FI][64]>(smem);                                // waves' sums
@@ -607,7 +607,7 @@ constexpr int tile_lds() {
 // cores, which its random operands hold to what power allows: 8192 x 4096 x 4096 takes
 // 118 to 124 us, 2.2 to 2.3 POP/s of the 3.1 that products of registers alone reach.
 template <class T, int WB, int TJ, int TI, int WJ, int WI, int KS, bool AD>
-__device__ __forceinline__ void tile_product(const LinearArgs &a, int tj, int ti, uint8_t *smem) {
+__device__ __forceinline__ void tile_product(LinearArgs a, int tj, int ti, uint8_t *smem) {
     constexpr int FJ = 4, FI = TI / (16 * WI), kThreads = WJ * WI * 64, kBuffer = (TJ + TI) * kStepBytes;
     static_assert(TJ == WJ * 64);
     static_assert(KS == 1 || FI == 1);

@@ -109,7 +109,7 @@ __device__ __forceinline__ uint32_t scaled_pair(uint32_t w, int half, float s0, 
 // GS: 0, or the bytes of a scale of a group of channels (4-bit codes); a wave's columns
 // lie within 32 channels, so it reads one scale for each t as it does without groups.
 template <class T, int WB, bool TRANSPOSED, bool COPY, int GS, int TJ, int TI, int WJ, int WI, int KS>
-__device__ __forceinline__ void grad_product(const GradArgs &a, const GroupArg &groups, int split, int ti, int tj,
+__device__ __forceinline__ void grad_product(GradArgs a, GroupArg groups, int split, int ti, int tj,
                                              uint8_t *all_smem) {
     constexpr int FJ = TJ / (16 * WJ), FI = TI / (16 * WI), kThreads = WJ * WI * 64, kWaves = kThreads / 64;
     constexpr int kCodes = 64 * TJ, kP = TI * 128, kStage = kCodes + kP + grad_scale_bytes(GS, TJ);
@@ -374,7 +374,7 @@ __device__ __forceinline__ void grad_product(const GradArgs &a, const GroupArg &
         for (int n = 0; n < (GS ? kSlots : 1); ++n) {
             const float v = GS ? scale_value<GS ? GS : 4>(groups, group_scale(t, n)) : a.b.scale[t];
             const uint32_t b = __builtin_bit_cast(uint32_t, v) & 0x7fffffffu;
-            if (b < 0x7f800000u) m = max(m, b);
+            m = max(m, b < 0x7f800000u ? b : 0u);
         }
         return m;
     };

@@ -13,126 +13,227 @@ namespace qconv {
 
 // --------------------------------------------------------------- few rows
 
-// Up to 16 / NG * RB rows against 16 FJ output channels a workgroup, eight waves taking
-// the 128-channel steps in turn, as in the few-row kernel of whole rows' scales.  A lane
-// has 16 bytes of weights of one channel, 32 values: they belong to one group, whichever
-// the groups' size, but the matrix instruction adds up what four lanes hold.  So the
-// rows of its other operand are NG copies of 16 / NG rows of x, each zero but for the
-// lanes of its own slice: a product then gives the slices' sums apart, at no cost in
-// reading weights, which bounds this kernel.  A result's lane holds one channel, so that
-// one scale serves its four results.
-constexpr int kGroupWaves = 8;
-constexpr int groups_few_lds(int fj, int rb, int ng) { return kGroupWaves * fj * rb * (64 / ng) * 16; }
-template <int GS, int NG, int FJ, int RB>
-__device__ __forceinline__ void groups_few(const LinearArgs &a, const GroupArg &groups, bool bf16, int tile_j, int tile_i,
-                                           uint8_t *smem) {
-    constexpr int kRows = 16 / NG, kFlight = 4, kLanes = 64 / NG;
-    auto part = reinterpret_cast<f32x4(*)[FJ * RB][kLanes]>(smem);
+// 16 / NG * RB rows against 16 output channels a wave, or, where there are few channels,
+// a run of `share` waves that take blocks of four 128-channel steps in turn and whose sums
+// meet in LDS.  Weights go straight from memory into registers, a block ahead; rows are
+// staged in LDS, `chunk` steps of them at a time.  (Bound by reading the weights, 8192 x
+// 4096 of one row in 5.3 us; rows and scales read from memory beside each step's weights
+// add 2.2 and 1.3 us to that, loads that give nothing among them: hence LDS, and a block's
+// scales in one or two loads.)
+//
+// A lane has 16 bytes of weights of one channel, 32 values: they belong to one group,
+// whichever the groups' size, but the matrix instruction adds up what four lanes hold.
+// So the rows of its other operand are NG copies of 16 / NG rows of x, each zero but for
+// the lanes of its own slice: a product then gives the slices' sums apart, at no cost in
+// reading weights.  A result's lane holds one channel, so that one scale serves its four
+// results.  EVEN: groups of 128 / NG channels; others are served by NG 4, whose scales are
+// loaded one by one.
+constexpr int kGroupWaves = 8, kBlock = 4;   // waves of a workgroup; steps of a block
+constexpr int kZeros = kBlock * kStepBytes;  // LDS that lanes of other slices read
+constexpr int few_pitch(int chunk) { return chunk * kStepBytes + 16; }
+constexpr int groups_few_lds(int rows, int chunk, int rb, int ng) {
+    const int x = rows * few_pitch(chunk), sums = kGroupWaves * rb * (64 / ng) * 16;
+    return kZeros + (x > sums ? x : sums);
+}
+template <int GS, int NG, bool EVEN, int RB>
+__device__ __forceinline__ void groups_few(LinearArgs a, GroupArg groups, bool bf16, int share, int chunk, int tile_j,
+                                           int tile_i, uint8_t *smem) {
+    static_assert(EVEN || NG == 4);
+    constexpr int kRows = 16 / NG, kLanes = 64 / NG, kScales = kBlock * NG;   // a row's scales of a block
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int r = lane & 15, g = lane >> 4;
-    const int ch0 = tile_j * 16 * FJ, row0 = tile_i * kRows * RB;
+    const int turn = wave & (share - 1);
+    const int ch0 = (tile_j * kGroupWaves + wave) / share * 16, row0 = tile_i * kRows * RB;
+    const int rows = min(a.m - row0, kRows * RB);
     const __amdgpu_buffer_rsrc_t rx = range_of(a.x.codes + (int64_t)row0 * a.x.pitch,
-                                               (int64_t)(a.m - 1 - row0) * a.x.pitch + a.x.used);
+                                               (int64_t)(rows - 1) * a.x.pitch + a.x.used);
     const __amdgpu_buffer_rsrc_t rw = range_of(a.w.codes + (int64_t)ch0 * a.w.pitch,
                                                (int64_t)(a.k - 1 - ch0) * a.w.pitch + a.w.used);
-    const int last = (a.c - 1) / 32;   // the row's last 32 channels
-    const __amdgpu_buffer_rsrc_t rs = range_of(static_cast<const uint8_t *>(groups.scale) + (int64_t)ch0 * groups.pitch * GS,
-                                               ((int64_t)(a.k - 1 - ch0) * groups.pitch + group_of(groups, last) + 1) * GS);
-    const int slice = g * NG / 4;             // of the lane's weights, and of its results
-    const bool mine = r / kRows == slice;     // the lane's row of x is its slice's copy
-    struct Step {
-        u32x4_t w[FJ], x[RB][2];
-        uint32_t scale[FJ];
-    };
-    const auto load = [&](int s, Step &q) {
-        const int at = s * 64 + g * 16;
-        const bool in = at < a.w.used;
-        const int unit = s * 4 + slice * (4 / NG);
-        const uint32_t group = (uint32_t)group_of(groups, min(unit, last));
+    const int last = (a.c - 1) / 32, held = group_of(groups, last) + 1;   // the row's last 32 channels, its groups
+    const uint8_t *const scales = static_cast<const uint8_t *>(groups.scale) + (int64_t)min(ch0 + r, a.k - 1) * groups.pitch * GS;
+    const int slice = g * NG / 4;   // of the lane's weights, and of its results
+
+    // Steps from `from` on of the rows of x into LDS, zeros past the row's end.  Waves are
+    // dealt to the rows.
+    const int per_row = rows >= 8 ? 1 : rows >= 4 ? 2 : rows >= 2 ? 4 : 8;
+    const auto stage = [&](int from, int count) {
+        for (int row = wave / per_row; row < rows; row += kGroupWaves / per_row) {
+            uint8_t *const to = smem + kZeros + row * few_pitch(chunk);
+            constexpr int kDeep = 4;
+            for (int v = (wave % per_row) * 64 + lane; v - lane < count * 8; v += kDeep * per_row * 64) {
+                u32x4_t q[kDeep];
 #pragma unroll
-        for (int j = 0; j < FJ; ++j) {
-            q.w[j] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(
-                rw, (int)(in ? (uint32_t)(j * 16 + r) * (uint32_t)a.w.pitch + (uint32_t)at : kNowhere), 0, 0));
-            const int to = (int)(unit <= last ? ((uint32_t)(j * 16 + r) * (uint32_t)groups.pitch + group) * GS : kNowhere);
-            if constexpr (GS == 4) q.scale[j] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, to, 0, 0);
-            else q.scale[j] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, to, 0, 0);
-        }
+                for (int e = 0; e < kDeep; ++e) {
+                    const int at = (from * 8 + v + e * per_row * 64) * 16;
+                    q[e] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(
+                        rx, (int)(at < a.x.used ? (uint32_t)row * (uint32_t)a.x.pitch + (uint32_t)at : kNowhere), 0, 0));
+                }
 #pragma unroll
-        for (int b = 0; b < RB; ++b)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int from = s * 128 + g * 32 + h * 16;
-                q.x[b][h] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(
-                    rx, (int)(mine && from < a.x.used
-                                  ? (uint32_t)(b * kRows + r % kRows) * (uint32_t)a.x.pitch + (uint32_t)from : kNowhere), 0, 0));
-            }
-    };
-    f32x4 acc[FJ][RB];
-#pragma unroll
-    for (int j = 0; j < FJ; ++j)
-#pragma unroll
-        for (int b = 0; b < RB; ++b) acc[j][b] = f32x4{0, 0, 0, 0};
-    const auto multiply = [&](const Step &q) {
-#pragma unroll
-        for (int j = 0; j < FJ; ++j) {
-            i32x4 w[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint2 p = widen8(q.w[j][2 * h]), t = widen8(q.w[j][2 * h + 1]);
-                w[h] = i32x4{(int)p.x, (int)p.y, (int)t.x, (int)t.y};
-            }
-            const float scale = scale_value<GS>(groups, q.scale[j]);
-#pragma unroll
-            for (int b = 0; b < RB; ++b) {
-                i32x4 t{0, 0, 0, 0};
-                t = MmaI8::mma(__builtin_bit_cast(i32x4, q.x[b][0]), w[0], t);
-                t = MmaI8::mma(__builtin_bit_cast(i32x4, q.x[b][1]), w[1], t);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[j][b][e] = __builtin_fmaf((float)t[e], scale, acc[j][b][e]);
+                for (int e = 0; e < kDeep; ++e)
+                    if (v + e * per_row * 64 < count * 8) *reinterpret_cast<u32x4_t *>(to + (v + e * per_row * 64) * 16) = q[e];
             }
         }
     };
-    Step q[kFlight];
+    // (what lies past a row of weights meets zeros of x; past the last row nothing is read)
+    u32x4_t w[kBlock];
+    const uint32_t w_at = (uint32_t)r * (uint32_t)a.w.pitch + (uint32_t)g * 16;
+    const auto load = [&](int s, u32x4_t &q) {
+        q = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(s < a.steps ? w_at + (uint32_t)s * 64u : kNowhere), 0, 0));
+    };
+    // The scales of a block's slices, as they lie in memory: all of them, or (one by one)
+    // the lane's own.
+    struct Scales {
+        uint32_t q[EVEN ? kScales * GS / 4 : kBlock];
+    };
+    const auto load_scales = [&](int block, Scales &q) {
+        if constexpr (EVEN) {
+            const int at = block * kScales;
+            if (at + kScales <= held) {
+                __builtin_memcpy(q.q, scales + at * GS, kScales * GS);
+            } else {   // the row's end
 #pragma unroll
-    for (int e = 0; e < kFlight; ++e)
-        if (wave + e * kGroupWaves < a.steps) load(wave + e * kGroupWaves, q[e]);
-    for (int s = wave; s < a.steps; s += kFlight * kGroupWaves) {
+                for (int n = 0; n < kScales * GS / 4; ++n) q.q[n] = 0;
 #pragma unroll
-        for (int e = 0; e < kFlight; ++e) {
-            if (s + e * kGroupWaves < a.steps) multiply(q[e]);
-            if (s + (kFlight + e) * kGroupWaves < a.steps) load(s + (kFlight + e) * kGroupWaves, q[e]);
+                for (int n = 0; n < kScales; ++n) {
+                    const int from = min(at + n, held - 1);
+                    const uint32_t v = GS == 4 ? reinterpret_cast<const uint32_t *>(scales)[from]
+                                               : reinterpret_cast<const uint16_t *>(scales)[from];
+                    if (at + n < held) q.q[n * GS / 4] |= v << (GS == 2 ? n % 2 * 16 : 0);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < kBlock; ++e) {
+                const int unit = (block * kBlock + e) * 4 + g;
+                const uint32_t v = load_scale<GS>(groups, (int64_t)min(ch0 + r, a.k - 1) * groups.pitch + group_of(groups, min(unit, last)));
+                q.q[e] = unit <= last ? v : 0u;
+            }
         }
+    };
+    const auto scale_of = [&](const Scales &q, int e) {   // of the lane's slice in step e
+        if constexpr (!EVEN) return scale_value<GS>(groups, q.q[e]);
+        // (by masks: a choice between two of an array's places would put it into memory)
+        const uint32_t odd = slice & 1 ? ~0u : 0u, high = slice & 2 ? ~0u : 0u;
+        const auto either = [](uint32_t mask, uint32_t yes, uint32_t no) { return (yes & mask) | (no & ~mask); };
+        uint32_t v;
+        if constexpr (GS == 4) {
+            if constexpr (NG == 1) v = q.q[e];
+            else if constexpr (NG == 2) v = either(odd, q.q[2 * e + 1], q.q[2 * e]);
+            else v = either(high, either(odd, q.q[4 * e + 3], q.q[4 * e + 2]), either(odd, q.q[4 * e + 1], q.q[4 * e]));
+        } else {
+            if constexpr (NG == 1) v = q.q[e / 2] >> (e % 2 * 16);
+            else if constexpr (NG == 2) v = q.q[e] >> (odd & 16);
+            else v = either(high, q.q[2 * e + 1], q.q[2 * e]) >> (odd & 16);
+            v &= 0xffffu;
+        }
+        return scale_value<GS>(groups, v);
+    };
+    // Lanes of x's operand: their row in LDS, or zeros.
+    uint32_t x_at[RB], moves[RB];   // moves: all ones where the address moves on with the block
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+        const int row = b * kRows + r % kRows;
+        const bool mine = r / kRows == slice && row < rows;
+        moves[b] = mine ? ~0u : 0u;
+        x_at[b] = mine ? (uint32_t)(kZeros + row * few_pitch(chunk) + g * 32) : 0u;
+    }
+    f32x4 acc[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) acc[b] = f32x4{0, 0, 0, 0};
+    const auto multiply = [&](const u32x4_t &q, float scale, const uint8_t *const (&from)[RB], int e) {
+        i32x4 ww[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint2 p = widen8(q[2 * h]), t = widen8(q[2 * h + 1]);
+            ww[h] = i32x4{(int)p.x, (int)p.y, (int)t.x, (int)t.y};
+        }
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+            i32x4 t{0, 0, 0, 0};
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                t = MmaI8::mma(*reinterpret_cast<const i32x4 *>(from[b] + e * kStepBytes + h * 16), ww[h], t);
+#pragma unroll
+            for (int n = 0; n < 4; ++n) acc[b][n] = __builtin_fmaf((float)t[n], scale, acc[b][n]);
+            asm volatile("" : "+v"(acc[b]));   // here, not where the sum is next used
+        }
+    };
+
+    const __amdgpu_buffer_rsrc_t rxs = range_of(a.x.scale + row0, (int64_t)rows * 4);
+    float xs[RB][4];   // of the lane's results, wanted at the end
+#pragma unroll
+    for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            xs[b][e] = __builtin_bit_cast(float, (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rxs, (b * kRows + g * 4 + e) * 4, 0, 0));
+    if ((int)threadIdx.x < kZeros / 16) reinterpret_cast<u32x4_t *>(smem)[threadIdx.x] = u32x4_t{0, 0, 0, 0};
+    const int blocks = (a.steps + kBlock - 1) / kBlock, turns = (blocks + share - 1) / share;   // a wave's
+    const int chunk_turns = chunk / (kBlock * share);
+    stage(0, min(chunk, turns * share * kBlock));
+    Scales scale;
+    load_scales(turn, scale);
+#pragma unroll
+    for (int e = 0; e < kBlock; ++e) load(turn * kBlock + e, w[e]);
+    __builtin_amdgcn_sched_barrier(0);
+    __syncthreads();
+    for (int n = 0, left = chunk_turns; n < turns; ++n, --left) {
+        if (left == 0) {   // the next chunk
+            left = chunk_turns;
+            __syncthreads();
+            stage(n * share * kBlock, min(chunk, (turns - n) * share * kBlock));
+            __syncthreads();
+        }
+        const uint32_t off = (uint32_t)((chunk_turns - left) * share + turn) * (kBlock * kStepBytes);
+        const uint8_t *from[RB];
+#pragma unroll
+        for (int b = 0; b < RB; ++b) from[b] = smem + x_at[b] + (off & moves[b]);
+        const int next = (n + 1) * share + turn;
+        Scales then;
+        load_scales(next, then);
+#pragma unroll
+        for (int e = 0; e < kBlock; ++e) {
+            multiply(w[e], scale_of(scale, e), from, e);
+            __builtin_amdgcn_sched_barrier(0);
+            load(next * kBlock + e, w[e]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        scale = then;
     }
     // the slices' sums of a row and channel meet: lanes 16 and 32 apart
 #pragma unroll
-    for (int j = 0; j < FJ; ++j)
-#pragma unroll
-        for (int b = 0; b < RB; ++b) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (NG == 4) acc[j][b][e] += __shfl_xor(acc[j][b][e], 16);
-                if (NG >= 2) acc[j][b][e] += __shfl_xor(acc[j][b][e], 32);
-            }
-            if (lane < kLanes) part[wave][j * RB + b][lane] = acc[j][b];
-        }
-    __syncthreads();
-    // four rows of one channel a thread
-    for (int o = (int)threadIdx.x; o < FJ * RB * kLanes; o += kGroupWaves * 64) {
-        const int f = o / kLanes, l = o % kLanes, j = f / RB, b = f % RB;
-        f32x4 t = part[0][f][l];
-#pragma unroll
-        for (int w = 1; w < kGroupWaves; ++w) t += part[w][f][l];
-        const int ch = ch0 + j * 16 + (l & 15), row = row0 + b * kRows + (l >> 4) * 4;
-        if (ch >= a.k) continue;
+    for (int b = 0; b < RB; ++b)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            if (row + e >= a.m) break;
-            const float y = t[e] * (a.x.scale[row + e] * 0.0625f);
-            const int64_t to = (int64_t)(row + e) * a.ldy + ch;
+            if (NG == 4) acc[b][e] += __shfl_xor(acc[b][e], 16);
+            if (NG >= 2) acc[b][e] += __shfl_xor(acc[b][e], 32);
+        }
+    if (share > 1) {
+        auto part = reinterpret_cast<f32x4(*)[RB][kLanes]>(smem + kZeros);
+        __syncthreads();   // everyone is done with the rows
+        if (lane < kLanes)
+#pragma unroll
+            for (int b = 0; b < RB; ++b) part[wave][b][lane] = acc[b];
+        __syncthreads();
+        if (turn) return;
+        if (lane < kLanes)
+            for (int n = 1; n < share; ++n)
+#pragma unroll
+                for (int b = 0; b < RB; ++b) acc[b] += part[wave + n][b][lane];
+    }
+    // four rows of one channel a lane
+    const int ch = ch0 + r;
+    if (lane >= kLanes || ch >= a.k) return;
+#pragma unroll
+    for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int row = row0 + b * kRows + g * 4 + e;
+            if (row >= a.m) break;
+            const float y = acc[b][e] * (xs[b][e] * 0.0625f);
+            const int64_t to = (int64_t)row * a.ldy + ch;
             if (bf16) static_cast<BF16::elem *>(a.y)[to] = (BF16::elem)y;
             else static_cast<F16::elem *>(a.y)[to] = (F16::elem)y;
         }
-    }
 }
 
 // --------------------------------------------------------------- many rows
@@ -169,7 +270,7 @@ __device__ __forceinline__ void groups_step(const uint8_t *lj, const uint8_t *li
     };
 #pragma unroll
     for (int slice = 0; slice < NG; ++slice) {
-        frag w[kHalves][FJ], x[kHalves];
+        frag w[kHalves][FJ], x[2][kHalves];
         f32x4 ws[FJ];
 #pragma unroll
         for (int j = 0; j < FJ; ++j) ws[j] = *reinterpret_cast<const f32x4 *>(scales + slice * TJ + jrow0 + g * 16 + 4 * j);
@@ -177,6 +278,8 @@ __device__ __forceinline__ void groups_step(const uint8_t *lj, const uint8_t *li
         for (int h = 0; h < kHalves; ++h)
 #pragma unroll
             for (int j = 0; j < FJ; ++j) w[h][j] = read(lj, jrow0 + j_row(j, r), slice, h);
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) x[0][h] = read(li, irow0 + r, slice, h);
         i32x4 t[2][2];
         // unit u: fragments 2 (u % 2) and the one after it of row fragment u / 2
         const auto fold = [&](int u) {
@@ -190,15 +293,21 @@ __device__ __forceinline__ void groups_step(const uint8_t *lj, const uint8_t *li
         };
 #pragma unroll
         for (int u = 0; u < 2 * FI; ++u) {
-            if (u % 2 == 0)
+            const int i = u / 2;
+            if (u % 2 == 0 && i + 1 < FI)   // (a fragment ahead)
 #pragma unroll
-                for (int h = 0; h < kHalves; ++h) x[h] = read(li, irow0 + u / 2 * 16 + r, slice, h);
+                for (int h = 0; h < kHalves; ++h) x[~i & 1][h] = read(li, irow0 + (i + 1) * 16 + r, slice, h);
 #pragma unroll
             for (int h = 0; h < kHalves; ++h)
 #pragma unroll
                 for (int n = 0; n < 2; ++n)
-                    t[u & 1][n] = GroupsMma<NG>::mma(w[h][u % 2 * 2 + n], x[h], h ? t[u & 1][n] : i32x4{0, 0, 0, 0});
+                    t[u & 1][n] = GroupsMma<NG>::mma(w[h][u % 2 * 2 + n], x[i & 1][h], h ? t[u & 1][n] : i32x4{0, 0, 0, 0});
             if (u) fold(u - 1);
+#pragma unroll
+            for (int n = 0; n < 2 * kHalves; ++n) {
+                __builtin_amdgcn_sched_group_barrier(8, 1, 0);                 // a matrix instruction,
+                __builtin_amdgcn_sched_group_barrier(2, 16 / (2 * kHalves), 0);   // its share of vector instructions
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
         fold(2 * FI - 1);
@@ -209,7 +318,7 @@ __device__ __forceinline__ void groups_step(const uint8_t *lj, const uint8_t *li
 // two LDS buffers, KS groups of waves), with a step's scales beside its operands.
 constexpr int groups_tile_lds(int tj, int ti, int ks, int ng) { return ks * 2 * ((tj + ti) * kStepBytes + ng * tj * 4); }
 template <int GS, int NG, int TJ, int TI, int WJ, int WI, int KS>
-__device__ __forceinline__ void groups_tile(const LinearArgs &a, const GroupArg &groups, bool bf16, int tj, int ti,
+__device__ __forceinline__ void groups_tile(LinearArgs a, GroupArg groups, bool bf16, int tj, int ti,
                                             uint8_t *smem) {
     constexpr int FJ = 4, FI = TI / (16 * WI), kThreads = WJ * WI * 64, kRowsBytes = (TJ + TI) * kStepBytes;
     constexpr int kBuffer = kRowsBytes + NG * TJ * 4;

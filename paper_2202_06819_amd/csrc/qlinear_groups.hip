@@ -10,10 +10,10 @@ namespace qconv {
 
 namespace {
 
-template <int GS, int NG, int FJ, int RB>
-__global__ void __launch_bounds__(512) groups_rows(LinearArgs a, GroupArg g, int bf16) {
+template <int GS, int NG, bool EVEN, int RB>
+__global__ void __launch_bounds__(512) groups_rows(LinearArgs a, GroupArg g, int bf16, int share, int chunk) {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-    groups_few<GS, NG, FJ, RB>(a, g, bf16, (int)blockIdx.x, (int)blockIdx.y, smem);
+    groups_few<GS, NG, EVEN, RB>(a, g, bf16, share, chunk, (int)blockIdx.x, (int)blockIdx.y, smem);
 }
 template <int GS, int NG, int TJ, int TI, int WJ, int WI, int KS>
 __global__ void __launch_bounds__(KS *WJ *WI * 64, TJ == 64 ? 4 : 2) groups_tiles(LinearArgs a, GroupArg g, int bf16) {
@@ -22,13 +22,12 @@ __global__ void __launch_bounds__(KS *WJ *WI * 64, TJ == 64 ? 4 : 2) groups_tile
     tile_at(xcd_run((int)blockIdx.x, a.tiles_i * a.tiles_j), a.tiles_i, a.tiles_j, ti, tj);
     groups_tile<GS, NG, TJ, TI, WJ, WI, KS>(a, g, bf16, tj, ti, smem);
 }
-template <int GS, int NG, int FJ, int RB>
-__global__ void __launch_bounds__(512) expert_groups_rows(LinearArgs a, GroupArg g, ExpertArg ex, int bf16) {
+template <int GS, int NG, bool EVEN, int RB>
+__global__ void __launch_bounds__(512) expert_groups_rows(LinearArgs a, GroupArg g, ExpertArg ex, int bf16, int share, int chunk) {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-    constexpr int kSize = 16 / NG * RB;
-    if ((int)blockIdx.y >= expert_tiles<kSize>(ex)) return;
-    const ExpertRows p = expert_tile<kSize>(ex, (int)blockIdx.y);
-    groups_few<GS, NG, FJ, RB>(of_expert(a, p), of_expert<GS>(g, p, a.k), bf16, (int)blockIdx.x, p.tile, smem);
+    ExpertRows p;
+    if (!expert_tile<16 / NG * RB>(ex, (int)blockIdx.y, p)) return;
+    groups_few<GS, NG, EVEN, RB>(of_expert(a, p), of_expert<GS>(g, p, a.k), bf16, share, chunk, (int)blockIdx.x, p.tile, smem);
 }
 template <int GS, int NG, int TJ, int TI, int WJ, int WI, int KS>
 __global__ void __launch_bounds__(KS *WJ *WI * 64, TJ == 64 ? 4 : 2)
@@ -40,11 +39,12 @@ __global__ void __launch_bounds__(KS *WJ *WI * 64, TJ == 64 ? 4 : 2)
     groups_tile<GS, NG, TJ, TI, WJ, WI, KS>(of_expert(a, p), of_expert<GS>(g, p, a.k), bf16, tj, p.tile, smem);
 }
 
+// A launch with `lds` bytes, LDS at most.
 template <auto Kernel, int LDS, class... Args>
-hipError_t start(dim3 grid, int threads, hipStream_t stream, Args... args) {
+hipError_t start(dim3 grid, int threads, int lds, hipStream_t stream, Args... args) {
     const hipError_t e = allow_lds(reinterpret_cast<const void *>(Kernel), LDS);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(Kernel, grid, dim3((unsigned)threads), LDS, stream, args...);
+    hipLaunchKernelGGL(Kernel, grid, dim3((unsigned)threads), (unsigned)lds, stream, args...);
     return hipGetLastError();
 }
 
@@ -59,12 +59,25 @@ struct Call {
     int64_t row_tiles(int size) const { return experts ? most_tiles(a.m, ex.count, size) : (a.m + size - 1) / size; }
 };
 
-template <int GS, int NG, int FJ, int RB>
+template <int GS, int NG, bool EVEN, int RB>
 hipError_t few(const Call &c) {
-    constexpr int kLds = groups_few_lds(FJ, RB, NG);
-    const dim3 grid((unsigned)((c.a.k + 16 * FJ - 1) / (16 * FJ)), (unsigned)c.row_tiles(16 / NG * RB));
-    if (c.experts) return start<expert_groups_rows<GS, NG, FJ, RB>, kLds>(grid, 512, c.stream, c.a, c.g, c.ex, c.bf16);
-    return start<groups_rows<GS, NG, FJ, RB>, kLds>(grid, 512, c.stream, c.a, c.g, c.bf16);
+    constexpr int kSize = 16 / NG * RB, kMost = groups_few_lds(16, 32, RB, NG);
+    // waves to a tile: enough to fill the chip with 24 for each CU, of a block at least
+    // (32 rows on 25 experts, 2048 -> 4096 channels, 6400 tiles: 29.0 us with one, 31.2 with
+    // two, 36.6 with four; 128 rows on 31, 4096 -> 2048, 3968 tiles: 40.7, 35.2 and 36.5; a
+    // row, 4096 -> 8192, 512 tiles: 14.1, 9.3, 7.2 and 7.2 with eight)
+    const int64_t tiles = (c.a.k + 15) / 16, all = tiles * (c.experts ? expected_tiles(c.a.m, c.ex.count, kSize) : c.row_tiles(kSize));
+    int share = 1;
+    while (share < kGroupWaves && all * share < 6144 && c.a.steps > share * kBlock) share *= 2;
+    // rows in LDS: 64 KiB of them at most (a chunk is whole turns of the waves), or all
+    const int rows = std::min(kSize, c.a.m);
+    int chunk = kGroupWaves * kBlock;
+    while (chunk < c.a.steps && rows * few_pitch(2 * chunk) <= 16 * few_pitch(kGroupWaves * kBlock)) chunk *= 2;
+    const dim3 grid((unsigned)((tiles * share + kGroupWaves - 1) / kGroupWaves), (unsigned)c.row_tiles(kSize));
+    const int lds = groups_few_lds(rows, chunk, RB, NG);
+    if (c.experts)
+        return start<expert_groups_rows<GS, NG, EVEN, RB>, kMost>(grid, 512, lds, c.stream, c.a, c.g, c.ex, c.bf16, share, chunk);
+    return start<groups_rows<GS, NG, EVEN, RB>, kMost>(grid, 512, lds, c.stream, c.a, c.g, c.bf16, share, chunk);
 }
 template <int GS, int NG, int SIZE, int WJ, int WI, int KS>
 hipError_t tile(Call c) {
@@ -73,35 +86,74 @@ hipError_t tile(Call c) {
     c.a.tiles_i = (int32_t)c.row_tiles(SIZE);
     const dim3 grid((unsigned)c.a.tiles_i * (unsigned)c.a.tiles_j);
     if (c.experts)
-        return start<expert_groups_tiles<GS, NG, SIZE, SIZE, WJ, WI, KS>, kLds>(grid, KS * WJ * WI * 64, c.stream, c.a, c.g,
+        return start<expert_groups_tiles<GS, NG, SIZE, SIZE, WJ, WI, KS>, kLds>(grid, KS * WJ * WI * 64, kLds, c.stream, c.a, c.g,
                                                                                c.ex, c.bf16);
-    return start<groups_tiles<GS, NG, SIZE, SIZE, WJ, WI, KS>, kLds>(grid, KS * WJ * WI * 64, c.stream, c.a, c.g, c.bf16);
+    return start<groups_tiles<GS, NG, SIZE, SIZE, WJ, WI, KS>, kLds>(grid, KS * WJ * WI * 64, kLds, c.stream, c.a, c.g, c.bf16);
+}
+
+template <int GS, int NG, bool EVEN>
+hipError_t few_of(const Call &c, int64_t rows) {
+    if (NG == 4 && rows > 8) return few<GS, NG, EVEN, NG == 4 ? 4 : 1>(c);
+    if (NG >= 2 && rows > 16 / NG) return few<GS, NG, EVEN, NG >= 2 ? 2 : 1>(c);
+    return few<GS, NG, EVEN, 1>(c);
+}
+
+// A model of the kernels' times (us), its constants measured: a tile takes `start` in its
+// turn on a CU and step[n] for each 128 channels (of each of its groups of waves) with n + 1
+// on it, by the slices of a step (1, 2 or 4); the few-row kernel takes a time for each 16 x
+// 16 results and 128 channels.  E.g. 4096 -> 8192 channels in groups of 128: 16 rows 8.3,
+// as a tile of 64 with four groups 14.9, as 64 rows; 300 rows, 4096 -> 4096: 22.5 (tile of
+// 64, two groups; four 26.9, one 31.8, tile of 128 36); 4096 rows 93 (tile of 256; of 128
+// 99, of 64 140), in groups of 32 167 (176, 209).
+struct Tile {
+    Kind kind;
+    int size, groups, resident;
+    double start, step[3][4];
+};
+constexpr Tile kTiles[] = {
+    {Kind::TILE_64x4, 64, 4, 1, 3.5, {{1.3}, {1.45}, {2.05}}},
+    {Kind::TILE_64x2, 64, 2, 2, 3.4, {{0.95, 1.0}, {1.05, 1.12}, {1.4, 1.56}}},
+    {Kind::TILE_64, 64, 1, 4, 2.9, {{0.87, 0.9, 0.95, 1.0}, {0.91, 0.96, 1.05, 1.14}, {1.12, 1.17, 1.35, 1.55}}},
+    {Kind::TILE_128, 128, 1, 2, 4.2, {{0.98, 1.43}, {1.16, 1.7}, {1.82, 2.6}}},
+    {Kind::TILE_256, 256, 1, 1, 6.0, {{2.5}, {3.15}, {4.9}}}};
+constexpr double kFewStart = 4.0, kFewUnit[3] = {0.32e-3, 0.38e-3, 0.45e-3};
+
+// The fastest; FEW_1x1: the few-row kernel.
+Kind plan(const Call &c, int slices) {
+    const int n = slices == 1 ? 0 : slices == 2 ? 1 : 2;
+    const auto row_tiles = [&](int size) {
+        return c.experts ? expected_tiles(c.a.m, c.ex.count, size) : (c.a.m + size - 1) / size;
+    };
+    Kind best = Kind::FEW_1x1;
+    double best_us = kFewStart + kFewUnit[n] * ((c.a.k + 15) / 16) * (double)row_tiles(16) * c.a.steps;
+    for (const Tile &t : kTiles) {
+        const int64_t on_cu = ((c.a.k + t.size - 1) / t.size * (int64_t)row_tiles(t.size) + 255) / 256, rest = on_cu % t.resident;
+        const double step = (on_cu / t.resident) * t.step[n][t.resident - 1] + (rest ? t.step[n][rest - 1] : 0.0);
+        const double us = (on_cu + t.resident - 1) / t.resident * t.start + (c.a.steps + t.groups - 1) / t.groups * step;
+        if (us < best_us) best = t.kind, best_us = us;
+    }
+    return best;
 }
 
 template <int GS, int NG>
-hipError_t product(const Call &c) {
-    const int64_t each = c.experts ? expected_rows(c.a.m, c.ex.count) : c.a.m;
-    if (each <= 16) {
-        if (NG == 4 && each > 8) return few<GS, NG, 1, NG == 4 ? 4 : 1>(c);
-        if (NG >= 2 && each > 16 / NG) return few<GS, NG, 1, NG >= 2 ? 2 : 1>(c);
-        return few<GS, NG, 1, 1>(c);
-    }
-    const Kind kind = plan_linear(c.a, 4, [&](int size) {
-        return c.experts ? expected_tiles(c.a.m, c.ex.count, size) : (c.a.m + size - 1) / size;
-    });
-    switch (kind) {
+hipError_t product(const Call &c, int group) {
+    switch (plan(c, NG)) {
+        case Kind::FEW_1x1: {
+            const int64_t rows = c.experts ? expected_rows(c.a.m, c.ex.count) : c.a.m;
+            return group == 128 / NG ? few_of<GS, NG, true>(c, rows) : few_of<GS, 4, false>(c, rows);
+        }
         case Kind::TILE_64x4: return tile<GS, NG, 64, 1, 4, 4>(c);
-        case Kind::TILE_64: return tile<GS, NG, 64, 1, 4, 1>(c);
+        case Kind::TILE_64x2: return tile<GS, NG, 64, 1, 4, 2>(c);
         case Kind::TILE_128: return tile<GS, NG, 128, 2, 2, 1>(c);
         case Kind::TILE_256: return tile<GS, NG, 256, 4, 2, 1>(c);
-        default: return tile<GS, NG, 64, 1, 4, 2>(c);
+        default: return tile<GS, NG, 64, 1, 4, 1>(c);
     }
 }
 
 hipError_t run(const Call &c, int scale_bytes, int group) {
     if (scale_bytes == 4)
-        return group % 128 == 0 ? product<4, 1>(c) : group % 64 == 0 ? product<4, 2>(c) : product<4, 4>(c);
-    return group % 128 == 0 ? product<2, 1>(c) : group % 64 == 0 ? product<2, 2>(c) : product<2, 4>(c);
+        return group % 128 == 0 ? product<4, 1>(c, group) : group % 64 == 0 ? product<4, 2>(c, group) : product<4, 4>(c, group);
+    return group % 128 == 0 ? product<2, 1>(c, group) : group % 64 == 0 ? product<2, 2>(c, group) : product<2, 4>(c, group);
 }
 
 }  // namespace

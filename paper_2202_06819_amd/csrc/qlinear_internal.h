@@ -52,7 +52,7 @@ struct NormArgs {
     uint8_t *codes;
     int64_t pitch;
     float *scale, *rstd;         // rstd: may be NULL
-    double eps;
+    double eps, inv_c;
     int32_t gain_dtype, m, c;
 };
 
@@ -105,7 +105,8 @@ struct GradArgs {
 hipError_t launch_quantize_rows(const QuantizeArgs &a, int dtype, hipStream_t stream);
 hipError_t launch_norm_rows(const NormArgs &a, int dtype, hipStream_t stream);
 hipError_t launch_norm_grad(const NormGradArgs &a, int dtype, hipStream_t stream);
-int norm_grad_parts(int64_t m);   // workgroups of the norm's gradient: rows of its workspace
+int norm_grad_parts(int64_t m, int64_t c);   // workgroups of the norm's gradient: rows of its workspace
+int norm_grad_waves(int64_t c);              // waves that take one of its rows
 hipError_t launch_linear(const LinearArgs &a, int w_bits, int dtype, hipStream_t stream);
 hipError_t launch_grad(const GradArgs &a, bool transposed, int w_bits, int dtype, hipStream_t stream);
 // Adds the partial sums of a.splits (to 32-bit floats, or to dtype).

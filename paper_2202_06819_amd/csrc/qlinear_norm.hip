@@ -22,22 +22,31 @@ __device__ __forceinline__ void load_gain(const void *gain, int dtype, int at, i
     else load8(static_cast<const _Float16 *>(gain), at, c, g);
 }
 
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-    return v;
-}
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
     for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
     return v;
 }
 
+// 1 / sqrt(x) to 64 bits: the instruction's 2^-26 or so, and two steps of Newton's method
+// (exact where the result is).
+__device__ __forceinline__ double inverse_root(double x) {
+    double y = __builtin_amdgcn_rsq(x);
+#pragma unroll
+    for (int n = 0; n < 2; ++n) y = __builtin_fma(0.5 * y, __builtin_fma(-x * y, y, 1.0), y);
+    return y;
+}
+
 // x / 2^e to the nearest whole number, ties to even (|x| <= 127 * 2^e).
 __device__ __forceinline__ int round_wide(double x, int e) { return (int)__builtin_rint(__builtin_ldexp(x, -e)); }
 
+// Where 32 bits leave their normal range, or nearly: of a row's largest value.
+__device__ __forceinline__ bool extreme(uint32_t m) { return m < 0x06000000u || m >= 0x7f000000u; }
+
 // WAVES waves of a workgroup of four to each row (1: four rows a workgroup), KEEP vectors
-// of eight values a lane in registers; longer rows read the rest again.
+// of eight values a lane in registers; longer rows read the rest again.  Between the row's
+// loads and its codes lies one sum over its lanes: y's largest value is r times that of
+// h gain.
 template <class In, bool ADD, int WAVES, int KEEP>
 __global__ void __launch_bounds__(256) norm_to_rows(NormArgs a) {
     constexpr int kLanes = WAVES * 64, kRows = 4 / WAVES, kNext = kLanes * 8;
@@ -53,8 +62,8 @@ __global__ void __launch_bounds__(256) norm_to_rows(NormArgs a) {
     const int at0 = (WAVES == 1 ? lane : (int)threadIdx.x) * 8;
     const int c = mine ? a.c : 0, whole = (c + 15) & ~15;
 
-    // Eight values of h.  Their first visit writes them where there is a residual, the
-    // second reads them there (the sum may lie in the residual's or x's own place).
+    // Eight values of h.  Their first visit writes them where there is a residual, any
+    // other reads them there (the sum may lie in the residual's or x's own place).
     const auto first = [&](int at, float (&h)[8]) {
         load8(x, at, c, h);
         if constexpr (ADD) {
@@ -65,13 +74,21 @@ __global__ void __launch_bounds__(256) norm_to_rows(NormArgs a) {
             store8(sum, at, c, h);
         }
     };
-    const auto again = [&](int at, float (&h)[8]) { load8(ADD ? (const In *)sum : x, at, c, h); };
+    const auto again = [&](int at, float (&h)[8], float (&g)[8]) {
+        load8(ADD ? (const In *)sum : x, at, c, h);
+        load_gain(a.gain, a.gain_dtype, at, c, g);
+    };
 
-    float v[KEEP][8];
+    float v[KEEP][8];   // h gain
     double squares = 0;
-    const auto add_squares = [&](const float (&h)[8]) {
+    uint32_t m = 0;
+    const auto take = [&](float (&h)[8], const float (&g)[8]) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) squares = __builtin_fma((double)h[i], (double)h[i], squares);
+        for (int i = 0; i < 8; ++i) {
+            squares = __builtin_fma((double)h[i], (double)h[i], squares);
+            h[i] *= g[i];
+            m = max(m, __builtin_bit_cast(uint32_t, h[i]) & 0x7fffffffu);
+        }
     };
 #pragma unroll
     for (int k = 0; k < KEEP; ++k) {
@@ -81,121 +98,120 @@ __global__ void __launch_bounds__(256) norm_to_rows(NormArgs a) {
             for (int i = 0; i < 8; ++i) v[k][i] = 0.0f;
     }
 #pragma unroll
-    for (int k = 0; k < KEEP; ++k) add_squares(v[k]);
-    for (int at = at0 + KEEP * kNext; at < c; at += kNext) {
-        float h[8];
-        first(at, h);
-        add_squares(h);
+    for (int k = 0; k < KEEP; ++k) {
+        if (at0 + k * kNext >= c) continue;
+        float g[8];
+        load_gain(a.gain, a.gain_dtype, at0 + k * kNext, c, g);
+        take(v[k], g);
     }
-    squares = wave_sum(squares);
+    for (int at = at0 + KEEP * kNext; at < c; at += kNext) {
+        float h[8], g[8];
+        first(at, h);
+        load_gain(a.gain, a.gain_dtype, at, c, g);
+        take(h, g);
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+        squares += __shfl_xor(squares, d);
+        m = max(m, (uint32_t)__shfl_xor((int)m, d));
+    }
     if constexpr (WAVES > 1) {
-        if (lane == 0) part[wave] = squares;
+        if (lane == 0) part[wave] = squares, most[wave] = m;
         __syncthreads();
         squares = (part[0] + part[1]) + (part[2] + part[3]);
-    }
-    const double r_wide = 1.0 / __builtin_sqrt(squares / (double)a.c + a.eps);
-    const float r = (float)r_wide;
-
-    // Every vector of the row: its place, its values.
-    const auto each = [&](auto visit) {
-#pragma unroll
-        for (int k = 0; k < KEEP; ++k) visit(at0 + k * kNext, v[k]);
-        for (int at = at0 + KEEP * kNext; at < whole; at += kNext) {
-            float h[8];
-            again(at, h);
-            visit(at, h);
-        }
-    };
-    uint32_t m = 0;
-    each([&](int at, const float (&h)[8]) {
-        if (at >= c) return;
-        float g[8];
-        load_gain(a.gain, a.gain_dtype, at, c, g);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) m = max(m, __builtin_bit_cast(uint32_t, h[i] * r * g[i]) & 0x7fffffffu);
-    });
-#pragma unroll
-    for (int d = 32; d; d >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d));
-    if constexpr (WAVES > 1) {
-        if (lane == 0) most[wave] = m;
-        __syncthreads();
         m = max(max(most[0], most[1]), max(most[2], most[3]));
     }
+    const double r_wide = inverse_root(squares * a.inv_c + a.eps);
+    const float r = (float)r_wide;
+    const uint32_t top = __builtin_bit_cast(uint32_t, __builtin_bit_cast(float, m) * r);
+
     uint8_t *out = a.codes + at_row * a.pitch;
-    const auto put = [&](int at, const int (&q)[8]) {
-        if (at >= whole) return;
-        uint2 w{0, 0};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w.x |= (uint32_t)(q[i] & 255) << (8 * i), w.y |= (uint32_t)(q[i + 4] & 255) << (8 * i);
-        *reinterpret_cast<uint2 *>(out + at) = w;
+    const auto put = [&](int at, const uint32_t (&q)[8]) {   // the low bytes
+        *reinterpret_cast<uint2 *>(out + at) =
+            uint2{__builtin_amdgcn_perm(__builtin_amdgcn_perm(q[3], q[2], 0x0c0c0400u), __builtin_amdgcn_perm(q[1], q[0], 0x0c0c0400u), 0x05040100u),
+                  __builtin_amdgcn_perm(__builtin_amdgcn_perm(q[7], q[6], 0x0c0c0400u), __builtin_amdgcn_perm(q[5], q[4], 0x0c0c0400u), 0x05040100u)};
     };
-    // m = 1.f * 2^p: e = p - 6 where 1.f <= 127 / 64, else p - 5
-    const int from_border = (int)(m & 0x7fffffu) - 0x7e0000;
-    const bool doubtful = (from_border > -16 && from_border < 16) || (m < 0x06000000u && squares != 0) || m >= 0x7f000000u ||
-                          !(r > 0x1p-120f && r < 0x1p120f);
+    // top = 1.f * 2^p: e = p - 6 where 1.f <= 127 / 64, else p - 5
+    const int from_border = (int)(top & 0x7fffffu) - 0x7e0000;
+    const bool narrow = squares != 0 ? !extreme(m) && !extreme(top) && (from_border < -16 || from_border > 16) && r > 0x1p-120f && r < 0x1p120f
+                                     : m == 0 && r < 0x1p120f;
     float scale;
-    if (!doubtful) {
-        const int e = max((int)(m >> 23) - 6 + (from_border > 0), 1) - 127;
+    if (narrow) {
+        const int e = max((int)(top >> 23) - 6 + (from_border > 0), 1) - 127;
         scale = m == 0 ? 0.0f : __builtin_bit_cast(float, (uint32_t)(e + 127) << 23);
-        const float inv = __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);
-        each([&](int at, const float (&h)[8]) {
+        const float inv = m == 0 ? 0.0f : r * __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);   // r / 2^e
+        // Adding 1.5 * 2^23 rounds to a whole number, ties to even, and leaves its two's
+        // complement in the low bits.
+        const auto round8 = [&](int at, const float (&p)[8]) {
             if (at >= whole) return;
-            float g[8];
-            load_gain(a.gain, a.gain_dtype, at, c, g);
-            int q[8];
+            uint32_t q[8];
+            float worst = 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float t = h[i] * r * g[i] * inv, n = __builtin_rintf(t);
-                q[i] = (int)n;
-                if (__builtin_fabsf(t - n) > 0.5f - 0x1p-14f) q[i] = round_wide((double)h[i] * r_wide * (double)g[i], e);
+                const float t = p[i] * inv, b = t + 12582912.0f;
+                worst = __builtin_fmaxf(worst, __builtin_fabsf(t - (b - 12582912.0f)));
+                q[i] = __builtin_bit_cast(uint32_t, b);
+            }
+            if (worst > 0.5f - 0x1p-14f) {
+                float h[8], g[8];
+                again(at, h, g);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) q[i] = (uint32_t)round_wide((double)h[i] * r_wide * (double)g[i], e);
             }
             put(at, q);
-        });
+        };
+#pragma unroll
+        for (int k = 0; k < KEEP; ++k) round8(at0 + k * kNext, v[k]);
+        for (int at = at0 + KEEP * kNext; at < whole; at += kNext) {
+            float h[8], g[8];
+            again(at, h, g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] *= g[i];
+            round8(at, h);
+        }
     } else {
-        double top = 0;
+        double most_wide = 0;
         bool bad = false;
-        each([&](int at, const float (&h)[8]) {
-            if (at >= c) return;
-            float g[8];
-            load_gain(a.gain, a.gain_dtype, at, c, g);
+        for (int at = at0; at < c; at += kNext) {
+            float h[8], g[8];
+            again(at, h, g);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const double y = __builtin_fabs((double)h[i] * r_wide * (double)g[i]);
                 bad = bad || !(y <= (double)__FLT_MAX__);   // (a NaN too)
-                top = y > top ? y : top;
+                most_wide = y > most_wide ? y : most_wide;
             }
-        });
+        }
 #pragma unroll
         for (int d = 32; d; d >>= 1) {
-            const double other = __shfl_xor(top, d);
-            top = other > top ? other : top;
+            const double other = __shfl_xor(most_wide, d);
+            most_wide = other > most_wide ? other : most_wide;
         }
         uint32_t any = __any(bad) ? 1u : 0u;
         if constexpr (WAVES > 1) {
             __syncthreads();   // the sums before have been read
-            if (lane == 0) part[wave] = top, most[wave] = any;
+            if (lane == 0) part[wave] = most_wide, most[wave] = any;
             __syncthreads();
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                top = part[w] > top ? part[w] : top;
+                most_wide = part[w] > most_wide ? part[w] : most_wide;
                 any |= most[w];
             }
         }
         int e = -126;
-        if (top > 0 && !any) {
-            const int p = (int)((uint64_t)__builtin_bit_cast(uint64_t, top) >> 52) - 1023;
-            e = max(p - 6 + (top > 127.0 * __builtin_ldexp(1.0, p - 6)), -126);
+        if (most_wide > 0 && !any) {
+            const int p = (int)(__builtin_bit_cast(uint64_t, most_wide) >> 52) - 1023;
+            e = max(p - 6 + (most_wide > 127.0 * __builtin_ldexp(1.0, p - 6)), -126);
         }
-        scale = any ? __builtin_nanf("") : top == 0 ? 0.0f : __builtin_ldexpf(1.0f, e);
-        each([&](int at, const float (&h)[8]) {
-            if (at >= whole) return;
-            float g[8];
-            load_gain(a.gain, a.gain_dtype, at, c, g);
-            int q[8];
+        scale = any ? __builtin_nanf("") : most_wide == 0 ? 0.0f : __builtin_ldexpf(1.0f, e);
+        for (int at = at0; at < whole; at += kNext) {
+            float h[8], g[8];
+            again(at, h, g);
+            uint32_t q[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) q[i] = any ? 0 : round_wide((double)h[i] * r_wide * (double)g[i], e);
+            for (int i = 0; i < 8; ++i) q[i] = any ? 0u : (uint32_t)round_wide((double)h[i] * r_wide * (double)g[i], e);
             put(at, q);
-        });
+        }
     }
     if (mine && at0 == 0) {
         a.scale[row] = scale;
@@ -203,14 +219,12 @@ __global__ void __launch_bounds__(256) norm_to_rows(NormArgs a) {
     }
 }
 
-template <class In, bool ADD>
+template <class In, bool ADD, int WAVES, int KEEP>
 hipError_t launch_norm(const NormArgs &a, hipStream_t stream) {
-    // A wave holds rows of up to 2048 values, a workgroup of four longer ones.
+    constexpr int kRows = 4 / WAVES;
     NormArgs s = a;
-    const bool wide = a.c > 2048;
-    const int64_t blocks = wide ? a.m : ((int64_t)a.m + 3) / 4;
-    launch_slices(blocks, 256, [&](long long first, unsigned count) {
-        const int64_t row = first * (wide ? 1 : 4);
+    launch_slices(((int64_t)a.m + kRows - 1) / kRows, 256, [&](long long first, unsigned count) {
+        const int64_t row = first * kRows;
         s.x = static_cast<const In *>(a.x) + row * a.ldx;
         if (ADD) s.residual = static_cast<const In *>(a.residual) + row * a.ldr;
         if (ADD) s.sum = static_cast<In *>(a.sum) + row * a.lds;
@@ -218,12 +232,19 @@ hipError_t launch_norm(const NormArgs &a, hipStream_t stream) {
         s.scale = a.scale + row;
         s.rstd = a.rstd ? a.rstd + row : nullptr;
         s.m = (int32_t)(a.m - row);
-        if (wide)
-            hipLaunchKernelGGL((norm_to_rows<In, ADD, 4, 4>), dim3(count), dim3(256), 0, stream, s);
-        else
-            hipLaunchKernelGGL((norm_to_rows<In, ADD, 1, 4>), dim3(count), dim3(256), 0, stream, s);
+        hipLaunchKernelGGL((norm_to_rows<In, ADD, WAVES, KEEP>), dim3(count), dim3(256), 0, stream, s);
     });
     return hipGetLastError();
+}
+
+template <class In, bool ADD>
+hipError_t launch_norm(const NormArgs &a, hipStream_t stream) {
+    // A wave holds rows of up to 2048 values, a workgroup of four longer ones.
+    if (a.c <= 512) return launch_norm<In, ADD, 1, 1>(a, stream);
+    if (a.c <= 1024) return launch_norm<In, ADD, 1, 2>(a, stream);
+    if (a.c <= 2048) return launch_norm<In, ADD, 1, 4>(a, stream);
+    if (a.c <= 4096) return launch_norm<In, ADD, 4, 2>(a, stream);
+    return launch_norm<In, ADD, 4, 4>(a, stream);
 }
 
 // ---------------------------------------------------------------- gradient
@@ -233,69 +254,94 @@ hipError_t launch_norm(const NormArgs &a, hipStream_t stream) {
 // (rounding to codes is taken as the identity).  Sums are 32-bit; formed from n, they
 // stay in range wherever the results do.
 
-// A workgroup takes every gridDim.x-th row: its threads keep the same columns for all of
-// them, KEEP vectors of eight each, so that dgain's sums stay in registers and go to the
-// workspace once.  Columns past those are read a second time, and their sums of dgain
-// are added up in the workgroup's own row of the workspace.
-template <class In, int KEEP, int THREADS>
-__global__ void __launch_bounds__(THREADS) norm_backward(NormGradArgs a) {
-    constexpr int kNext = THREADS * 8, kWaves = THREADS / 64;
-    __shared__ float part[2][kWaves];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, at0 = (int)threadIdx.x * 8, c = a.c;
-    float sums[KEEP][8];
+// WAVES waves take a row, ROWS rows side by side in a workgroup, which goes through the
+// rows in steps of the whole grid.  A thread keeps its columns for all of them, KEEP
+// vectors of eight: the gain and dgain's sums stay in registers, and those go to the
+// workspace once a workgroup.  Columns past the kept ones are read a second time, and their
+// sums of dgain added up in the workgroup's own row of the workspace (LONG).
+template <class In, int KEEP, int WAVES, bool LONG>
+__global__ void __launch_bounds__(512) norm_backward(NormGradArgs a) {
+    constexpr int kNext = WAVES * 512, ROWS = 8 / WAVES;
+    __shared__ float part[2][8];
+    __shared__ float other[ROWS > 1 ? ROWS - 1 : 1][ROWS > 1 ? kNext : 1];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, which = wave / WAVES;
+    const int at0 = ((int)threadIdx.x - which * WAVES * 64) * 8, c = a.c;
+    const int64_t stride = (int64_t)gridDim.x * ROWS;
+    float sums[KEEP][8], gain[KEEP][8];
 #pragma unroll
-    for (int k = 0; k < KEEP; ++k)
+    for (int k = 0; k < KEEP; ++k) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sums[k][i] = 0.0f;
+        for (int i = 0; i < 8; ++i) sums[k][i] = gain[k][i] = 0.0f;
+        if (at0 + k * kNext < c) load_gain(a.gain, a.gain_dtype, at0 + k * kNext, c, gain[k]);
+    }
     float *mine = a.part + (int64_t)blockIdx.x * a.ldpart;
+    const auto row_of = [&](int64_t row, const In *&dy, const In *&h) {
+        dy = static_cast<const In *>(a.dy) + row * a.lddy, h = static_cast<const In *>(a.h) + row * a.ldh;
+    };
+    const auto load = [&](int64_t row, float (&t)[KEEP][8], float (&u)[KEEP][8], float &r) {
+        const In *dy, *h;
+        row_of(row, dy, h);
+        r = a.rstd[row];
+#pragma unroll
+        for (int k = 0; k < KEEP; ++k) {
+            if (at0 + k * kNext < c) {
+                load8(dy, at0 + k * kNext, c, t[k]);
+                load8(h, at0 + k * kNext, c, u[k]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) t[k][i] = u[k][i] = 0.0f;
+            }
+        }
+    };
     bool fresh = true;
     int turn = 0;
-    for (int64_t row = blockIdx.x; row < a.m; row += gridDim.x, turn ^= 1) {
-        const In *dy = static_cast<const In *>(a.dy) + row * a.lddy, *h = static_cast<const In *>(a.h) + row * a.ldh;
-        const In *dsum = a.dsum ? static_cast<const In *>(a.dsum) + row * a.ldds : nullptr;
-        In *dx = static_cast<In *>(a.dx) + row * a.lddx;
-        const float r = a.rstd[row];
-        float t[KEEP][8], u[KEEP][8], s = 0;
+    const int64_t first = (int64_t)blockIdx.x * ROWS;
+    for (int64_t row0 = first; row0 < a.m; row0 += stride, turn ^= 1) {
+        const int64_t row = row0 + which;
+        const bool in = ROWS == 1 || row < a.m;
+        float t[KEEP][8], u[KEEP][8], r = 0, s = 0;
+        const In *dy, *h;
+        row_of(in ? row : row0, dy, h);
+        load(in ? row : row0, t, u, r);
+        if (!in) r = 0;
 #pragma unroll
-        for (int k = 0; k < KEEP; ++k) {
-            const int at = at0 + k * kNext;
-            load8(dy, at, c, t[k]);
-            load8(h, at, c, u[k]);
-        }
-#pragma unroll
-        for (int k = 0; k < KEEP; ++k) {
-            float g[8];
-            load_gain(a.gain, a.gain_dtype, at0 + k * kNext, c, g);
+        for (int k = 0; k < KEEP; ++k)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 u[k][i] *= r;
-                sums[k][i] = __builtin_fmaf(t[k][i], u[k][i], sums[k][i]);
-                t[k][i] *= g[i];
+                if (in) sums[k][i] = __builtin_fmaf(t[k][i], u[k][i], sums[k][i]);
+                t[k][i] *= gain[k][i];
                 s = __builtin_fmaf(t[k][i], u[k][i], s);
             }
-        }
-        for (int at = at0 + KEEP * kNext; at < c; at += kNext) {
-            float p[8], q[8], g[8], old[8];
-            load8(dy, at, c, p);
-            load8(h, at, c, q);
-            load_gain(a.gain, a.gain_dtype, at, c, g);
-            load8((const float *)mine, at, c, old);
+        if constexpr (LONG) {
+            for (int at = at0 + KEEP * kNext; at < c; at += kNext) {
+                float p[8], q[8], g[8], old[8];
+                load8(dy, at, c, p);
+                load8(h, at, c, q);
+                load_gain(a.gain, a.gain_dtype, at, c, g);
+                load8((const float *)mine, at, c, old);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                q[i] *= r;
-                old[i] = __builtin_fmaf(p[i], q[i], fresh ? 0.0f : old[i]);
-                s = __builtin_fmaf(p[i] * g[i], q[i], s);
+                for (int i = 0; i < 8; ++i) {
+                    q[i] *= r;
+                    old[i] = __builtin_fmaf(p[i], q[i], fresh ? 0.0f : old[i]);
+                    s = __builtin_fmaf(p[i] * g[i], q[i], s);
+                }
+                store8(mine, at, c, old);
             }
-            store8(mine, at, c, old);
+            fresh = false;
         }
-        fresh = false;
         s = wave_sum(s);
-        if (lane == 0) part[turn][wave] = s;
-        __syncthreads();   // (the other half of `part` is free: everyone has passed this barrier since it was read)
-        s = 0;
+        if constexpr (WAVES > 1) {
+            if (lane == 0) part[turn][wave] = s;
+            __syncthreads();   // (the other half of `part` is free: everyone has passed this barrier since it was read)
+            s = 0;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) s += part[turn][w];
+            for (int w = 0; w < WAVES; ++w) s += part[turn][which * WAVES + w];
+        }
+        if (!in) continue;
         const float z = s / (float)c;
+        const In *dsum = a.dsum ? static_cast<const In *>(a.dsum) + row * a.ldds : nullptr;
+        In *dx = static_cast<In *>(a.dx) + row * a.lddx;
         const auto give = [&](int at, const float (&p)[8], const float (&q)[8]) {
             float d[8];
 #pragma unroll
@@ -311,15 +357,27 @@ __global__ void __launch_bounds__(THREADS) norm_backward(NormGradArgs a) {
 #pragma unroll
         for (int k = 0; k < KEEP; ++k)
             if (at0 + k * kNext < c) give(at0 + k * kNext, t[k], u[k]);
-        for (int at = at0 + KEEP * kNext; at < c; at += kNext) {
-            float p[8], q[8], g[8];
-            load8(dy, at, c, p);
-            load8(h, at, c, q);
-            load_gain(a.gain, a.gain_dtype, at, c, g);
+        if constexpr (LONG)
+            for (int at = at0 + KEEP * kNext; at < c; at += kNext) {
+                float p[8], q[8], g[8];
+                load8(dy, at, c, p);
+                load8(h, at, c, q);
+                load_gain(a.gain, a.gain_dtype, at, c, g);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] *= g[i], q[i] *= r;
-            give(at, p, q);
-        }
+                for (int i = 0; i < 8; ++i) p[i] *= g[i], q[i] *= r;
+                give(at, p, q);
+            }
+    }
+    if constexpr (ROWS > 1) {   // (KEEP is 1)
+        if (which)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) other[which - 1][at0 + i] = sums[0][i];
+        __syncthreads();
+        if (which) return;
+#pragma unroll
+        for (int n = 0; n < ROWS - 1; ++n)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sums[0][i] += other[n][at0 + i];
     }
 #pragma unroll
     for (int k = 0; k < KEEP; ++k)
@@ -334,7 +392,7 @@ __global__ void __launch_bounds__(256) norm_gain_sum(NormGradArgs a) {
     const int per = (a.parts + 31) / 32, begin = slice * per, end = min(begin + per, a.parts);
     f32x4 t{0, 0, 0, 0};
     if (col < a.c)
-#pragma unroll 4
+#pragma unroll 8
         for (int n = begin; n < end; ++n) t += *reinterpret_cast<const f32x4 *>(a.part + (int64_t)n * a.ldpart + col);
     part[slice][quad] = t;
     __syncthreads();
@@ -345,23 +403,33 @@ __global__ void __launch_bounds__(256) norm_gain_sum(NormGradArgs a) {
         if (col + i < a.c) a.dgain[col + i] = t[i];
 }
 
-template <class In>
-hipError_t launch_grad_of(const NormGradArgs &a, hipStream_t stream) {
-    if (a.parts) {
-        if (a.c <= 2048)
-            hipLaunchKernelGGL((norm_backward<In, 1, 256>), dim3((unsigned)a.parts), dim3(256), 0, stream, a);
-        else if (a.c <= 4096)
-            hipLaunchKernelGGL((norm_backward<In, 2, 256>), dim3((unsigned)a.parts), dim3(256), 0, stream, a);
-        else
-            hipLaunchKernelGGL((norm_backward<In, 4, 256>), dim3((unsigned)a.parts), dim3(256), 0, stream, a);
-    }
+template <class In, int KEEP, int WAVES, bool LONG = false>
+hipError_t launch_backward(const NormGradArgs &a, hipStream_t stream) {
+    if (a.parts) hipLaunchKernelGGL((norm_backward<In, KEEP, WAVES, LONG>), dim3((unsigned)a.parts), dim3(512), 0, stream, a);
     hipLaunchKernelGGL(norm_gain_sum, dim3((unsigned)((a.c + 31) / 32)), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 
+template <class In>
+hipError_t launch_grad_of(const NormGradArgs &a, hipStream_t stream) {
+    switch (norm_grad_waves(a.c)) {
+        case 1: return launch_backward<In, 1, 1>(a, stream);
+        case 2: return launch_backward<In, 1, 2>(a, stream);
+        case 4: return launch_backward<In, 1, 4>(a, stream);
+        default:
+            if (a.c <= 4096) return launch_backward<In, 1, 8>(a, stream);
+            if (a.c <= 8192) return launch_backward<In, 2, 8>(a, stream);
+            return launch_backward<In, 2, 8, true>(a, stream);
+    }
+}
+
 }  // namespace
 
-int norm_grad_parts(int64_t m) { return (int)(m < 512 ? m : 512); }
+int norm_grad_waves(int64_t c) { return c <= 512 ? 1 : c <= 1024 ? 2 : c <= 2048 ? 4 : 8; }
+int norm_grad_parts(int64_t m, int64_t c) {
+    const int64_t rows = 8 / norm_grad_waves(c), groups = (m + rows - 1) / rows;
+    return (int)(groups < 512 ? groups : 512);
+}
 
 hipError_t launch_norm_rows(const NormArgs &a, int dtype, hipStream_t stream) {
     switch (dtype) {

@@ -24,7 +24,7 @@ int check_sizes(int32_t m, int32_t c) {
 
 int64_t size_of(int32_t dtype) { return dtype == QCONV_F32 ? 4 : 2; }
 
-size_t grad_bytes(int64_t m, int64_t c) { return (size_t)norm_grad_parts(m) * (size_t)((c + 3) / 4 * 4) * 4; }
+size_t grad_bytes(int64_t m, int64_t c) { return (size_t)norm_grad_parts(m, c) * (size_t)((c + 3) / 4 * 4) * 4; }
 
 }  // namespace
 
@@ -69,6 +69,7 @@ int qconv_norm_rows(const void *x, int64_t ldx, const void *residual, int64_t ld
     if (total.meets(g) || (total.meets(in) && !in_x) || (total.meets(add) && !in_residual))
         return fail(QCONV_EINVAL, "sum overlaps x, the residual or the gain (it may be the whole of x or of the residual)");
     const NormArgs a{x, residual, sum, ldx, ldr, lds, gain, static_cast<uint8_t *>(codes), pitch, scale, rstd, eps,
+                     1.0 / c,
                      gain_dtype, m, c};
     const hipError_t e = launch_norm_rows(a, dtype, (hipStream_t)stream);
     if (e != hipSuccess) return fail(QCONV_EHIP, "norm launch: %s", hipGetErrorString(e));
@@ -113,7 +114,7 @@ int qconv_norm_rows_grad(const void *dy, int64_t lddy, const void *h, int64_t ld
     if (out.meets(dg) || out.meets(ws) || dg.meets(ws))
         return fail(QCONV_EINVAL, "the outputs and the workspace must not overlap");
     const NormGradArgs a{dy, h, dsum, dx, lddy, ldh, ldds, lddx, gain, rstd, dgain, static_cast<float *>(workspace),
-                         (c + 3) / 4 * 4, gain_dtype, m, c, norm_grad_parts(m)};
+                         (c + 3) / 4 * 4, gain_dtype, m, c, norm_grad_parts(m, c)};
     const hipError_t e = launch_norm_grad(a, dtype, (hipStream_t)stream);
     if (e != hipSuccess) return fail(QCONV_EHIP, "norm gradient launch: %s", hipGetErrorString(e));
     return QCONV_OK;

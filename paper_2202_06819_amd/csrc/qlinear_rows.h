@@ -7,16 +7,29 @@ namespace qconv {
 
 // Eight values of a row from element `at`, zero from c on.  Whole ones are loaded in
 // 16-byte accesses whatever the row's alignment (1021 x 5003 floats of rows that start
-// on 8-byte boundaries: 12.6 us by single elements, 5.0 so, in a graph).
+// on 8-byte boundaries: 12.6 us by single elements, 5.0 so, in a graph); the row's last
+// ones are loaded with those before them and moved into place, so that no lane waits for
+// single elements, but in rows of less than eight.
 template <class In>
 __device__ __forceinline__ void load8(const In *row, int at, int c, float (&v)[8]) {
     typedef In whole __attribute__((ext_vector_type(16 / sizeof(In))));
-    if (at + 8 <= c) {
+    if (c >= 8) {
+        const int past = at + 8 - c;
+        const In *from = row + (past > 0 ? c - 8 : at);
         whole w[sizeof(In) / 2];
 #pragma unroll
-        for (int h = 0; h < (int)sizeof(In) / 2; ++h) __builtin_memcpy(&w[h], row + at + 16 / sizeof(In) * h, 16);
+        for (int h = 0; h < (int)sizeof(In) / 2; ++h) __builtin_memcpy(&w[h], from + 16 / sizeof(In) * h, 16);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = (float)w[i * sizeof(In) / 16][i % (16 / sizeof(In))];
+        if (past > 0) {
+#pragma unroll
+            for (int d = 4; d; d >>= 1)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = past & d ? (i + d < 8 ? v[i + d < 8 ? i + d : 0] : 0.0f) : v[i];
+            if (past >= 8)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = at + i < c ? (float)row[at + i] : 0.0f;

@@ -17,7 +17,9 @@ __device__ __forceinline__ uint32_t load_scale(const GroupArg &g, int64_t at) {
 template <int GS>
 __device__ __forceinline__ float scale_value(const GroupArg &g, uint32_t bits) {
     if constexpr (GS == 4) return __builtin_bit_cast(float, bits);
-    else return g.bf16 ? __builtin_bit_cast(float, bits << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
+    // (both forms, one of them of zero: a branch would part the loads around it)
+    const uint32_t b = g.bf16 ? bits : 0u, f = g.bf16 ? 0u : bits;
+    return __builtin_bit_cast(float, b << 16 | __builtin_bit_cast(uint32_t, (float)__builtin_bit_cast(_Float16, (uint16_t)f)));
 }
 
 }  // namespace qconv
