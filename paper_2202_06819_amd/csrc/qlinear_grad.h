@@ -28,18 +28,27 @@ constexpr int grad_lds(int tile, int scale_bytes = 0) {
     return kGradStages * (tile * 64 + tile * 128 + grad_scale_bytes(scale_bytes, tile));
 }
 
+// A thread's scales of groups on their way (none without groups).
+template <int N>
+struct HeldScales {
+    uint32_t q[N];
+};
+template <>
+struct HeldScales<0> {};
+
 // A power of two that brings the largest finite |scale| of a range to at most 65504 /
 // 128, the largest f16 by the largest code, and above half of that: a code of -128 stays
 // finite, and f16 products of code and scale are normal numbers for scales down to 2^-21
 // of the largest (bf16 has float's range and needs none).  Each group of THREADS threads
 // finds it for itself, in LDS of its own.
-template <class T, int THREADS, class Scales>
+template <class T, int THREADS, int UNROLL, class Scales>
 __device__ __forceinline__ void scale_window(Scales largest, int begin, int end, uint32_t *lds, float &to,
                                              float &from) {
     if constexpr (sizeof(typename T::elem) != 2 || __is_same(T, BF16)) {
         to = from = 1.0f;
     } else {
         uint32_t m = 0;
+#pragma unroll UNROLL
         for (int t = begin + (int)threadIdx.x % THREADS; t < end; t += THREADS) m = max(m, largest(t));
 #pragma unroll
         for (int d = 32; d; d >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d));
@@ -191,7 +200,7 @@ __device__ __forceinline__ void grad_product(GradArgs a, GroupArg groups, int sp
     struct Units {
         uint2 code[kCodeUnits ? kCodeUnits : 1];
         u32x4_t p[kPUnits ? kPUnits : 1];
-        uint32_t scale[kScaleUnits ? kScaleUnits : 1];
+        [[no_unique_address]] HeldScales<kScaleUnits> scales;
     };
     // The scale of row t for the columns of slot `slot` (32 each) of the tile.
     const auto group_scale = [&](int t, int slot) {
@@ -218,7 +227,7 @@ __device__ __forceinline__ void grad_product(GradArgs a, GroupArg groups, int sp
 #pragma unroll
             for (int n = 0; n < kScaleUnits; ++n) {
                 const int unit = n * kThreads + tid;
-                q.scale[n] = group_scale(min(s * 64 + (unit & 63), a.nt - 1), unit / 64 % kSlots);
+                q.scales.q[n] = group_scale(min(s * 64 + (unit & 63), a.nt - 1), unit / 64 % kSlots);
             }
         }
         if constexpr (!COPY) {
@@ -255,7 +264,7 @@ __device__ __forceinline__ void grad_product(GradArgs a, GroupArg groups, int sp
             for (int n = 0; n < kScaleUnits; ++n) {
                 const int unit = n * kThreads + tid, t = unit & 63;
                 *reinterpret_cast<float *>(buf + kCodes + kP + unit / 64 % kSlots * 256 + t * 4) =
-                    s * 64 + t < t_end ? scale_value<GS ? GS : 4>(groups, q.scale[n]) : 0.0f;
+                    s * 64 + t < t_end ? scale_value<GS ? GS : 4>(groups, q.scales.q[n]) : 0.0f;
             }
         }
         if constexpr (!COPY) {
@@ -269,6 +278,7 @@ __device__ __forceinline__ void grad_product(GradArgs a, GroupArg groups, int sp
                     v = u32x4_t{0, 0, 0, 0};
                 } else if (!narrow && at + 8 > p_count) {
                     const int past = at + 8 - p_count;   // loaded so many elements too early
+                    asm volatile("");   // a branch: few waves have such a unit (as choices: 777 rows 18.4 -> 19.5 us)
                     v = past < 8 ? __builtin_bit_cast(u32x4_t, __builtin_bit_cast(unsigned __int128, v) >> (16 * past))
                                  : u32x4_t{0, 0, 0, 0};
                 }
@@ -378,7 +388,7 @@ __device__ __forceinline__ void grad_product(GradArgs a, GroupArg groups, int sp
         }
         return m;
     };
-    scale_window<T, kThreads>(largest, begin * 64, t_end, reinterpret_cast<uint32_t *>(smem + (kStages - 1) * kStage), to,
+    scale_window<T, kThreads, GS ? 4 : 1>(largest, begin * 64, t_end, reinterpret_cast<uint32_t *>(smem + (kStages - 1) * kStage), to,
                               from);
     if constexpr (WB == 4) to *= 0.0625f;
     if constexpr (kFetches > 0) {

@@ -16,10 +16,27 @@ namespace qconv {
 namespace {
 
 // Eight gains from element `at`, of any of the three types (the branch is uniform).
+struct RawGain {
+    u32x4_t w[2];
+};
+__device__ __forceinline__ RawGain fetch_gain(const void *gain, int dtype, int at, int c) {
+    RawGain g;
+    if (dtype == QCONV_F32) {
+        const Raw8<float> q = fetch8(static_cast<const float *>(gain), at, c);
+        g.w[0] = __builtin_bit_cast(u32x4_t, q.w[0]), g.w[1] = __builtin_bit_cast(u32x4_t, q.w[1]);
+    } else {
+        g.w[0] = __builtin_bit_cast(u32x4_t, fetch8(static_cast<const _Float16 *>(gain), at, c).w[0]);
+        g.w[1] = g.w[0];
+    }
+    return g;
+}
+__device__ __forceinline__ void unpack_gain(const RawGain &q, int dtype, int at, int c, float (&g)[8]) {
+    if (dtype == QCONV_F32) unpack8(__builtin_bit_cast(Raw8<float>, q), at, c, g);
+    else if (dtype == QCONV_BF16) unpack8(__builtin_bit_cast(Raw8<__bf16>, q.w[0]), at, c, g);
+    else unpack8(__builtin_bit_cast(Raw8<_Float16>, q.w[0]), at, c, g);
+}
 __device__ __forceinline__ void load_gain(const void *gain, int dtype, int at, int c, float (&g)[8]) {
-    if (dtype == QCONV_F32) load8(static_cast<const float *>(gain), at, c, g);
-    else if (dtype == QCONV_BF16) load8(static_cast<const __bf16 *>(gain), at, c, g);
-    else load8(static_cast<const _Float16 *>(gain), at, c, g);
+    unpack_gain(fetch_gain(gain, dtype, at, c), dtype, at, c, g);
 }
 
 __device__ __forceinline__ float wave_sum(float v) {
@@ -48,7 +65,7 @@ __device__ __forceinline__ bool extreme(uint32_t m) { return m < 0x06000000u || 
 // loads and its codes lies one sum over its lanes: y's largest value is r times that of
 // h gain.
 template <class In, bool ADD, int WAVES, int KEEP>
-__global__ void __launch_bounds__(256) norm_to_rows(NormArgs a) {
+__global__ void __launch_bounds__(256, WAVES == 1 && KEEP < 4 ? 6 : 1) norm_to_rows(NormArgs a) {
     constexpr int kLanes = WAVES * 64, kRows = 4 / WAVES, kNext = kLanes * 8;
     __shared__ double part[4];
     __shared__ uint32_t most[4];
@@ -64,11 +81,21 @@ __global__ void __launch_bounds__(256) norm_to_rows(NormArgs a) {
 
     // Eight values of h.  Their first visit writes them where there is a residual, any
     // other reads them there (the sum may lie in the residual's or x's own place).
-    const auto first = [&](int at, float (&h)[8]) {
-        load8(x, at, c, h);
+    struct First {
+        Raw8<In> x, residual;
+        RawGain gain;
+    };
+    const auto fetch = [&](int at, First &q) {
+        q.x = fetch8(x, at, a.c);
+        if constexpr (ADD) q.residual = fetch8(residual, at, a.c);
+        q.gain = fetch_gain(a.gain, a.gain_dtype, at, a.c);
+    };
+    const auto first = [&](int at, const First &q, float (&h)[8], float (&g)[8]) {
+        unpack8(q.x, at, a.c, h);
+        unpack_gain(q.gain, a.gain_dtype, at, a.c, g);
         if constexpr (ADD) {
             float s[8];
-            load8(residual, at, c, s);
+            unpack8(q.residual, at, a.c, s);
 #pragma unroll
             for (int i = 0; i < 8; ++i) h[i] = (float)(In)(h[i] + s[i]);
             store8(sum, at, c, h);
@@ -90,24 +117,23 @@ __global__ void __launch_bounds__(256) norm_to_rows(NormArgs a) {
             m = max(m, __builtin_bit_cast(uint32_t, h[i]) & 0x7fffffffu);
         }
     };
+    First q[KEEP];
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k) fetch(at0 + k * kNext, q[k]);
 #pragma unroll
     for (int k = 0; k < KEEP; ++k) {
-        if (at0 + k * kNext < c) first(at0 + k * kNext, v[k]);
-        else
+        float g[8];
+        first(at0 + k * kNext, q[k], v[k], g);
+        if (!mine)
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[k][i] = 0.0f;
-    }
-#pragma unroll
-    for (int k = 0; k < KEEP; ++k) {
-        if (at0 + k * kNext >= c) continue;
-        float g[8];
-        load_gain(a.gain, a.gain_dtype, at0 + k * kNext, c, g);
         take(v[k], g);
     }
     for (int at = at0 + KEEP * kNext; at < c; at += kNext) {
+        First more;
         float h[8], g[8];
-        first(at, h);
-        load_gain(a.gain, a.gain_dtype, at, c, g);
+        fetch(at, more);
+        first(at, more, h, g);
         take(h, g);
     }
 #pragma unroll
@@ -255,70 +281,67 @@ hipError_t launch_norm(const NormArgs &a, hipStream_t stream) {
 // stay in range wherever the results do.
 
 // WAVES waves take a row, ROWS rows side by side in a workgroup, which goes through the
-// rows in steps of the whole grid.  A thread keeps its columns for all of them, KEEP
-// vectors of eight: the gain and dgain's sums stay in registers, and those go to the
-// workspace once a workgroup.  Columns past the kept ones are read a second time, and their
-// sums of dgain added up in the workgroup's own row of the workspace (LONG).
-template <class In, int KEEP, int WAVES, bool LONG>
-__global__ void __launch_bounds__(512) norm_backward(NormGradArgs a) {
-    constexpr int kNext = WAVES * 512, ROWS = 8 / WAVES;
-    __shared__ float part[2][8];
+// rows in steps of the whole grid, the next row's loads on their way.  A thread keeps its
+// eight columns for all of them: the gain and dgain's sums stay in registers, and those go
+// to the workspace once a workgroup.  Columns past the threads' own are read a second time,
+// and their sums of dgain are added up in the workgroup's row of the workspace (LONG).
+// Bound by memory: 8192 x 4096 bf16 with dsum take 59 us in all, 4.5 TB/s.
+constexpr int backward_threads(int waves) { return waves == 16 ? 1024 : 512; }
+template <class In, int WAVES, bool LONG>
+__global__ void __launch_bounds__(backward_threads(WAVES)) norm_backward(NormGradArgs a) {
+    constexpr int kNext = WAVES * 512, ROWS = backward_threads(WAVES) / 64 / WAVES;
+    __shared__ float part[2][ROWS * WAVES];
     __shared__ float other[ROWS > 1 ? ROWS - 1 : 1][ROWS > 1 ? kNext : 1];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, which = wave / WAVES;
     const int at0 = ((int)threadIdx.x - which * WAVES * 64) * 8, c = a.c;
     const int64_t stride = (int64_t)gridDim.x * ROWS;
-    float sums[KEEP][8], gain[KEEP][8];
+    float sums[8], gain[8];
+    load_gain(a.gain, a.gain_dtype, at0, c, gain);
 #pragma unroll
-    for (int k = 0; k < KEEP; ++k) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sums[k][i] = gain[k][i] = 0.0f;
-        if (at0 + k * kNext < c) load_gain(a.gain, a.gain_dtype, at0 + k * kNext, c, gain[k]);
-    }
+    for (int i = 0; i < 8; ++i) sums[i] = 0.0f;
     float *mine = a.part + (int64_t)blockIdx.x * a.ldpart;
-    const auto row_of = [&](int64_t row, const In *&dy, const In *&h) {
-        dy = static_cast<const In *>(a.dy) + row * a.lddy, h = static_cast<const In *>(a.h) + row * a.ldh;
+    struct Row {
+        Raw8<In> dy, h, dsum;
+        float r;
     };
-    const auto load = [&](int64_t row, float (&t)[KEEP][8], float (&u)[KEEP][8], float &r) {
-        const In *dy, *h;
-        row_of(row, dy, h);
-        r = a.rstd[row];
-#pragma unroll
-        for (int k = 0; k < KEEP; ++k) {
-            if (at0 + k * kNext < c) {
-                load8(dy, at0 + k * kNext, c, t[k]);
-                load8(h, at0 + k * kNext, c, u[k]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) t[k][i] = u[k][i] = 0.0f;
-            }
-        }
+    const auto fetch = [&](int64_t row, Row &q) {
+        q.r = a.rstd[row];
+        q.dy = fetch8(static_cast<const In *>(a.dy) + row * a.lddy, at0, c);
+        q.h = fetch8(static_cast<const In *>(a.h) + row * a.ldh, at0, c);
+        if (a.dsum) q.dsum = fetch8(static_cast<const In *>(a.dsum) + row * a.ldds, at0, c);
     };
     bool fresh = true;
     int turn = 0;
     const int64_t first = (int64_t)blockIdx.x * ROWS;
+    // (where none is left: the last row again, for nothing)
+    const auto row_at = [&](int64_t row0) { return min(row0 + which, (int64_t)a.m - 1); };
+    Row ahead;
+    fetch(row_at(first), ahead);
     for (int64_t row0 = first; row0 < a.m; row0 += stride, turn ^= 1) {
-        const int64_t row = row0 + which;
-        const bool in = ROWS == 1 || row < a.m;
-        float t[KEEP][8], u[KEEP][8], r = 0, s = 0;
-        const In *dy, *h;
-        row_of(in ? row : row0, dy, h);
-        load(in ? row : row0, t, u, r);
-        if (!in) r = 0;
+        const int64_t row = row_at(row0);
+        const bool in = row0 + which < a.m;
+        const Row now = ahead;
+        fetch(row_at(row0 + stride), ahead);
+        const float r = now.r;
+        float t[8], n[8], s = 0;   // dy gain and h r
+        unpack8(now.dy, at0, c, t);
+        unpack8(now.h, at0, c, n);
 #pragma unroll
-        for (int k = 0; k < KEEP; ++k)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                u[k][i] *= r;
-                if (in) sums[k][i] = __builtin_fmaf(t[k][i], u[k][i], sums[k][i]);
-                t[k][i] *= gain[k][i];
-                s = __builtin_fmaf(t[k][i], u[k][i], s);
-            }
+        for (int i = 0; i < 8; ++i) {
+            n[i] *= r;
+            if (in) sums[i] = __builtin_fmaf(t[i], n[i], sums[i]);
+            t[i] *= gain[i];
+            s = __builtin_fmaf(t[i], n[i], s);
+        }
+        const auto load = [&](int at, float (&dy)[8], float (&h)[8], float (&g)[8]) {
+            load8(static_cast<const In *>(a.dy) + row * a.lddy, at, c, dy);
+            load8(static_cast<const In *>(a.h) + row * a.ldh, at, c, h);
+            load_gain(a.gain, a.gain_dtype, at, c, g);
+        };
         if constexpr (LONG) {
-            for (int at = at0 + KEEP * kNext; at < c; at += kNext) {
+            for (int at = at0 + kNext; at < c; at += kNext) {
                 float p[8], q[8], g[8], old[8];
-                load8(dy, at, c, p);
-                load8(h, at, c, q);
-                load_gain(a.gain, a.gain_dtype, at, c, g);
+                load(at, p, q, g);
                 load8((const float *)mine, at, c, old);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -340,48 +363,42 @@ __global__ void __launch_bounds__(512) norm_backward(NormGradArgs a) {
         }
         if (!in) continue;
         const float z = s / (float)c;
-        const In *dsum = a.dsum ? static_cast<const In *>(a.dsum) + row * a.ldds : nullptr;
-        In *dx = static_cast<In *>(a.dx) + row * a.lddx;
-        const auto give = [&](int at, const float (&p)[8], const float (&q)[8]) {
+        const auto give = [&](int at, const float (&p)[8], const float (&q)[8], const Raw8<In> &add) {
             float d[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) d[i] = r * __builtin_fmaf(-q[i], z, p[i]);
-            if (dsum) {
+            if (a.dsum) {
                 float more[8];
-                load8(dsum, at, c, more);
+                unpack8(add, at, c, more);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) d[i] += more[i];
             }
-            store8(dx, at, c, d);
+            store8(static_cast<In *>(a.dx) + row * a.lddx, at, c, d);
         };
-#pragma unroll
-        for (int k = 0; k < KEEP; ++k)
-            if (at0 + k * kNext < c) give(at0 + k * kNext, t[k], u[k]);
+        give(at0, t, n, now.dsum);
         if constexpr (LONG)
-            for (int at = at0 + KEEP * kNext; at < c; at += kNext) {
+            for (int at = at0 + kNext; at < c; at += kNext) {
                 float p[8], q[8], g[8];
-                load8(dy, at, c, p);
-                load8(h, at, c, q);
-                load_gain(a.gain, a.gain_dtype, at, c, g);
+                load(at, p, q, g);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) p[i] *= g[i], q[i] *= r;
-                give(at, p, q);
+                Raw8<In> add{};
+                if (a.dsum) add = fetch8(static_cast<const In *>(a.dsum) + row * a.ldds, at, c);
+                give(at, p, q, add);
             }
     }
-    if constexpr (ROWS > 1) {   // (KEEP is 1)
+    if constexpr (ROWS > 1) {
         if (which)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) other[which - 1][at0 + i] = sums[0][i];
+            for (int i = 0; i < 8; ++i) other[which - 1][at0 + i] = sums[i];
         __syncthreads();
         if (which) return;
 #pragma unroll
         for (int n = 0; n < ROWS - 1; ++n)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sums[0][i] += other[n][at0 + i];
+            for (int i = 0; i < 8; ++i) sums[i] += other[n][at0 + i];
     }
-#pragma unroll
-    for (int k = 0; k < KEEP; ++k)
-        if (at0 + k * kNext < c) store8(mine, at0 + k * kNext, c, sums[k]);
+    store8(mine, at0, c, sums);
 }
 
 // dgain: the workgroups' sums added in their order, 32 columns a workgroup.
@@ -403,9 +420,10 @@ __global__ void __launch_bounds__(256) norm_gain_sum(NormGradArgs a) {
         if (col + i < a.c) a.dgain[col + i] = t[i];
 }
 
-template <class In, int KEEP, int WAVES, bool LONG = false>
+template <class In, int WAVES, bool LONG = false>
 hipError_t launch_backward(const NormGradArgs &a, hipStream_t stream) {
-    if (a.parts) hipLaunchKernelGGL((norm_backward<In, KEEP, WAVES, LONG>), dim3((unsigned)a.parts), dim3(512), 0, stream, a);
+    if (a.parts) hipLaunchKernelGGL((norm_backward<In, WAVES, LONG>), dim3((unsigned)a.parts),
+                                    dim3(backward_threads(WAVES)), 0, stream, a);
     hipLaunchKernelGGL(norm_gain_sum, dim3((unsigned)((a.c + 31) / 32)), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
@@ -413,22 +431,24 @@ hipError_t launch_backward(const NormGradArgs &a, hipStream_t stream) {
 template <class In>
 hipError_t launch_grad_of(const NormGradArgs &a, hipStream_t stream) {
     switch (norm_grad_waves(a.c)) {
-        case 1: return launch_backward<In, 1, 1>(a, stream);
-        case 2: return launch_backward<In, 1, 2>(a, stream);
-        case 4: return launch_backward<In, 1, 4>(a, stream);
-        default:
-            if (a.c <= 4096) return launch_backward<In, 1, 8>(a, stream);
-            if (a.c <= 8192) return launch_backward<In, 2, 8>(a, stream);
-            return launch_backward<In, 2, 8, true>(a, stream);
+        case 1: return launch_backward<In, 1>(a, stream);
+        case 2: return launch_backward<In, 2>(a, stream);
+        case 4: return launch_backward<In, 4>(a, stream);
+        case 8: return launch_backward<In, 8>(a, stream);
+        default: return a.c <= 8192 ? launch_backward<In, 16>(a, stream) : launch_backward<In, 16, true>(a, stream);
     }
 }
 
 }  // namespace
 
-int norm_grad_waves(int64_t c) { return c <= 512 ? 1 : c <= 1024 ? 2 : c <= 2048 ? 4 : 8; }
+int norm_grad_waves(int64_t c) { return c <= 512 ? 1 : c <= 1024 ? 2 : c <= 2048 ? 4 : c <= 4096 ? 8 : 16; }
 int norm_grad_parts(int64_t m, int64_t c) {
-    const int64_t rows = 8 / norm_grad_waves(c), groups = (m + rows - 1) / rows;
-    return (int)(groups < 512 ? groups : 512);
+    // the workgroups that the CUs hold at once (their loads a row ahead fill the memory), of
+    // four turns each at least, so that dgain's partial sums stay few beside the rows; of few
+    // rows, one turn each
+    const int64_t waves = norm_grad_waves(c), rows = waves == 16 ? 1 : 8 / waves, turns = (m + rows - 1) / rows;
+    const int64_t most = waves == 16 ? 256 : 512, parts = turns / 4 > 64 ? turns / 4 : 64;
+    return (int)(turns < parts ? turns : parts < most ? parts : most);
 }
 
 hipError_t launch_norm_rows(const NormArgs &a, int dtype, hipStream_t stream) {
