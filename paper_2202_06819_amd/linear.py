@@ -19,7 +19,20 @@ weights are rows of the same form (8-bit, or 4-bit from :func:`pack_rows4`) in
 
 :func:`linear_layer` is those calls as one differentiable function; with
 ``adapters`` the forward product serves many requests, each with its own
-low-rank adapter.  Tensors may live on any GPU: a call runs on their device's
+low-rank adapter.
+
+Around it: :func:`norm_rows` makes the 8-bit rows as the root-mean-square norm of
+a sum with the residual, and :func:`norm_rows_grad` is its gradient (both layers
+together: :func:`norm_linear_layer`); :class:`GroupRows` are 4-bit weights with a
+scale for each group of channels, for :func:`linear` and :func:`linear_grad_input`;
+:func:`linear_experts` and its gradients take rows sorted by expert, each through
+its expert's weights (:func:`experts_layer`).
+
+    x8, h, rstd = norm_rows(x, gain, residual=h)
+    y = linear(x8, pack_groups4(codes, scales, 128))
+    z = linear_experts(x8, experts8, offsets)   # rows offsets[e] .. offsets[e + 1] - 1: expert e's
+
+Tensors may live on any GPU: a call runs on their device's
 current stream, or on ``stream`` (a torch stream or a raw handle), after that
 stream's earlier work and no other's; what it allocates is that stream's memory, and
 what it reads is kept until it has run.
@@ -531,7 +544,7 @@ def linear_experts(x: Rows, w: Rows | GroupRows, offsets: torch.Tensor, *, dtype
     """Rows sorted by expert, each times its expert's k x c weights (qconv_linear_experts):
     expert e has rows ``offsets[e]`` to ``offsets[e + 1] - 1`` of x, and rows e k to
     e k + k - 1 of w.  ``offsets`` is int32 on the device and read there.  Rows of no
-    expert keep what ``out`` holds."""
+    expert keep what ``out`` holds (memory made by the call: anything)."""
     if dtype not in (torch.bfloat16, torch.float16):
         raise QConvError(EINVAL, "dtype must be torch.bfloat16 or torch.float16")
     device = x.codes.device
@@ -632,3 +645,94 @@ def linear_layer(x: torch.Tensor, w: torch.Tensor) -> torch.Tensor:
     the passes only the 8-bit rows are kept: 1 byte a value of x instead of 2."""
     y = _LinearLayer.apply(x.reshape(-1, x.shape[-1]), w)
     return y.reshape(*x.shape[:-1], w.shape[0])
+
+
+class _NormLinearLayer(torch.autograd.Function):
+    """The norm's rounding to 8 bits, and the weights', are taken as the identity in the
+    backward pass, as in :class:`_LinearLayer`."""
+
+    @staticmethod
+    def forward(ctx, x, residual, gain, w, eps):
+        ctx.set_materialize_grads(False)
+        x8, h, rstd = norm_rows(_readable(x), gain.contiguous(), eps=eps,
+                                residual=None if residual is None else _readable(residual))
+        w8 = quantize_rows(_readable(w))
+        ctx.save_for_backward(x8.codes, x8.scale, w8.codes, w8.scale, h, gain, rstd)
+        ctx.channels, ctx.w_dtype = x8.channels, w.dtype
+        y = linear(x8, w8, dtype=x.dtype)
+        return y if residual is None else (y, h)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy, dsum=None):
+        x_codes, x_scale, w_codes, w_scale, h, gain, rstd = ctx.saved_tensors
+        needs_x, needs_residual, needs_gain, needs_w, _ = ctx.needs_input_grad
+        dx = dgain = dw = None
+        if dy is None:   # y was not used
+            return *_NormLinearLayer._both(dsum, needs_x, needs_residual), None, None, None
+        dy = _readable(dy)
+        if needs_x or needs_residual or needs_gain:
+            dn = linear_grad_input(dy, Rows(w_codes, w_scale, ctx.channels))
+            dx, dgain = norm_rows_grad(dn, h, gain.contiguous(), rstd, dsum=None if dsum is None else _readable(dsum))
+        if needs_w:
+            dw = linear_grad_weight(dy, Rows(x_codes, x_scale, ctx.channels)).to(ctx.w_dtype)
+        return *_NormLinearLayer._both(dx, needs_x, needs_residual), dgain.to(gain.dtype) if needs_gain else None, dw, None
+
+    @staticmethod
+    def _both(dx, needs_x, needs_residual):
+        """The gradient of x and of the residual: tensors of their own, since either may
+        become a leaf's and be changed in place."""
+        if dx is None or not (needs_x and needs_residual):
+            return dx if needs_x else None, dx if needs_residual else None
+        return dx, dx.clone()
+
+
+def norm_linear_layer(x: torch.Tensor, gain: torch.Tensor, w: torch.Tensor, *, residual: torch.Tensor | None = None,
+                      eps: float = 1e-6) -> tuple[torch.Tensor, torch.Tensor]:
+    """The root-mean-square norm of x plus the residual (... x c, bfloat16 or float16)
+    times the k x c weights' transpose, through 8-bit rows, and that sum, the next
+    residual: differentiable in x, the residual, the gain and the weights.  Between the
+    passes the sum and the 8-bit rows are kept."""
+    if residual is not None and (residual.shape != x.shape or residual.dtype is not x.dtype):
+        raise QConvError(EINVAL, "residual must be of x's shape and type")
+    c = x.shape[-1]
+    flat = x.reshape(-1, c)
+    if residual is None:
+        y, total = _NormLinearLayer.apply(flat, None, gain, w, eps), flat
+    else:
+        y, total = _NormLinearLayer.apply(flat, residual.reshape(-1, c), gain, w, eps)
+    return y.reshape(*x.shape[:-1], w.shape[0]), total.reshape(x.shape)
+
+
+class _ExpertsLayer(torch.autograd.Function):
+    """As :class:`_LinearLayer`; rows of no expert give zeros, and get a gradient of zero."""
+
+    @staticmethod
+    def forward(ctx, x, w, offsets):
+        experts, k, c = w.shape
+        x8, w8 = quantize_rows(_readable(x)), quantize_rows(_readable(w.reshape(experts * k, c)))
+        ctx.save_for_backward(x8.codes, x8.scale, w8.codes, w8.scale, offsets)
+        ctx.channels, ctx.w_dtype = c, w.dtype
+        return linear_experts(x8, w8, offsets, dtype=x.dtype, out=x.new_zeros((x.shape[0], k)))
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x_codes, x_scale, w_codes, w_scale, offsets = ctx.saved_tensors
+        dy = _readable(dy)
+        dx = dw = None
+        if ctx.needs_input_grad[0]:
+            dx = linear_experts_grad_input(dy, Rows(w_codes, w_scale, ctx.channels), offsets,
+                                           out=dy.new_zeros((dy.shape[0], ctx.channels)))
+        if ctx.needs_input_grad[1]:
+            dw = linear_experts_grad_weight(dy, Rows(x_codes, x_scale, ctx.channels), offsets).to(ctx.w_dtype)
+        return dx, dw, None
+
+
+def experts_layer(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor) -> torch.Tensor:
+    """Rows sorted by expert (m x c, bfloat16 or float16), each times its expert's weights
+    (w: experts x k x c) through 8-bit rows: differentiable in both.  ``offsets`` as of
+    :func:`linear_experts`."""
+    if w.dim() != 3 or offsets.dim() != 1 or offsets.shape[0] != w.shape[0] + 1:
+        raise QConvError(EINVAL, "w must be experts x k x c, and offsets hold one number more than experts")
+    return _ExpertsLayer.apply(x, w, offsets)
