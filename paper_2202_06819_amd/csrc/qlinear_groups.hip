@@ -1,6 +1,7 @@
 // Launches of the projection by 4-bit weights with scales of groups of channels, dense
 // and of experts.
 #include <algorithm>
+#include <cmath>
 
 #include "qlinear_experts.h"
 #include "qlinear_groups.h"
@@ -126,6 +127,7 @@ Kind plan(const Call &c, int slices) {
     };
     Kind best = Kind::FEW_1x1;
     double best_us = kFewStart + kFewUnit[n] * ((c.a.k + 15) / 16) * (double)row_tiles(16) * c.a.steps;
+    if (c.row_tiles(16) > 65535) best_us = INFINITY;   // (a grid's second axis)
     for (const Tile &t : kTiles) {
         const int64_t on_cu = ((c.a.k + t.size - 1) / t.size * (int64_t)row_tiles(t.size) + 255) / 256, rest = on_cu % t.resident;
         const double step = (on_cu / t.resident) * t.step[n][t.resident - 1] + (rest ? t.step[n][rest - 1] : 0.0);

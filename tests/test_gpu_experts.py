@@ -12,6 +12,8 @@ import math
 import pytest
 import torch
 
+import around_sizes as sizes
+
 pytestmark = pytest.mark.gpu
 
 HALF_ULP = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
@@ -47,7 +49,7 @@ def _weights(L, g, k, c, bits=4, group=0, scales=torch.float32):
         return rows, rows.codes[:, :c]
     q = torch.randint(-8, 8, (k, c), generator=g, device="cuda").to(torch.int8)
     shape = (k, -(-c // group)) if group else (k,)
-    scale = (torch.rand(*shape, generator=g, device="cuda") * 0.02 + 0.005).to(scales)
+    scale = (torch.rand(*shape, generator=g, device="cuda") * 0.02 + 0.005).to(scales if group else torch.float32)
     return (L.pack_groups4(q, scale, group) if group else L.pack_rows4(q, scale)), q
 
 
@@ -315,3 +317,49 @@ def test_no_rows(L):
     assert L.linear_experts_grad_input(none, w, offsets).shape == (0, 64)
     dw = L.linear_experts_grad_weight(none, x, offsets)
     assert dw.shape == (2, 32, 64) and not dw.any()
+
+
+# ------------------------------------------------------------- every kernel
+
+def _dealt(m, experts):
+    """Very different shares, none for some."""
+    g = torch.Generator().manual_seed(m + experts)
+    cuts = (torch.rand(experts - 1, generator=g) ** 2 * (m + 1)).long().sort().values.tolist() if experts > 1 else []
+    return [b - a for a, b in zip([0] + cuts, cuts + [m])]
+
+
+@pytest.mark.parametrize("op,m,c,k,bits,group,scales,experts,dtype", sizes.PRODUCTS)
+def test_every_kernel(L, op, m, c, k, bits, group, scales, experts, dtype):
+    """The sizes between them launch every kernel (which another test records)."""
+    g = _gen(m + c + k + experts)
+    dtype = DTYPES[dtype]
+    counts = _dealt(m, experts) if experts else [m]
+    offsets = _offsets(counts)
+    if op != "grad_weight":
+        w, q = _weights(L, g, max(experts, 1) * k, c, bits, group, (torch.bfloat16, torch.float16, torch.float32)[scales])
+    if op != "grad_input":
+        x = _rows8(L, g, m, c)
+    if op != "forward":
+        dy = _dy(g, m, k, dtype)
+    if op == "forward":
+        got = L.linear_experts(x, w, offsets, dtype=dtype) if experts else L.linear(x, w, dtype=dtype)
+    elif op == "grad_input":
+        got = L.linear_experts_grad_input(dy, w, offsets) if experts else L.linear_grad_input(dy, w)
+    else:
+        got = L.linear_experts_grad_weight(dy, x, offsets)
+    at = 0
+    for e, n in enumerate(counts):
+        rows, mine = slice(at, at + n), slice(e * k, e * k + k)
+        at += n
+        if op == "grad_weight":
+            d, v = dy[rows].double(), x.codes[rows, :c].double() * x.scale.double()[rows, None]
+            want, size = d.t().contiguous() @ v, d.abs().t().contiguous() @ v.abs()
+            assert bool(((got[e].double() - want).abs() <= size * (HALF_ULP[dtype] * 1.01 + (n + 4) * 2.0 ** -24)).all())
+        elif n:
+            part = L.GroupRows(w.codes[mine], w.scale[mine], c, group) if group else L.Rows(w.codes[mine], w.scale[mine], c, bits)
+            if op == "forward":
+                want, size = _product(L.Rows(x.codes[rows], x.scale[rows], c), part, q[mine])
+                _near(got[rows], want, size, c // 32 + 8, dtype)
+            else:
+                want, size = _grad(dy[rows], part, q[mine], c)
+                _grad_near(got[rows], want, size, k, dtype)

@@ -10,6 +10,8 @@ import math
 import pytest
 import torch
 
+import around_sizes as sizes
+
 pytestmark = pytest.mark.gpu
 
 DTYPES = (torch.bfloat16, torch.float16, torch.float32)
@@ -262,3 +264,20 @@ def test_gradient_is_that_of_differences(L):
         move[col] = step
         slope = (value(h.double(), gain.double() + move) - value(h.double(), gain.double() - move)) / (2 * step)
         assert abs(dgain[col].item() - slope.item()) < 1e-4
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("c", sizes.NORMS)
+def test_every_kernel(L, c, residual, dtype):
+    """At and past each bound of the kernels' sizes."""
+    g = _gen(c)
+    m = 21
+    x, more = _randn(g, m, c).to(dtype), _randn(g, m, c).to(dtype) if residual else None
+    gain = 1 + 0.3 * _randn(g, c)
+    got = L.norm_rows(x, gain, residual=more, eps=1e-5)
+    h = (x.float() + more.float()).to(dtype) if residual else x
+    assert torch.equal(got.sum, h)
+    _same(got, h, gain, 1e-5)
+    dy = _randn(g, m, c).to(dtype)
+    _grad_near(L.norm_rows_grad(dy, h, gain, got.rstd, dsum=more), _grad_expected(dy, h, gain, got.rstd, more), m, c, dtype)
