@@ -119,14 +119,14 @@ constexpr Tile kTiles[] = {
     {Kind::TILE_256, 256, 1, 1, 6.0, {{2.5}, {3.15}, {4.9}}}};
 constexpr double kFewStart = 4.0, kFewUnit[3] = {0.32e-3, 0.38e-3, 0.45e-3};
 
-// The fastest; FEW_1x1: the few-row kernel.
-Kind plan(const Call &c, int slices) {
+// The fastest, and its time; FEW_1x1: the few-row kernel.
+Kind plan(const Call &c, int slices, double &best_us) {
     const int n = slices == 1 ? 0 : slices == 2 ? 1 : 2;
     const auto row_tiles = [&](int size) {
         return c.experts ? expected_tiles(c.a.m, c.ex.count, size) : (c.a.m + size - 1) / size;
     };
     Kind best = Kind::FEW_1x1;
-    double best_us = kFewStart + kFewUnit[n] * ((c.a.k + 15) / 16) * (double)row_tiles(16) * c.a.steps;
+    best_us = kFewStart + kFewUnit[n] * ((c.a.k + 15) / 16) * (double)row_tiles(16) * c.a.steps;
     if (c.row_tiles(16) > 65535) best_us = INFINITY;   // (a grid's second axis)
     for (const Tile &t : kTiles) {
         const int64_t on_cu = ((c.a.k + t.size - 1) / t.size * (int64_t)row_tiles(t.size) + 255) / 256, rest = on_cu % t.resident;
@@ -139,7 +139,26 @@ Kind plan(const Call &c, int slices) {
 
 template <int GS, int NG>
 hipError_t product(const Call &c, int group) {
-    switch (plan(c, NG)) {
+    double us;
+    const Kind kind = plan(c, NG, us);
+    // A last tile of few rows may cost a turn of all CUs: those rows by a launch of their own
+    // (1543 rows, 2824 -> 5003 channels in groups of 32: 520 tiles of 128 where 512 fit at
+    // once; 7 rows apart 82.5 us, with them 88.9).
+    if (!c.experts && kind != Kind::FEW_1x1 && c.a.m % 64 && c.a.m % 64 <= 16) {
+        Call whole = c, rest = c;
+        rest.a.m = c.a.m % 64;
+        whole.a.m -= rest.a.m;
+        double whole_us, rest_us;
+        plan(whole, NG, whole_us);
+        if (plan(rest, NG, rest_us) == Kind::FEW_1x1 && whole_us + rest_us + 2.0 < us) {
+            rest.a.x.codes += (int64_t)whole.a.m * c.a.x.pitch;
+            rest.a.x.scale += whole.a.m;
+            rest.a.y = static_cast<uint16_t *>(c.a.y) + (int64_t)whole.a.m * c.a.ldy;
+            const hipError_t e = product<GS, NG>(whole, group);
+            return e != hipSuccess ? e : product<GS, NG>(rest, group);
+        }
+    }
+    switch (kind) {
         case Kind::FEW_1x1: {
             const int64_t rows = c.experts ? expected_rows(c.a.m, c.ex.count) : c.a.m;
             return group == 128 / NG ? few_of<GS, NG, true>(c, rows) : few_of<GS, 4, false>(c, rows);

@@ -295,8 +295,10 @@ __global__ void __launch_bounds__(backward_threads(WAVES)) norm_backward(NormGra
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, which = wave / WAVES;
     const int at0 = ((int)threadIdx.x - which * WAVES * 64) * 8, c = a.c;
     const int64_t stride = (int64_t)gridDim.x * ROWS;
+    // (a wave whose columns all lie past the row's end takes part in its barriers alone)
+    const bool busy = __builtin_amdgcn_readfirstlane(at0) < c;
     float sums[8], gain[8];
-    load_gain(a.gain, a.gain_dtype, at0, c, gain);
+    if (busy) load_gain(a.gain, a.gain_dtype, at0, c, gain);
 #pragma unroll
     for (int i = 0; i < 8; ++i) sums[i] = 0.0f;
     float *mine = a.part + (int64_t)blockIdx.x * a.ldpart;
@@ -316,22 +318,24 @@ __global__ void __launch_bounds__(backward_threads(WAVES)) norm_backward(NormGra
     // (where none is left: the last row again, for nothing)
     const auto row_at = [&](int64_t row0) { return min(row0 + which, (int64_t)a.m - 1); };
     Row ahead;
-    fetch(row_at(first), ahead);
+    if (busy) fetch(row_at(first), ahead);
     for (int64_t row0 = first; row0 < a.m; row0 += stride, turn ^= 1) {
         const int64_t row = row_at(row0);
         const bool in = row0 + which < a.m;
         const Row now = ahead;
-        fetch(row_at(row0 + stride), ahead);
         const float r = now.r;
         float t[8], n[8], s = 0;   // dy gain and h r
-        unpack8(now.dy, at0, c, t);
-        unpack8(now.h, at0, c, n);
+        if (busy) {
+            fetch(row_at(row0 + stride), ahead);
+            unpack8(now.dy, at0, c, t);
+            unpack8(now.h, at0, c, n);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            n[i] *= r;
-            if (in) sums[i] = __builtin_fmaf(t[i], n[i], sums[i]);
-            t[i] *= gain[i];
-            s = __builtin_fmaf(t[i], n[i], s);
+            for (int i = 0; i < 8; ++i) {
+                n[i] *= r;
+                if (in) sums[i] = __builtin_fmaf(t[i], n[i], sums[i]);
+                t[i] *= gain[i];
+                s = __builtin_fmaf(t[i], n[i], s);
+            }
         }
         const auto load = [&](int at, float (&dy)[8], float (&h)[8], float (&g)[8]) {
             load8(static_cast<const In *>(a.dy) + row * a.lddy, at, c, dy);
@@ -353,7 +357,7 @@ __global__ void __launch_bounds__(backward_threads(WAVES)) norm_backward(NormGra
             }
             fresh = false;
         }
-        s = wave_sum(s);
+        if (busy) s = wave_sum(s);
         if constexpr (WAVES > 1) {
             if (lane == 0) part[turn][wave] = s;
             __syncthreads();   // (the other half of `part` is free: everyone has passed this barrier since it was read)
@@ -361,7 +365,7 @@ __global__ void __launch_bounds__(backward_threads(WAVES)) norm_backward(NormGra
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) s += part[turn][which * WAVES + w];
         }
-        if (!in) continue;
+        if (!in || !busy) continue;
         const float z = s / (float)c;
         const auto give = [&](int at, const float (&p)[8], const float (&q)[8], const Raw8<In> &add) {
             float d[8];
@@ -401,20 +405,25 @@ __global__ void __launch_bounds__(backward_threads(WAVES)) norm_backward(NormGra
     store8(mine, at0, c, sums);
 }
 
-// dgain: the workgroups' sums added in their order, 32 columns a workgroup.
+// dgain: the workgroups' sums, 32 columns a workgroup: 32 runs of them, added up in their
+// order, meet by halves.
 __global__ void __launch_bounds__(256) norm_gain_sum(NormGradArgs a) {
-    __shared__ f32x4 part[32][8];
-    const int quad = threadIdx.x & 7, slice = threadIdx.x >> 3;
+    __shared__ f32x4 part[4][8];
+    const int quad = threadIdx.x & 7, run = threadIdx.x >> 3, wave = threadIdx.x >> 6;
     const int col = (int)blockIdx.x * 32 + quad * 4;
-    const int per = (a.parts + 31) / 32, begin = slice * per, end = min(begin + per, a.parts);
+    const int per = (a.parts + 31) / 32, begin = run * per, end = min(begin + per, a.parts);
     f32x4 t{0, 0, 0, 0};
     if (col < a.c)
 #pragma unroll 8
         for (int n = begin; n < end; ++n) t += *reinterpret_cast<const f32x4 *>(a.part + (int64_t)n * a.ldpart + col);
-    part[slice][quad] = t;
+#pragma unroll
+    for (int d = 8; d < 64; d <<= 1)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t[i] += __shfl_xor(t[i], d);
+    if ((threadIdx.x & 63) < 8) part[wave][quad] = t;
     __syncthreads();
-    if (slice) return;
-    for (int n = 1; n < 32; ++n) t += part[n][quad];
+    if (threadIdx.x >= 8) return;
+    t = (part[0][quad] + part[1][quad]) + (part[2][quad] + part[3][quad]);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         if (col + i < a.c) a.dgain[col + i] = t[i];

@@ -284,17 +284,7 @@ def quantize_rows(x: torch.Tensor, out: Rows | None = None, stream=None) -> Rows
     _matrix(x, "x", tuple(DTYPES))
     m, c = x.shape
     device = x.device
-    if out is None:
-        pitch = rows_pitch(c)
-        codes = _empty((m, pitch), torch.int8, device, stream)
-        scale = _empty(m, torch.float32, device, stream)
-        out = Rows(codes, scale, c)
-        to = (codes.data_ptr(), pitch, scale.data_ptr())
-    else:
-        if out.bits != 8 or out.channels != c or out.codes.shape[0] != m:
-            raise QConvError(EINVAL, f"out must be 8-bit rows, {m} of {c} channels")
-        r = _rows_arg(out, "out", device)
-        to = (r.codes, r.pitch, r.scale)
+    out, to = _rows_out(out, m, c, device, stream)
     _check(_call(device, _lib().qconv_quantize_rows, x.data_ptr(), DTYPES[x.dtype], _ld(x), m, c, *to,
                  _stream(stream, device)), "qconv_quantize_rows")
     _hold(stream, x, out.codes, out.scale)
@@ -313,13 +303,16 @@ def _like(t: torch.Tensor, x: torch.Tensor, name: str) -> None:
         raise QConvError(EINVAL, f"{name}: the columns of a row must be contiguous")
 
 
-def _rows_out(out: Rows | None, m: int, c: int, device: torch.device, stream) -> Rows:
-    """8-bit rows to write: new, or the caller's after a check."""
+def _rows_out(out: Rows | None, m: int, c: int, device: torch.device, stream):
+    """8-bit rows to write, new or the caller's after a check, and what a call takes of them."""
     if out is None:
-        return Rows(_empty((m, rows_pitch(c)), torch.int8, device, stream), _empty(m, torch.float32, device, stream), c)
+        pitch = rows_pitch(c)
+        codes, scale = _empty((m, pitch), torch.int8, device, stream), _empty(m, torch.float32, device, stream)
+        return Rows(codes, scale, c), (codes.data_ptr(), pitch, scale.data_ptr())
     if out.bits != 8 or out.channels != c or out.codes.shape[0] != m:
         raise QConvError(EINVAL, f"out must be 8-bit rows, {m} of {c} channels")
-    return out
+    r = _rows_arg(out, "out", device)
+    return out, (r.codes, r.pitch, r.scale)
 
 
 def norm_rows(x: torch.Tensor, gain: torch.Tensor, *, residual: torch.Tensor | None = None, eps: float = 1e-6,
@@ -337,13 +330,11 @@ def norm_rows(x: torch.Tensor, gain: torch.Tensor, *, residual: torch.Tensor | N
         total = _on(device, sum_out, (m, c), x.dtype, "sum_out", stream)
     elif sum_out is not None:
         raise QConvError(EINVAL, "sum_out without a residual")
-    rows = _rows_out(out, m, c, device, stream)
+    rows, to = _rows_out(out, m, c, device, stream)
     rstd = _empty(m, torch.float32, device, stream)
-    to = _rows_arg(rows, "out", device)
     add = (None, 0, None, 0) if residual is None else (residual.data_ptr(), _ld(residual), total.data_ptr(), _ld(total))
     _check(_call(device, _lib().qconv_norm_rows, x.data_ptr(), _ld(x), *add, DTYPES[x.dtype], gain.data_ptr(),
-                 DTYPES[gain.dtype], float(eps), m, c, to.codes, to.pitch, to.scale, rstd.data_ptr(), _stream(stream, device)),
-           "qconv_norm_rows")
+                 DTYPES[gain.dtype], eps, m, c, *to, rstd.data_ptr(), _stream(stream, device)), "qconv_norm_rows")
     _hold(stream, x, gain, residual, rows.codes, rows.scale, sum_out)
     return Normed(rows, total, rstd)
 
@@ -351,8 +342,7 @@ def norm_rows(x: torch.Tensor, gain: torch.Tensor, *, residual: torch.Tensor | N
 def norm_grad_workspace_bytes(rows: int, channels: int) -> int:
     """Scratch of :func:`norm_rows_grad`."""
     n = _size(0)
-    _check(_lib().qconv_norm_rows_grad_workspace_bytes(int(rows), int(channels), ctypes.byref(n)),
-           "qconv_norm_rows_grad_workspace_bytes")
+    _check(_lib().qconv_norm_rows_grad_workspace_bytes(rows, channels, ctypes.byref(n)), "qconv_norm_rows_grad_workspace_bytes")
     return n.value
 
 
