@@ -54,24 +54,39 @@ __device__ __forceinline__ void groups_few(LinearArgs a, GroupArg groups, bool b
     const int slice = g * NG / 4;   // of the lane's weights, and of its results
 
     // Steps from `from` on of the rows of x into LDS, zeros past the row's end.  Waves are
-    // dealt to the rows.
+    // dealt to the rows.  meanwhile(): what else to load while the first vectors are on
+    // their way.
     const int per_row = rows >= 8 ? 1 : rows >= 4 ? 2 : rows >= 2 ? 4 : 8;
-    const auto stage = [&](int from, int count) {
-        for (int row = wave / per_row; row < rows; row += kGroupWaves / per_row) {
-            uint8_t *const to = smem + kZeros + row * few_pitch(chunk);
-            constexpr int kDeep = 4;
-            for (int v = (wave % per_row) * 64 + lane; v - lane < count * 8; v += kDeep * per_row * 64) {
-                u32x4_t q[kDeep];
+    const auto stage = [&](int from, int count, auto meanwhile) {
+        constexpr int kDeep = 4;
+        const int stride = per_row * 64, ends = count * 8;
+        u32x4_t q[kDeep];
+        const auto fetch = [&](int row, int v) {
 #pragma unroll
-                for (int e = 0; e < kDeep; ++e) {
-                    const int at = (from * 8 + v + e * per_row * 64) * 16;
-                    q[e] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(
-                        rx, (int)(at < a.x.used ? (uint32_t)row * (uint32_t)a.x.pitch + (uint32_t)at : kNowhere), 0, 0));
-                }
-#pragma unroll
-                for (int e = 0; e < kDeep; ++e)
-                    if (v + e * per_row * 64 < count * 8) *reinterpret_cast<u32x4_t *>(to + (v + e * per_row * 64) * 16) = q[e];
+            for (int e = 0; e < kDeep; ++e) {
+                const int at = (from * 8 + v + e * stride) * 16;
+                q[e] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(
+                    rx, (int)(row < rows && at < a.x.used ? (uint32_t)row * (uint32_t)a.x.pitch + (uint32_t)at : kNowhere), 0, 0));
             }
+        };
+        const auto put = [&](int row, int v) {
+#pragma unroll
+            for (int e = 0; e < kDeep; ++e)
+                if (row < rows && v + e * stride < ends)
+                    *reinterpret_cast<u32x4_t *>(smem + kZeros + row * few_pitch(chunk) + (v + e * stride) * 16) = q[e];
+        };
+        int row = wave / per_row, v = (wave % per_row) * 64 + lane;
+        fetch(row, v);
+        __builtin_amdgcn_sched_barrier(0);
+        meanwhile();
+        __builtin_amdgcn_sched_barrier(0);
+        put(row, v);
+        while (row < rows) {
+            v += kDeep * stride;
+            if (v - lane >= ends) row += kGroupWaves / per_row, v = (wave % per_row) * 64 + lane;
+            if (row >= rows) break;
+            fetch(row, v);
+            put(row, v);
         }
     };
     // (what lies past a row of weights meets zeros of x; past the last row nothing is read)
@@ -90,16 +105,18 @@ __device__ __forceinline__ void groups_few(LinearArgs a, GroupArg groups, bool b
             const int at = block * kScales;
             if (at + kScales <= held) {
                 __builtin_memcpy(q.q, scales + at * GS, kScales * GS);
-            } else {   // the row's end
-#pragma unroll
-                for (int n = 0; n < kScales * GS / 4; ++n) q.q[n] = 0;
+            } else {   // the row's end: one by one, all of them on their way at once
+                uint32_t v[kScales];
 #pragma unroll
                 for (int n = 0; n < kScales; ++n) {
                     const int from = min(at + n, held - 1);
-                    const uint32_t v = GS == 4 ? reinterpret_cast<const uint32_t *>(scales)[from]
-                                               : reinterpret_cast<const uint16_t *>(scales)[from];
-                    if (at + n < held) q.q[n * GS / 4] |= v << (GS == 2 ? n % 2 * 16 : 0);
+                    v[n] = GS == 4 ? reinterpret_cast<const uint32_t *>(scales)[from] : reinterpret_cast<const uint16_t *>(scales)[from];
                 }
+#pragma unroll
+                for (int n = 0; n < kScales * GS / 4; ++n) q.q[n] = 0;
+#pragma unroll
+                for (int n = 0; n < kScales; ++n)
+                    q.q[n * GS / 4] |= (at + n < held ? v[n] : 0u) << (GS == 2 ? n % 2 * 16 : 0);
             }
         } else {
 #pragma unroll
@@ -159,6 +176,19 @@ __device__ __forceinline__ void groups_few(LinearArgs a, GroupArg groups, bool b
         }
     };
 
+    if ((int)threadIdx.x < kZeros / 16) reinterpret_cast<u32x4_t *>(smem)[threadIdx.x] = u32x4_t{0, 0, 0, 0};
+    const int blocks = (a.steps + kBlock - 1) / kBlock, turns = (blocks + share - 1) / share;   // a wave's
+    const int chunk_turns = chunk / (kBlock * share);
+    Scales scale{};
+    stage(0, min(chunk, turns * share * kBlock), [&] {
+        if (turn < blocks) load_scales(turn, scale);
+#pragma unroll
+        for (int e = 0; e < kBlock; ++e) load(turn * kBlock + e, w[e]);
+    });
+    // (LDS alone is waited for: the weights stay on their way)
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
     const __amdgpu_buffer_rsrc_t rxs = range_of(a.x.scale + row0, (int64_t)rows * 4);
     float xs[RB][4];   // of the lane's results, wanted at the end
 #pragma unroll
@@ -166,21 +196,11 @@ __device__ __forceinline__ void groups_few(LinearArgs a, GroupArg groups, bool b
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             xs[b][e] = __builtin_bit_cast(float, (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rxs, (b * kRows + g * 4 + e) * 4, 0, 0));
-    if ((int)threadIdx.x < kZeros / 16) reinterpret_cast<u32x4_t *>(smem)[threadIdx.x] = u32x4_t{0, 0, 0, 0};
-    const int blocks = (a.steps + kBlock - 1) / kBlock, turns = (blocks + share - 1) / share;   // a wave's
-    const int chunk_turns = chunk / (kBlock * share);
-    stage(0, min(chunk, turns * share * kBlock));
-    Scales scale;
-    load_scales(turn, scale);
-#pragma unroll
-    for (int e = 0; e < kBlock; ++e) load(turn * kBlock + e, w[e]);
-    __builtin_amdgcn_sched_barrier(0);
-    __syncthreads();
     for (int n = 0, left = chunk_turns; n < turns; ++n, --left) {
         if (left == 0) {   // the next chunk
             left = chunk_turns;
             __syncthreads();
-            stage(n * share * kBlock, min(chunk, (turns - n) * share * kBlock));
+            stage(n * share * kBlock, min(chunk, (turns - n) * share * kBlock), [] {});
             __syncthreads();
         }
         const uint32_t off = (uint32_t)((chunk_turns - left) * share + turn) * (kBlock * kStepBytes);
@@ -188,8 +208,8 @@ __device__ __forceinline__ void groups_few(LinearArgs a, GroupArg groups, bool b
 #pragma unroll
         for (int b = 0; b < RB; ++b) from[b] = smem + x_at[b] + (off & moves[b]);
         const int next = (n + 1) * share + turn;
-        Scales then;
-        load_scales(next, then);
+        Scales then{};
+        if (next < blocks) load_scales(next, then);
 #pragma unroll
         for (int e = 0; e < kBlock; ++e) {
             multiply(w[e], scale_of(scale, e), from, e);

@@ -56,6 +56,8 @@ struct Call {
     bool experts;
     int bf16;
     hipStream_t stream;
+    // rows of a product, of an expert that has any
+    int64_t rows() const { return experts ? expected_rows(a.m, ex.count) : a.m; }
     // tiles of `size` rows that a launch has to have
     int64_t row_tiles(int size) const { return experts ? most_tiles(a.m, ex.count, size) : (a.m + size - 1) / size; }
 };
@@ -92,20 +94,12 @@ hipError_t tile(Call c) {
     return start<groups_tiles<GS, NG, SIZE, SIZE, WJ, WI, KS>, kLds>(grid, KS * WJ * WI * 64, kLds, c.stream, c.a, c.g, c.bf16);
 }
 
-template <int GS, int NG, bool EVEN>
-hipError_t few_of(const Call &c, int64_t rows) {
-    if (NG == 4 && rows > 8) return few<GS, NG, EVEN, NG == 4 ? 4 : 1>(c);
-    if (NG >= 2 && rows > 16 / NG) return few<GS, NG, EVEN, NG >= 2 ? 2 : 1>(c);
-    return few<GS, NG, EVEN, 1>(c);
-}
-
 // A model of the kernels' times (us), its constants measured: a tile takes `start` in its
 // turn on a CU and step[n] for each 128 channels (of each of its groups of waves) with n + 1
-// on it, by the slices of a step (1, 2 or 4); the few-row kernel takes a time for each 16 x
-// 16 results and 128 channels.  E.g. 4096 -> 8192 channels in groups of 128: 16 rows 8.3,
-// as a tile of 64 with four groups 14.9, as 64 rows; 300 rows, 4096 -> 4096: 22.5 (tile of
-// 64, two groups; four 26.9, one 31.8, tile of 128 36); 4096 rows 93 (tile of 256; of 128
-// 99, of 64 140), in groups of 32 167 (176, 209).
+// on it, by the slices of a step (1, 2 or 4).  E.g. 2048 -> 8192 channels in groups of 128:
+// 24 rows 7.0, as a tile of 64 with four groups 8.9; 64 rows 9.4 as that tile, 12.4 as rows;
+// 300 rows, 4096 -> 4096: 22.5 (tile of 64, two groups; four 26.9, one 31.8, tile of 128 36);
+// 4096 rows 93 (tile of 256; of 128 99, of 64 140), in groups of 32 167 (176, 209).
 struct Tile {
     Kind kind;
     int size, groups, resident;
@@ -117,17 +111,29 @@ constexpr Tile kTiles[] = {
     {Kind::TILE_64, 64, 1, 4, 2.9, {{0.87, 0.9, 0.95, 1.0}, {0.91, 0.96, 1.05, 1.14}, {1.12, 1.17, 1.35, 1.55}}},
     {Kind::TILE_128, 128, 1, 2, 4.2, {{0.98, 1.43}, {1.16, 1.7}, {1.82, 2.6}}},
     {Kind::TILE_256, 256, 1, 1, 6.0, {{2.5}, {3.15}, {4.9}}}};
-constexpr double kFewStart = 4.0, kFewUnit[3] = {0.32e-3, 0.38e-3, 0.45e-3};
+// Of the few-row kernel: for each 16 channels by 128 of a tile's rows, and what its blocks of
+// 16 / slices rows past the first add; but a wave's turn for each block at least, however few
+// the channels (20 rows, 128 -> 1024: 4.9 in groups of 128, 5.8 of 64, 7.9 of 32; tiles 3.7
+// to 3.9).
+constexpr double kFewStart = 3.5, kFewUnit = 0.24e-3, kFewBlock = 0.08e-3, kFewTurn = 1.0;
 
-// The fastest, and its time; FEW_1x1: the few-row kernel.
-Kind plan(const Call &c, int slices, double &best_us) {
+// Blocks of rows of a tile of the few-row kernel, for so many rows.
+int few_blocks(int slices, int64_t rows) {
+    const int64_t block = 16 / slices;
+    return slices == 1 || rows <= block ? 1 : slices == 2 || rows <= 2 * block ? 2 : 4;
+}
+
+// The fastest, and its time; FEW_1x1: the few-row kernel, of few_slices.
+Kind plan(const Call &c, int slices, int few_slices, double &best_us) {
     const int n = slices == 1 ? 0 : slices == 2 ? 1 : 2;
     const auto row_tiles = [&](int size) {
         return c.experts ? expected_tiles(c.a.m, c.ex.count, size) : (c.a.m + size - 1) / size;
     };
+    const int blocks = few_blocks(few_slices, c.rows()), few_rows = 16 / few_slices * blocks;
     Kind best = Kind::FEW_1x1;
-    best_us = kFewStart + kFewUnit[n] * ((c.a.k + 15) / 16) * (double)row_tiles(16) * c.a.steps;
-    if (c.row_tiles(16) > 65535) best_us = INFINITY;   // (a grid's second axis)
+    const double units = (double)((c.a.k + 15) / 16) * row_tiles(few_rows) * c.a.steps;
+    best_us = kFewStart + std::max((kFewUnit + kFewBlock * (blocks - 1)) * units, kFewTurn * blocks);
+    if (c.row_tiles(few_rows) > 65535) best_us = INFINITY;   // (a grid's second axis)
     for (const Tile &t : kTiles) {
         const int64_t on_cu = ((c.a.k + t.size - 1) / t.size * (int64_t)row_tiles(t.size) + 255) / 256, rest = on_cu % t.resident;
         const double step = (on_cu / t.resident) * t.step[n][t.resident - 1] + (rest ? t.step[n][rest - 1] : 0.0);
@@ -137,10 +143,22 @@ Kind plan(const Call &c, int slices, double &best_us) {
     return best;
 }
 
+template <int GS, int NG, bool EVEN>
+hipError_t few_of(const Call &c) {
+    const int blocks = few_blocks(NG, c.rows());
+    if constexpr (NG == 4)
+        if (blocks == 4) return few<GS, NG, EVEN, 4>(c);
+    if constexpr (NG >= 2)
+        if (blocks == 2) return few<GS, NG, EVEN, 2>(c);
+    return few<GS, NG, EVEN, 1>(c);
+}
+
 template <int GS, int NG>
 hipError_t product(const Call &c, int group) {
+    const bool even = group == 128 / NG;
+    const int few_slices = even ? NG : 4;
     double us;
-    const Kind kind = plan(c, NG, us);
+    const Kind kind = plan(c, NG, few_slices, us);
     // A last tile of few rows may cost a turn of all CUs: those rows by a launch of their own
     // (1543 rows, 2824 -> 5003 channels in groups of 32: 520 tiles of 128 where 512 fit at
     // once; 7 rows apart 82.5 us, with them 88.9).
@@ -149,8 +167,8 @@ hipError_t product(const Call &c, int group) {
         rest.a.m = c.a.m % 64;
         whole.a.m -= rest.a.m;
         double whole_us, rest_us;
-        plan(whole, NG, whole_us);
-        if (plan(rest, NG, rest_us) == Kind::FEW_1x1 && whole_us + rest_us + 2.0 < us) {
+        plan(whole, NG, few_slices, whole_us);
+        if (plan(rest, NG, few_slices, rest_us) == Kind::FEW_1x1 && whole_us + rest_us + 2.0 < us) {
             rest.a.x.codes += (int64_t)whole.a.m * c.a.x.pitch;
             rest.a.x.scale += whole.a.m;
             rest.a.y = static_cast<uint16_t *>(c.a.y) + (int64_t)whole.a.m * c.a.ldy;
@@ -159,10 +177,7 @@ hipError_t product(const Call &c, int group) {
         }
     }
     switch (kind) {
-        case Kind::FEW_1x1: {
-            const int64_t rows = c.experts ? expected_rows(c.a.m, c.ex.count) : c.a.m;
-            return group == 128 / NG ? few_of<GS, NG, true>(c, rows) : few_of<GS, 4, false>(c, rows);
-        }
+        case Kind::FEW_1x1: return even ? few_of<GS, NG, true>(c) : few_of<GS, 4, false>(c);
         case Kind::TILE_64x4: return tile<GS, NG, 64, 1, 4, 4>(c);
         case Kind::TILE_64x2: return tile<GS, NG, 64, 1, 4, 2>(c);
         case Kind::TILE_128: return tile<GS, NG, 128, 2, 2, 1>(c);
