@@ -51,6 +51,15 @@ hipError_t tile(LinearArgs a, const ExpertArg &ex, hipStream_t stream) {
 
 template <class T, int WB>
 hipError_t product(const LinearArgs &a, const ExpertArg &ex, hipStream_t stream) {
+    // 4-bit rows of many experts of up to 8 rows each: a wave for each 16 x 16 results, so
+    // that the weights stream (64 experts, 2048 -> 4096 channels: 32 rows 28.0 us, by the
+    // kernels below 37.7, 128 rows 43.6 and 79.4, 512 rows 62.4 and 80.3).  Fewer results
+    // than 12 waves for each CU take a share of the channels each, which those do as well
+    // or better (32 experts, 2048 -> 1024: 32 rows 11.4 and 9.5), and more rows are theirs
+    // (8 experts, 4096 -> 4096: 128 rows 22.7 and 20.2, 256 rows 33.2 and 20.9).
+    if constexpr (WB == 4)
+        if (expected_rows(a.m, ex.count) <= 8 && (a.k + 15) / 16 * expected_tiles(a.m, ex.count, 16) >= 3072)
+            return launch_expert_rows4(a, ex, __is_same(T, BF16) ? QCONV_BF16 : QCONV_F16, stream);
     switch (plan_linear(a, WB, [&](int size) { return expected_tiles(a.m, ex.count, size); })) {
         case Kind::FEW_1x1: return few<T, WB, 1, 1>(a, ex, stream);
         case Kind::FEW_2x1: return few<T, WB, 2, 1>(a, ex, stream);

@@ -27,7 +27,8 @@ namespace qconv {
 // the lanes of its own slice: a product then gives the slices' sums apart, at no cost in
 // reading weights.  A result's lane holds one channel, so that one scale serves its four
 // results.  EVEN: groups of 128 / NG channels; others are served by NG 4, whose scales are
-// loaded one by one.
+// loaded one by one.  GS 0: no groups but a scale for each row of weights, with the sum of
+// all channels exact (for experts' 4-bit rows).
 constexpr int kGroupWaves = 8, kBlock = 4;   // waves of a workgroup; steps of a block
 constexpr int kZeros = kBlock * kStepBytes;  // LDS that lanes of other slices read
 constexpr int few_pitch(int chunk) { return chunk * kStepBytes + 16; }
@@ -35,10 +36,19 @@ constexpr int groups_few_lds(int rows, int chunk, int rb, int ng) {
     const int x = rows * few_pitch(chunk), sums = kGroupWaves * rb * (64 / ng) * 16;
     return kZeros + (x > sums ? x : sums);
 }
+template <int GS>
+struct GroupsSum {
+    using type = f32x4;
+};
+template <>
+struct GroupsSum<0> {
+    using type = i32x4;
+};
 template <int GS, int NG, bool EVEN, int RB>
 __device__ __forceinline__ void groups_few(LinearArgs a, GroupArg groups, bool bf16, int share, int chunk, int tile_j,
                                            int tile_i, uint8_t *smem) {
-    static_assert(EVEN || NG == 4);
+    static_assert(GS ? EVEN || NG == 4 : EVEN && NG == 1);
+    using Sum = typename GroupsSum<GS>::type;
     constexpr int kRows = 16 / NG, kLanes = 64 / NG, kScales = kBlock * NG;   // a row's scales of a block
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int r = lane & 15, g = lane >> 4;
@@ -49,8 +59,9 @@ __device__ __forceinline__ void groups_few(LinearArgs a, GroupArg groups, bool b
                                                (int64_t)(rows - 1) * a.x.pitch + a.x.used);
     const __amdgpu_buffer_rsrc_t rw = range_of(a.w.codes + (int64_t)ch0 * a.w.pitch,
                                                (int64_t)(a.k - 1 - ch0) * a.w.pitch + a.w.used);
-    const int last = (a.c - 1) / 32, held = group_of(groups, last) + 1;   // the row's last 32 channels, its groups
-    const uint8_t *const scales = static_cast<const uint8_t *>(groups.scale) + (int64_t)min(ch0 + r, a.k - 1) * groups.pitch * GS;
+    const int channel = min(ch0 + r, a.k - 1);
+    const int last = (a.c - 1) / 32, held = GS ? group_of(groups, last) + 1 : 0;   // the row's last 32 channels, its groups
+    const uint8_t *const scales = static_cast<const uint8_t *>(groups.scale) + (int64_t)channel * groups.pitch * GS;
     const int slice = g * NG / 4;   // of the lane's weights, and of its results
 
     // Steps from `from` on of the rows of x into LDS, zeros past the row's end.  Waves are
@@ -98,10 +109,12 @@ __device__ __forceinline__ void groups_few(LinearArgs a, GroupArg groups, bool b
     // The scales of a block's slices, as they lie in memory: all of them, or (one by one)
     // the lane's own.
     struct Scales {
-        uint32_t q[EVEN ? kScales * GS / 4 : kBlock];
+        uint32_t q[EVEN ? GS ? kScales * GS / 4 : 1 : kBlock];
     };
     const auto load_scales = [&](int block, Scales &q) {
-        if constexpr (EVEN) {
+        if constexpr (GS == 0) {
+            q.q[0] = 0;
+        } else if constexpr (EVEN) {
             const int at = block * kScales;
             if (at + kScales <= held) {
                 __builtin_memcpy(q.q, scales + at * GS, kScales * GS);
@@ -122,12 +135,13 @@ __device__ __forceinline__ void groups_few(LinearArgs a, GroupArg groups, bool b
 #pragma unroll
             for (int e = 0; e < kBlock; ++e) {
                 const int unit = (block * kBlock + e) * 4 + g;
-                const uint32_t v = load_scale<GS>(groups, (int64_t)min(ch0 + r, a.k - 1) * groups.pitch + group_of(groups, min(unit, last)));
+                const uint32_t v = load_scale<GS>(groups, (int64_t)channel * groups.pitch + group_of(groups, min(unit, last)));
                 q.q[e] = unit <= last ? v : 0u;
             }
         }
     };
     const auto scale_of = [&](const Scales &q, int e) {   // of the lane's slice in step e
+        if constexpr (GS == 0) return 0.0f;
         if constexpr (!EVEN) return scale_value<GS>(groups, q.q[e]);
         // (by masks: a choice between two of an array's places would put it into memory)
         const uint32_t odd = slice & 1 ? ~0u : 0u, high = slice & 2 ? ~0u : 0u;
@@ -154,9 +168,9 @@ __device__ __forceinline__ void groups_few(LinearArgs a, GroupArg groups, bool b
         moves[b] = mine ? ~0u : 0u;
         x_at[b] = mine ? (uint32_t)(kZeros + row * few_pitch(chunk) + g * 32) : 0u;
     }
-    f32x4 acc[RB];
+    Sum acc[RB];
 #pragma unroll
-    for (int b = 0; b < RB; ++b) acc[b] = f32x4{0, 0, 0, 0};
+    for (int b = 0; b < RB; ++b) acc[b] = Sum{0, 0, 0, 0};
     const auto multiply = [&](const u32x4_t &q, float scale, const uint8_t *const (&from)[RB], int e) {
         i32x4 ww[2];
 #pragma unroll
@@ -167,12 +181,17 @@ __device__ __forceinline__ void groups_few(LinearArgs a, GroupArg groups, bool b
 #pragma unroll
         for (int b = 0; b < RB; ++b) {
             i32x4 t{0, 0, 0, 0};
+            if constexpr (GS == 0) t = acc[b];
 #pragma unroll
             for (int h = 0; h < 2; ++h)
                 t = MmaI8::mma(*reinterpret_cast<const i32x4 *>(from[b] + e * kStepBytes + h * 16), ww[h], t);
+            if constexpr (GS == 0) {
+                acc[b] = t;
+            } else {
 #pragma unroll
-            for (int n = 0; n < 4; ++n) acc[b][n] = __builtin_fmaf((float)t[n], scale, acc[b][n]);
-            asm volatile("" : "+v"(acc[b]));   // here, not where the sum is next used
+                for (int n = 0; n < 4; ++n) acc[b][n] = __builtin_fmaf((float)t[n], scale, acc[b][n]);
+                asm volatile("" : "+v"(acc[b]));   // here, not where the sum is next used
+            }
         }
     };
 
@@ -224,11 +243,11 @@ __device__ __forceinline__ void groups_few(LinearArgs a, GroupArg groups, bool b
     for (int b = 0; b < RB; ++b)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            if (NG == 4) acc[b][e] += __shfl_xor(acc[b][e], 16);
-            if (NG >= 2) acc[b][e] += __shfl_xor(acc[b][e], 32);
+            if constexpr (NG == 4) acc[b][e] += __shfl_xor(acc[b][e], 16);
+            if constexpr (NG >= 2) acc[b][e] += __shfl_xor(acc[b][e], 32);
         }
     if (share > 1) {
-        auto part = reinterpret_cast<f32x4(*)[RB][kLanes]>(smem + kZeros);
+        auto part = reinterpret_cast<Sum(*)[RB][kLanes]>(smem + kZeros);
         __syncthreads();   // everyone is done with the rows
         if (lane < kLanes)
 #pragma unroll
@@ -243,13 +262,16 @@ __device__ __forceinline__ void groups_few(LinearArgs a, GroupArg groups, bool b
     // four rows of one channel a lane
     const int ch = ch0 + r;
     if (lane >= kLanes || ch >= a.k) return;
+    float ws = 1.0f;
+    if constexpr (GS == 0) ws = a.w.scale[ch];
 #pragma unroll
     for (int b = 0; b < RB; ++b)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int row = row0 + b * kRows + g * 4 + e;
             if (row >= a.m) break;
-            const float y = acc[b][e] * (xs[b][e] * 0.0625f);
+            float y = (float)acc[b][e] * (xs[b][e] * 0.0625f);
+            if constexpr (GS == 0) y *= ws;
             const int64_t to = (int64_t)row * a.ldy + ch;
             if (bf16) static_cast<BF16::elem *>(a.y)[to] = (BF16::elem)y;
             else static_cast<F16::elem *>(a.y)[to] = (F16::elem)y;

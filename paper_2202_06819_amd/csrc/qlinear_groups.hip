@@ -78,9 +78,9 @@ hipError_t few(const Call &c) {
     while (chunk < c.a.steps && rows * few_pitch(2 * chunk) <= 16 * few_pitch(kGroupWaves * kBlock)) chunk *= 2;
     const dim3 grid((unsigned)((tiles * share + kGroupWaves - 1) / kGroupWaves), (unsigned)c.row_tiles(kSize));
     const int lds = groups_few_lds(rows, chunk, RB, NG);
-    if (c.experts)
-        return start<expert_groups_rows<GS, NG, EVEN, RB>, kMost>(grid, 512, lds, c.stream, c.a, c.g, c.ex, c.bf16, share, chunk);
-    return start<groups_rows<GS, NG, EVEN, RB>, kMost>(grid, 512, lds, c.stream, c.a, c.g, c.bf16, share, chunk);
+    if constexpr (GS > 0)
+        if (!c.experts) return start<groups_rows<GS, NG, EVEN, RB>, kMost>(grid, 512, lds, c.stream, c.a, c.g, c.bf16, share, chunk);
+    return start<expert_groups_rows<GS, NG, EVEN, RB>, kMost>(grid, 512, lds, c.stream, c.a, c.g, c.ex, c.bf16, share, chunk);
 }
 template <int GS, int NG, int SIZE, int WJ, int WI, int KS>
 hipError_t tile(Call c) {
@@ -130,8 +130,8 @@ Kind plan(const Call &c, int slices, int few_slices, double &best_us) {
         return c.experts ? expected_tiles(c.a.m, c.ex.count, size) : (c.a.m + size - 1) / size;
     };
     const int blocks = few_blocks(few_slices, c.rows()), few_rows = 16 / few_slices * blocks;
-    Kind best = Kind::FEW_1x1;
     const double units = (double)((c.a.k + 15) / 16) * row_tiles(few_rows) * c.a.steps;
+    Kind best = Kind::FEW_1x1;
     best_us = kFewStart + std::max((kFewUnit + kFewBlock * (blocks - 1)) * units, kFewTurn * blocks);
     if (c.row_tiles(few_rows) > 65535) best_us = INFINITY;   // (a grid's second axis)
     for (const Tile &t : kTiles) {
@@ -193,6 +193,10 @@ hipError_t run(const Call &c, int scale_bytes, int group) {
 }
 
 }  // namespace
+
+hipError_t launch_expert_rows4(const LinearArgs &a, const ExpertArg &ex, int dtype, hipStream_t stream) {
+    return few<0, 1, true, 1>({a, GroupArg{}, ex, true, dtype == QCONV_BF16, stream});
+}
 
 hipError_t launch_groups(const LinearArgs &a, const GroupArg &g, int scale_bytes, int group, int dtype, hipStream_t stream) {
     return run({a, g, ExpertArg{}, false, dtype == QCONV_BF16, stream}, scale_bytes, group);

@@ -116,6 +116,8 @@ hipError_t launch_grad_sum(const GradArgs &a, bool to_float, int dtype, hipStrea
 hipError_t launch_groups(const LinearArgs &a, const GroupArg &g, int scale_bytes, int group, int dtype, hipStream_t stream);
 hipError_t launch_group_grad(const GradArgs &a, const GroupArg &g, int scale_bytes, int dtype, hipStream_t stream);
 hipError_t launch_experts(const LinearArgs &a, const ExpertArg &ex, int w_bits, int dtype, hipStream_t stream);
+// 4-bit rows of weights, few rows for each of many experts.
+hipError_t launch_expert_rows4(const LinearArgs &a, const ExpertArg &ex, int dtype, hipStream_t stream);
 hipError_t launch_expert_groups(const LinearArgs &a, const GroupArg &g, const ExpertArg &ex, int scale_bytes, int group,
                                 int dtype, hipStream_t stream);
 hipError_t launch_expert_grad_input(const GradArgs &a, const GroupArg &g, const ExpertArg &ex, int w_bits, int scale_bytes,
