@@ -58,7 +58,7 @@ hipError_t product(const LinearArgs &a, const ExpertArg &ex, hipStream_t stream)
     // or better (32 experts, 2048 -> 1024: 32 rows 11.4 and 9.5), and more rows are theirs
     // (8 experts, 4096 -> 4096: 128 rows 22.7 and 20.2, 256 rows 33.2 and 20.9).
     if constexpr (WB == 4)
-        if (expected_rows(a.m, ex.count) <= 8 && (a.k + 15) / 16 * expected_tiles(a.m, ex.count, 16) >= 3072)
+        if (expected_rows(a.m, ex.count) <= 8 && (a.k + 15) / 16 * expected_tiles(a.m, ex.count, 16) >= 12 * 256)
             return launch_expert_rows4(a, ex, __is_same(T, BF16) ? QCONV_BF16 : QCONV_F16, stream);
     switch (plan_linear(a, WB, [&](int size) { return expected_tiles(a.m, ex.count, size); })) {
         case Kind::FEW_1x1: return few<T, WB, 1, 1>(a, ex, stream);
