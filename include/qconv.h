@@ -632,7 +632,10 @@ int qconv_linear_grad_weight(const void *dy, int32_t dtype, int64_t lddy, int32_
  * of codes is a whole number, exact; times its scale, in 32 bits, it is added to the sum
  * of the groups, and x's scale multiplies that.
  * qconv_linear_groups_grad_input -- qconv_linear_grad_input by such weights; workspace
- * as there (qconv_linear_grad_workspace_bytes of m, w->channels, w->rows).
+ * as there (qconv_linear_grad_workspace_bytes of m, w->channels, w->rows).  A scale is not
+ * rounded: it enters the products as the sum of two parts, which are exact for bf16 and f16
+ * scales and leave 2^-13 (bf16) or 2^-19 (f16 gradients) of a product at most for 32-bit ones
+ * (f16: of scales no more than 2^14 times smaller than the call's largest).
  * Rules, limits and errors as of qconv_linear and qconv_linear_grad_input.
  */
 typedef struct qconv_group_rows {
@@ -659,7 +662,8 @@ int qconv_linear_groups_grad_input(const void *dy, int32_t dtype, int64_t lddy, 
  * qconv_linear_experts, qconv_linear_experts_groups -- y[i] = w_e x[i] for every row i of
  *   expert e, as qconv_linear and qconv_linear_groups (y: x->rows x k).
  * qconv_linear_experts_grad_input, qconv_linear_experts_groups_grad_input --
- *   dx[i] = dy[i] w_e, as qconv_linear_grad_input, for m rows (dy: m x k, dx: m x w->channels).
+ *   dx[i] = dy[i] w_e, as qconv_linear_grad_input, for m rows (dy: m x k, dx: m x w->channels);
+ *   scales of 4-bit weights, one a row or of groups, as of qconv_linear_groups_grad_input.
  * qconv_linear_experts_grad_weight -- dw[e * k + j][c] = sum over e's rows i of dy[i][j]
  *   x[i][c], 32-bit floats (dy: x->rows x k; dw: experts * k x x->channels, all of it
  *   written: zeros for an expert without rows).

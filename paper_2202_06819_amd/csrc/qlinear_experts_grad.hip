@@ -15,7 +15,7 @@ namespace {
 // dx of the experts' rows: a tile's rows are one expert's, its sum runs over that
 // expert's output channels.
 template <class T, int WB, bool COPY, int GS, int TJ, int TI, int WJ, int WI, int KS>
-__global__ void __launch_bounds__(KS *WJ *WI * 64) experts_back_rows(GradArgs a, GroupArg g, ExpertArg ex) {
+__global__ void __launch_bounds__(KS *WJ *WI * 64, GS == 0 ? 1 : TJ == 64 ? 4 : 2) experts_back_rows(GradArgs a, GroupArg g, ExpertArg ex) {
     extern __shared__ __attribute__((aligned(16))) uint8_t all_smem[];
     ExpertRows p;
     int tj;
@@ -75,7 +75,7 @@ hipError_t rows_product(const GradArgs &a, const GroupArg &g, const ExpertArg &e
     return rows_tile<T, WB, COPY, GS, 64, 2, 2, 1>(a, g, ex, stream);
 }
 template <class T>
-hipError_t rows(GradArgs a, const GroupArg &g, const ExpertArg &ex, int w_bits, int scale_bytes, hipStream_t stream) {
+hipError_t rows(GradArgs a, GroupArg g, const ExpertArg &ex, int w_bits, int scale_bytes, hipStream_t stream) {
     const bool copies = whole_vectors(a, false);
     const GradPlan plan = plan_expert_grad(
         [&](int size) { return expected_tiles(a.ni, ex.count, size) * ((a.nj + size - 1) / size); }, (a.nt + 63) / 64);
@@ -83,8 +83,8 @@ hipError_t rows(GradArgs a, const GroupArg &g, const ExpertArg &ex, int w_bits, 
     a.steps = a.steps_per_split = plan.steps;
     if (w_bits == 8)
         return copies ? rows_product<T, 8, true, 0>(a, g, ex, plan, stream) : rows_product<T, 8, false, 0>(a, g, ex, plan, stream);
-    if (scale_bytes == 0)
-        return copies ? rows_product<T, 4, true, 0>(a, g, ex, plan, stream) : rows_product<T, 4, false, 0>(a, g, ex, plan, stream);
+    if (scale_bytes == 0)   // one scale a row: any value too, so a group of all channels
+        g = {a.b.scale, 1, 0, 0};
     if (scale_bytes == 2)
         return copies ? rows_product<T, 4, true, 2>(a, g, ex, plan, stream) : rows_product<T, 4, false, 2>(a, g, ex, plan, stream);
     return copies ? rows_product<T, 4, true, 4>(a, g, ex, plan, stream) : rows_product<T, 4, false, 4>(a, g, ex, plan, stream);

@@ -10,9 +10,17 @@
 // powers of two (as the quantiser gives them); for others it is one rounding of each
 // operand to the gradient's own precision, which adds about as much error as the result's
 // own rounding: relative to the results 0.0024 instead of 0.0017 in bf16 (4-bit weights,
-// 4096 of them summed), 0.0003 instead of 0.0002 in f16.  (What the rounding leaves, as a
-// second product, takes that away and doubles the matrix instructions: tried, 19 -> 40 us
-// for 333 rows of 2824 by 1001, 235 -> 589 for 8192 x 4096 x 4096.)  Sums are 32-bit.
+// 4096 of them summed), 0.0003 instead of 0.0002 in f16.  Sums are 32-bit.
+//
+// Scales of groups (GS) are seldom powers of two, so there a scale enters as the sum of two
+// parts: the first of as few bits as leave a 4-bit code times it exact in the 16-bit type,
+// the second what is left, and each takes a product of its own.  bf16 and f16 scales lose
+// nothing (f16 ones in a bf16 gradient: 11 bits are 5 and 5 and a sign); of 32-bit scales
+// the second product's rounding is 2^-13 of a product in bf16, 2^-19 in f16, at most.  So a
+// gradient is as far from 64 bits as 32-bit products are, at twice the matrix instructions
+// (4096 x 4096 x 4096 in bf16 189 us, 0.0017 off; with one rounded part 123 and 0.0024; 333
+// rows of 2824 by 1001 in f16 29 and 24).  Experts' 4-bit weights with one scale a row are
+// taken as one group.
 #pragma once
 
 #include "qlinear_device.h"
@@ -20,8 +28,8 @@
 
 namespace qconv {
 
-// LDS of a step's scales: one for each t, or for each t and 32 columns.
-constexpr int grad_scale_bytes(int scale_bytes, int tile) { return scale_bytes ? tile / 32 * 256 : 256; }
+// LDS of a step's scales: one for each t, or the two parts of one for each t and 32 columns.
+constexpr int grad_scale_bytes(int scale_bytes, int tile) { return scale_bytes ? tile / 32 * 512 : 256; }
 constexpr int kGradStages = 3;
 // Of a group of waves: its steps' codes, p and scales.
 constexpr int grad_lds(int tile, int scale_bytes = 0) {
@@ -111,6 +119,18 @@ __device__ __forceinline__ uint32_t scaled_pair(uint32_t w, int half, float s0, 
     return pack2<T>((float)(int8_t)(w >> (16 * half)) * s0, (float)(int8_t)(w >> (16 * half + 8)) * s1);
 }
 
+// A scale as two parts that add up to it: the nearest number of 5 (bf16) or 8 (f16) bits,
+// which a 4-bit code leaves exact in the 16-bit type, and the rest.  (One that is not
+// finite, or that would round past the largest float, has its own bits or their first ones.)
+template <class T>
+__device__ __forceinline__ void split_scale(float s, float &first, float &rest) {
+    constexpr uint32_t kHalf = __is_same(T, BF16) ? 0x40000u : 0x8000u, kKept = ~(2 * kHalf - 1);
+    const uint32_t b = __builtin_bit_cast(uint32_t, s), up = b + kHalf;
+    const bool finite = (b & 0x7f800000u) != 0x7f800000u, fits = (up & 0x7f800000u) != 0x7f800000u;
+    first = __builtin_bit_cast(float, finite ? (fits ? up : b) & kKept : b);
+    rest = finite ? s - first : 0.0f;
+}
+
 //
 // KS groups of waves deal a tile's steps out among them, each with buffers of its own,
 // and their sums meet in LDS: with few tiles a CU's waves then still hide each other's
@@ -127,6 +147,7 @@ __device__ __forceinline__ void grad_product(GradArgs a, GroupArg groups, int sp
     constexpr int kCopies = kCodeCopies + kPCopies + (GS ? 0 : 1);   // a wave's copies of a step
     constexpr int kSlots = TJ / 32, kScaleUnits = GS ? (64 * kSlots + kThreads - 1) / kThreads : 0;
     static_assert(!GS || (WB == 4 && !TRANSPOSED && FJ == 2));
+    constexpr int kParts = GS ? 2 : 1;   // of a scale: products of a fragment of codes
     using elem = typename T::elem;
     using v8 = typename T::v8;
     const int group = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kThreads);
@@ -263,8 +284,8 @@ __device__ __forceinline__ void grad_product(GradArgs a, GroupArg groups, int sp
 #pragma unroll
             for (int n = 0; n < kScaleUnits; ++n) {
                 const int unit = n * kThreads + tid, t = unit & 63;
-                *reinterpret_cast<float *>(buf + kCodes + kP + unit / 64 % kSlots * 256 + t * 4) =
-                    s * 64 + t < t_end ? scale_value<GS ? GS : 4>(groups, q.scales.q[n]) : 0.0f;
+                float *const at = reinterpret_cast<float *>(buf + kCodes + kP + unit / 64 % kSlots * 512) + t;
+                split_scale<T>(s * 64 + t < t_end ? scale_value<GS ? GS : 4>(groups, q.scales.q[n]) * to : 0.0f, at[0], at[64]);
             }
         }
         if constexpr (!COPY) {
@@ -315,19 +336,25 @@ __device__ __forceinline__ void grad_product(GradArgs a, GroupArg groups, int sp
     };
     struct Codes {
         i32x2 q[FJ];
-        f32x4 scale[2];
+        f32x4 scale[2 * kParts];
     };
     auto read_codes = [&](const uint8_t *buf, int ks) {
         Codes c;
-        const float *sc = reinterpret_cast<const float *>(buf + kCodes + kP + (GS ? (jrow0 >> 5) * 256 : 0)) + ks * 32 + g * 8;
-        c.scale[0] = *reinterpret_cast<const f32x4 *>(sc);
-        c.scale[1] = *reinterpret_cast<const f32x4 *>(sc + 4);
+        const float *sc = reinterpret_cast<const float *>(buf + kCodes + kP + (GS ? (jrow0 >> 5) * 512 : 0)) + ks * 32 + g * 8;
+#pragma unroll
+        for (int n = 0; n < 2 * kParts; ++n) c.scale[n] = *reinterpret_cast<const f32x4 *>(sc + (n >> 1) * 64 + (n & 1) * 4);
         const int t = ks * 32 + g * 8 + (r >> 1);
 #pragma unroll
         for (int f = 0; f < FJ; ++f)
             c.q[f] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
                 (lds_i32x2 *)(buf + t * TJ + ((((jrow0 >> 4) + f) ^ code_unit_of<TJ>(t)) << 4) + (r & 1) * 8));
         return c;
+    };
+    // Pair n (0..3) of a fragment's eight codes, times part `part` of their scales.
+    auto pair_of = [&](const Codes &c, int f, int n, int part) {
+        const f32x4 s = c.scale[part * 2 + (n >> 1)];
+        return scaled_pair<T>((uint32_t)c.q[f][n >> 1], n & 1, GS ? s[(n & 1) * 2] : s[(n & 1) * 2] * to,
+                              GS ? s[(n & 1) * 2 + 1] : s[(n & 1) * 2 + 1] * to);
     };
     // One half of a step from x (its codes, converted) and the first kAhead fragments
     // of p: each fragment of p is read kAhead groups of matrix instructions before its
@@ -336,33 +363,36 @@ __device__ __forceinline__ void grad_product(GradArgs a, GroupArg groups, int sp
     // own vector instructions are the only ones sure to run in the matrix
     // instructions' shadow, and the scheduler gathers them.
     constexpr int kAhead = FI < 3 ? FI : 3;
-    auto half = [&](const uint8_t *cur, int ks, const uint8_t *then, u32x4_t (&x)[FJ], v8 (&ahead)[kAhead], auto spread) {
+    auto half = [&](const uint8_t *cur, int ks, const uint8_t *then, u32x4_t (&x)[kParts * FJ], v8 (&ahead)[kAhead],
+                    auto spread) {
         v8 y[FI + kAhead];
 #pragma unroll
         for (int f = 0; f < kAhead; ++f) y[f] = ahead[f];
         const Codes c = read_codes(then, ks ^ 1);
-        u32x4_t next[FJ];
+        u32x4_t next[kParts * FJ];
 #pragma unroll
         for (int i = 0; i < FI; ++i) {
             const int f = i + kAhead;
             y[f] = f < FI ? read_p(cur, ks, f) : read_p(then, ks ^ 1, f - FI);
             spread(i);
 #pragma unroll
-            for (int j = 0; j < FJ; ++j) acc[j][i] = T::mma(__builtin_bit_cast(v8, x[j]), y[i], acc[j][i]);
-            // pairs of codes: 4 FJ of them over the groups after the first
-            constexpr int kPairs = 4 * FJ, kGroups = FI > 1 ? FI - 1 : 1, kFirst = FI > 1 ? 1 : 0;
+            for (int n = kParts * FJ - 1; n >= 0; --n) {   // (the small products first)
+                const int j = FJ - 1 - n % FJ, part = n / FJ;
+                acc[j][i] = T::mma(__builtin_bit_cast(v8, x[part * FJ + j]), y[i], acc[j][i]);
+            }
+            // pairs of codes: 4 FJ of each part over the groups after the first
+            constexpr int kPairs = 4 * FJ * kParts, kGroups = FI > 1 ? FI - 1 : 1, kFirst = FI > 1 ? 1 : 0;
 #pragma unroll
             for (int n = (i - kFirst) * kPairs / kGroups; n < (i - kFirst + 1) * kPairs / kGroups; ++n) {
                 if (n < 0 || i < kFirst) continue;
-                const int k = n >> 2, e = (n & 3) * 2;
-                next[k][n & 3] = scaled_pair<T>((uint32_t)c.q[k][e >> 2], (e >> 1) & 1, c.scale[e >> 2][e & 3] * to,
-                                                c.scale[e >> 2][(e & 3) + 1] * to);
-                asm volatile("" : "+v"(next[k][n & 3]));   // here, not where the value is next used
+                const int part = n % kParts, pair = n / kParts, k = part * FJ + (pair >> 2);
+                next[k][pair & 3] = pair_of(c, pair >> 2, pair & 3, part);
+                asm volatile("" : "+v"(next[k][pair & 3]));   // here, not where the value is next used
             }
             __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
-        for (int f = 0; f < FJ; ++f) x[f] = next[f];
+        for (int f = 0; f < kParts * FJ; ++f) x[f] = next[f];
 #pragma unroll
         for (int f = 0; f < kAhead; ++f) ahead[f] = y[FI + f];
     };
@@ -403,16 +433,14 @@ __device__ __forceinline__ void grad_product(GradArgs a, GroupArg groups, int sp
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    u32x4_t x[FJ];
+    u32x4_t x[kParts * FJ];
     v8 ahead[kAhead];
     {
         const Codes c = read_codes(smem, 0);
 #pragma unroll
-        for (int f = 0; f < FJ; ++f)
+        for (int f = 0; f < kParts * FJ; ++f)
 #pragma unroll
-            for (int n = 0; n < 4; ++n)
-                x[f][n] = scaled_pair<T>((uint32_t)c.q[f][n >> 1], n & 1, c.scale[n >> 1][(n & 1) * 2] * to,
-                                         c.scale[n >> 1][(n & 1) * 2 + 1] * to);
+            for (int n = 0; n < 4; ++n) x[f][n] = pair_of(c, f % FJ, n, f / FJ);
 #pragma unroll
         for (int f = 0; f < kAhead; ++f) ahead[f] = read_p(smem, 0, f);
     }

@@ -9,7 +9,7 @@ namespace qconv {
 namespace {
 
 template <class T, bool COPY, int GS, int TJ, int TI, int WJ, int WI, int KS>
-__global__ void __launch_bounds__(KS *WJ *WI * 64) groups_back(GradArgs a, GroupArg groups) {
+__global__ void __launch_bounds__(KS *WJ *WI * 64, TJ == 64 ? 4 : 2) groups_back(GradArgs a, GroupArg groups) {
     extern __shared__ __attribute__((aligned(16))) uint8_t all_smem[];
     const GradPlace p = grad_place(a);
     grad_product<T, 4, false, COPY, GS, TJ, TI, WJ, WI, KS>(a, groups, p.split, p.ti, p.tj, all_smem);

@@ -1,0 +1,106 @@
+"""Input gradients through frozen 4-bit weights: scales of groups of channels, and the
+weights of experts with one scale a row, of any values.
+
+Tolerances follow from the roundings alone.  A scale enters the product as two parts, the
+first of so few bits that a code times it is exact in the 16-bit type; the second is at most
+2^-5 (bf16) or 2^-8 (f16) of the scale, and a code times it is rounded once, half an ulp:
+2^-13 and 2^-19 of a product.  Twice as many products as the sum has terms are added in 32
+bits, each with an error of at most 2^-24 of the sum of their absolute values, and the
+result is rounded once, half an ulp."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+HALF_ULP = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+PARTS = {torch.bfloat16: 2.0 ** -13, torch.float16: 2.0 ** -19}
+DTYPES = (torch.bfloat16, torch.float16)
+SCALES = (torch.float16, torch.bfloat16, torch.float32)
+
+# rows, channels, outputs (of each expert), experts (0: none): tiles of 64 with one, two and
+# four groups of waves, split or not, of 128 and of 256, copied to LDS and through registers
+SIZES = [(1, 64, 33, 0), (20, 520, 5000, 0), (333, 2824, 1001, 0), (1000, 1024, 2640, 0), (130, 1000, 256, 0),
+         (2000, 2048, 1001, 0), (3000, 4104, 520, 0), (3000, 4104, 1001, 0),
+         (40, 264, 300, 3), (700, 1024, 264, 4), (4000, 1024, 264, 6), (6000, 2048, 264, 3), (6000, 2048, 261, 3)]
+
+
+@pytest.fixture(scope="module")
+def L():
+    from paper_2202_06819_amd import build, linear
+    build.ensure_built()
+    return linear
+
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _weights(L, g, k, c, group, scales):
+    """4-bit rows (group 0: one scale a row), and the whole numbers that they hold."""
+    q = torch.randint(-8, 8, (k, c), generator=g, device="cuda").to(torch.int8)
+    shape = (k, -(-c // group)) if group else (k,)
+    scale = (torch.rand(*shape, generator=g, device="cuda") * 0.02 + 0.005).to(scales)
+    return (L.pack_groups4(q, scale, group) if group else L.pack_rows4(q, scale)), q
+
+
+def _values(w, q):
+    s = w.scale.double()
+    c = q.shape[1]
+    return q.double() * (s[:, None] if s.dim() == 1 else s[:, torch.arange(c, device="cuda") // w.group])
+
+
+def _split(m, experts):
+    """The rows of each expert: unlike ones, none for the second."""
+    if not experts:
+        return [0, m]
+    first = m // (experts + 1)
+    return [0, first, first] + [first + (m - first) * (n + 1) // (experts - 2) for n in range(experts - 2)]
+
+
+def _run(L, dy, w, ends, experts, c):
+    """The gradient, into memory that holds NaN."""
+    out = torch.full((dy.shape[0], c), math.nan, dtype=dy.dtype, device="cuda")
+    if not experts:
+        return L.linear_grad_input(dy, w, out=out)
+    return L.linear_experts_grad_input(dy, w, torch.tensor(ends, dtype=torch.int32, device="cuda"), out=out)
+
+
+def _expected(dy, values, ends, k):
+    """The gradient in 64 bits, and the sums of the absolute values behind it."""
+    d = dy.double().contiguous()
+    parts = [(d[a:b], values[e * k:e * k + k]) for e, (a, b) in enumerate(zip(ends[:-1], ends[1:]))]
+    return torch.cat([a @ b for a, b in parts]), torch.cat([a.abs() @ b.abs() for a, b in parts])
+
+
+def _tolerance(want, size, k, dtype):
+    tol = size * (PARTS[dtype] + (2 * k + 4) * 2.0 ** -24)
+    return tol * (1 + HALF_ULP[dtype]) + want.abs() * HALF_ULP[dtype] + (2.0 ** -25 if dtype == torch.float16 else 1e-300)
+
+
+def _near(got, want, tol):
+    ok = (got.double() - want).abs() <= tol   # (false for a NaN)
+    assert bool(ok.all()), f"{int((~ok).sum())} of {ok.numel()} off, worst {float(((got.double() - want).abs() / tol).max()):.3g}"
+
+
+def _case(L, m, c, k, experts, group, scales, dtype):
+    g = _gen(m + c + k + group)
+    dy = torch.randn(m, k, generator=g, device="cuda").to(dtype)
+    w, q = _weights(L, g, max(experts, 1) * k, c, group, scales)
+    ends = _split(m, experts)
+    return dy, w, q, ends
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,c,k,experts", SIZES)
+def test_scales_keep_their_bits(L, m, c, k, experts, dtype):
+    """Scales of any values, in all of their bits."""
+    for n, (group, scales) in enumerate([(32, SCALES[(m + c) % 3]), (64, torch.float32), (128, torch.float16), (0, torch.float32)]):
+        if not group and not experts or n and c < 2 * group:
+            continue
+        dy, w, q, ends = _case(L, m, c, k, experts, group, scales, dtype)
+        got = _run(L, dy, w, ends, experts, c)
+        want, size = _expected(dy, _values(w, q), ends, k)
+        _near(got, want, _tolerance(want, size, k, dtype))
+        assert torch.equal(got, _run(L, dy, w, ends, experts, c))
