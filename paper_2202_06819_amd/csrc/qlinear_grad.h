@@ -19,7 +19,7 @@
 // the second product's rounding is 2^-13 of a product in bf16, 2^-19 in f16, at most.  So a
 // gradient is as far from 64 bits as 32-bit products are, at twice the matrix instructions
 // (4096 x 4096 x 4096 in bf16 189 us, 0.0017 off; with one rounded part 123 and 0.0024; 333
-// rows of 2824 by 1001 in f16 29 and 24).  Experts' 4-bit weights with one scale a row are
+// rows of 2824 by 1001 in f16 25.6 and 23.9).  Experts' 4-bit weights with one scale a row are
 // taken as one group.
 #pragma once
 
@@ -47,24 +47,27 @@ struct HeldScales<0> {};
 // A power of two that brings the largest finite |scale| of a range to at most 65504 /
 // 128, the largest f16 by the largest code, and above half of that: a code of -128 stays
 // finite, and f16 products of code and scale are normal numbers for scales down to 2^-21
-// of the largest (bf16 has float's range and needs none).  Each group of THREADS threads
-// finds it for itself, in LDS of its own.
-template <class T, int THREADS, int UNROLL, class Scales>
-__device__ __forceinline__ void scale_window(Scales largest, int begin, int end, uint32_t *lds, float &to,
-                                             float &from) {
-    if constexpr (sizeof(typename T::elem) != 2 || __is_same(T, BF16)) {
+// of the largest (bf16 has float's range and needs none).
+__device__ __forceinline__ uint32_t finite_size(float scale) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, scale) & 0x7fffffffu;
+    return b < 0x7f800000u ? b : 0u;
+}
+// WAVES waves find it together, `which` of them being this one: m is the largest magnitude
+// that the wave's lanes have seen, lds a place for all of theirs.
+template <class T, int WAVES>
+__device__ __forceinline__ void scale_window(uint32_t m, int which, uint32_t *lds, float &to, float &from) {
+    if constexpr (__is_same(T, BF16)) {
         to = from = 1.0f;
     } else {
-        uint32_t m = 0;
-#pragma unroll UNROLL
-        for (int t = begin + (int)threadIdx.x % THREADS; t < end; t += THREADS) m = max(m, largest(t));
 #pragma unroll
         for (int d = 32; d; d >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d));
-        if ((threadIdx.x & 63) == 0) lds[threadIdx.x % THREADS >> 6] = m;
-        __syncthreads();
+        if constexpr (WAVES > 1) {
+            if ((threadIdx.x & 63) == 0) lds[which] = m;
+            __syncthreads();
 #pragma unroll
-        for (int w = 0; w < THREADS / 64; ++w) m = max(m, lds[w]);
-        __syncthreads();
+            for (int w = 0; w < WAVES; ++w) m = max(m, lds[w]);
+            __syncthreads();
+        }
         // exponents of to = 2^(8 - e) and its inverse, both normal (-118 <= e <= 128); a
         // mantissa past 65504 / 32768 = 1 + 0x7fe000 / 2^23 takes the next e
         const int e = max((int)(m >> 23) - 127 + ((m & 0x7fffffu) > 0x7fe000u), -118);
@@ -145,7 +148,7 @@ __device__ __forceinline__ void grad_product(GradArgs a, GroupArg groups, int sp
     constexpr int kCodeCopies = WB == 8 ? kCodes / (1024 * kWaves) : 0, kPCopies = COPY ? kP / (1024 * kWaves) : 0;
     constexpr int kCodeUnits = WB == 4 ? kCodes / (16 * kThreads) : 0, kPUnits = COPY ? 0 : kP / (16 * kThreads);
     constexpr int kCopies = kCodeCopies + kPCopies + (GS ? 0 : 1);   // a wave's copies of a step
-    constexpr int kSlots = TJ / 32, kScaleUnits = GS ? (64 * kSlots + kThreads - 1) / kThreads : 0;
+    constexpr int kScaleUnits = GS ? 1 : 0;   // a thread's scales of a step: a row's, of its wave's columns
     static_assert(!GS || (WB == 4 && !TRANSPOSED && FJ == 2));
     constexpr int kParts = GS ? 2 : 1;   // of a scale: products of a fragment of codes
     using elem = typename T::elem;
@@ -223,9 +226,10 @@ __device__ __forceinline__ void grad_product(GradArgs a, GroupArg groups, int sp
         u32x4_t p[kPUnits ? kPUnits : 1];
         [[no_unique_address]] HeldScales<kScaleUnits> scales;
     };
-    // The scale of row t for the columns of slot `slot` (32 each) of the tile.
-    const auto group_scale = [&](int t, int slot) {
-        const int64_t at = (int64_t)t * groups.pitch + group_of(groups, min(j0 / 32 + slot, (a.nj - 1) / 32));
+    // The scale of row t for the wave's 32 columns.
+    const int jrow0 = (wave / WI) * 16 * FJ, irow0 = (wave % WI) * FI * 16;
+    const auto group_scale = [&](int t) {
+        const int64_t at = (int64_t)t * groups.pitch + group_of(groups, min((j0 + jrow0) / 32, (a.nj - 1) / 32));
         return load_scale<GS ? GS : 4>(groups, at);
     };
     const int p_rows = TRANSPOSED ? t_end : a.ni, p_count = TRANSPOSED ? a.ni : t_end;   // p as it lies in memory
@@ -244,13 +248,8 @@ __device__ __forceinline__ void grad_product(GradArgs a, GroupArg groups, int sp
                 q.code[n] = *reinterpret_cast<const uint2 *>(a.b.codes + (int64_t)t * a.b.pitch + at);
             }
         }
-        if constexpr (GS > 0) {   // (where there are more threads than scales, some load one again)
-#pragma unroll
-            for (int n = 0; n < kScaleUnits; ++n) {
-                const int unit = n * kThreads + tid;
-                q.scales.q[n] = group_scale(min(s * 64 + (unit & 63), a.nt - 1), unit / 64 % kSlots);
-            }
-        }
+        // (waves of the same columns load the same scales, and write them to the same place)
+        if constexpr (GS > 0) q.scales.q[0] = group_scale(min(s * 64 + lane, a.nt - 1));
         if constexpr (!COPY) {
 #pragma unroll
             for (int n = 0; n < kPUnits; ++n) {
@@ -281,12 +280,8 @@ __device__ __forceinline__ void grad_product(GradArgs a, GroupArg groups, int sp
             }
         }
         if constexpr (GS > 0) {
-#pragma unroll
-            for (int n = 0; n < kScaleUnits; ++n) {
-                const int unit = n * kThreads + tid, t = unit & 63;
-                float *const at = reinterpret_cast<float *>(buf + kCodes + kP + unit / 64 % kSlots * 512) + t;
-                split_scale<T>(s * 64 + t < t_end ? scale_value<GS ? GS : 4>(groups, q.scales.q[n]) * to : 0.0f, at[0], at[64]);
-            }
+            float *const at = reinterpret_cast<float *>(buf + kCodes + kP + (jrow0 >> 5) * 512) + lane;
+            split_scale<T>(s * 64 + lane < t_end ? scale_value<GS ? GS : 4>(groups, q.scales.q[0]) * to : 0.0f, at[0], at[64]);
         }
         if constexpr (!COPY) {
 #pragma unroll
@@ -314,7 +309,6 @@ __device__ __forceinline__ void grad_product(GradArgs a, GroupArg groups, int sp
             }
         }
     };
-    const int jrow0 = (wave / WI) * 16 * FJ, irow0 = (wave % WI) * FI * 16;
     const int r = lane & 15, g = lane >> 4;
     f32x4 acc[FJ][FI];
 #pragma unroll
@@ -408,18 +402,24 @@ __device__ __forceinline__ void grad_product(GradArgs a, GroupArg groups, int sp
 #pragma unroll
         for (int m = 0; m < kStages - 1; ++m) fetch(s0 + m, units[m]);
     // (found while those are on their way; the last buffer is free until the first step)
-    const auto largest = [&](int t) {
+    if constexpr (GS > 0) {
+        // that of the wave's own 32 columns, which no other column's scale concerns: the waves
+        // of the same columns take 64 rows of t each in turn
+        constexpr int kSame = WI * KS, kDeep = 4;   // loads at once; past the end the last one again
+        const int which = group * WI + wave % WI;
         uint32_t m = 0;
+        if constexpr (!__is_same(T, BF16))
+            for (int t0 = begin * 64 + which * 64; t0 < t_end; t0 += 64 * kSame * kDeep)
 #pragma unroll
-        for (int n = 0; n < (GS ? kSlots : 1); ++n) {
-            const float v = GS ? scale_value<GS ? GS : 4>(groups, group_scale(t, n)) : a.b.scale[t];
-            const uint32_t b = __builtin_bit_cast(uint32_t, v) & 0x7fffffffu;
-            m = max(m, b < 0x7f800000u ? b : 0u);
-        }
-        return m;
-    };
-    scale_window<T, kThreads, GS ? 4 : 1>(largest, begin * 64, t_end, reinterpret_cast<uint32_t *>(smem + (kStages - 1) * kStage), to,
-                              from);
+                for (int n = 0; n < kDeep; ++n)
+                    m = max(m, finite_size(scale_value<GS>(groups, group_scale(min(t0 + n * 64 * kSame + lane, t_end - 1)))));
+        scale_window<T, kSame>(m, which, reinterpret_cast<uint32_t *>(all_smem + (kStages - 1) * kStage) + wave / WI * kSame, to, from);
+    } else {
+        uint32_t m = 0;
+        if constexpr (!__is_same(T, BF16))
+            for (int t = begin * 64 + tid; t < t_end; t += kThreads) m = max(m, finite_size(a.b.scale[t]));
+        scale_window<T, kWaves>(m, wave, reinterpret_cast<uint32_t *>(smem + (kStages - 1) * kStage), to, from);
+    }
     if constexpr (WB == 4) to *= 0.0625f;
     if constexpr (kFetches > 0) {
 #pragma unroll

@@ -84,10 +84,12 @@ def _near(got, want, tol):
     assert bool(ok.all()), f"{int((~ok).sum())} of {ok.numel()} off, worst {float(((got.double() - want).abs() / tol).max()):.3g}"
 
 
-def _case(L, m, c, k, experts, group, scales, dtype):
+def _case(L, m, c, k, experts, group, scales, dtype, factors=None):
     g = _gen(m + c + k + group)
     dy = torch.randn(m, k, generator=g, device="cuda").to(dtype)
     w, q = _weights(L, g, max(experts, 1) * k, c, group, scales)
+    if factors is not None:
+        w = w._replace(scale=w.scale * factors)
     ends = _split(m, experts)
     return dy, w, q, ends
 
@@ -104,3 +106,56 @@ def test_scales_keep_their_bits(L, m, c, k, experts, dtype):
         want, size = _expected(dy, _values(w, q), ends, k)
         _near(got, want, _tolerance(want, size, k, dtype))
         assert torch.equal(got, _run(L, dy, w, ends, experts, c))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("experts", [0, 3])
+def test_scales_at_the_edges(L, dtype, experts):
+    """Negative, zero and infinite scales, NaN, the largest float, and some whose first part
+    rounds up to the next power of two: what each reaches is what 32-bit products give it."""
+    m, c, k = 40, 256, 96
+    dy, w, q, ends = _case(L, m, c, k, experts, 32, torch.float32, dtype)
+    top = torch.finfo(torch.float32).max
+    w.scale[:, 0] = 0.0
+    w.scale[:, 1] *= -1
+    w.scale[3, 2], w.scale[4, 2] = 1.9999998, -1.99
+    w.scale[5, 3], w.scale[6, 4], w.scale[7, 5] = math.inf, math.nan, -math.inf
+    w.scale[8, 6] = top
+    if experts:   # (the same of every expert)
+        for e in range(1, experts):
+            w.scale[e * k:(e + 1) * k] = w.scale[:k]
+    got = _run(L, dy, w, ends, experts, c)
+    want, size = _expected(dy, _values(w, q), ends, k)
+    channels = torch.arange(c, device="cuda") // 32
+    plain = (channels <= 2) | (channels == 7)
+    _near(got[:, plain], want[:, plain], _tolerance(want, size, k, dtype)[:, plain])
+    assert not got[:, channels == 0].any()
+    # an infinite scale: infinities of one sign, NaN where the code (or dy) is zero; NaN everywhere
+    for group in (3, 4, 5):
+        a, b = got[:, channels == group], want[:, channels == group]
+        assert torch.equal(a.isnan(), b.isnan()) and torch.equal(a.isinf(), b.isinf())
+        assert bool((a[a.isinf()] > 0).eq(b[b.isinf()] > 0).all())
+    # the largest float: no NaN (a code above one takes it past 32 bits)
+    assert not got[:, channels == 6].isnan().any()
+
+
+@pytest.mark.parametrize("m,c,k,experts", SIZES)
+@pytest.mark.parametrize("group", [32, 64])
+def test_far_scales_leave_other_groups(L, m, c, k, experts, group):
+    """f16: a group of channels keeps its bits whatever the scales of the groups beside it,
+    as different columns of the result that they are."""
+    if c < 2 * group:
+        pytest.skip("one group")
+    groups = -(-c // group)
+    n = torch.arange(groups, device="cuda")
+    for factors in (torch.where(n % 3 == 1, 2.0 ** 14, 2.0 ** -10),           # 2^24 apart, all of f16's normal range
+                    torch.where(n % 3 == 1, 1e30, 1.0),                     # infinite results beside ordinary ones
+                    torch.where(n % 4 == 2, 1.0, 2.0 ** (3 + n % 2 * -20.0))):
+        dy, w, q, ends = _case(L, m, c, k, experts, group, torch.float32, torch.float16, factors)
+        got = _run(L, dy, w, ends, experts, c)
+        want, size = _expected(dy, _values(w, q), ends, k)
+        inside = (factors < 1e9)[torch.arange(c, device="cuda") // group]
+        fits = inside[None] & (want.abs() < 65000)
+        tol = _tolerance(want, size, k, torch.float16)
+        _near(got[fits], want[fits], tol[fits])
+        assert not got.isnan().any()
