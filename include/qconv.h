@@ -691,7 +691,8 @@ int qconv_linear_experts_grad_weight(const void *dy, int32_t dtype, int64_t lddy
  *   y[m][c] = h[m][c] r[m] gain[c]
  *   codes, scale: y as qconv_quantize_rows quantises its rows
  * The mean and r are formed in 64 bits and a code is the rounding of the 64-bit y (ties
- * to even), so it does not depend on the order of a sum.  A row in which an h or a y is
+ * to even; y formed as h gain / (mean + eps)^(1/2), so that a tie is met where the mean of
+ * squares is a 64-bit number), so it does not depend on the order of a sum.  A row in which an h or a y is
  * not a finite 32-bit float has scale NaN and codes 0; a row of zeros with eps == 0 is one.
  *   x, residual   DEVICE, m x c of `dtype`; ldx, ldr elements from row to row, to 2^21.
  *                 residual NULL: none

@@ -7,8 +7,12 @@
 // decide it: the sum of squares and r are formed in 64 bits, y in 32, and a y / 2^e
 // within 2^-14 of a half (32 bits are off by 127 * 3 * 2^-24 = 2^-15.4 at most) is formed
 // again in 64.  A row whose largest |y| lies that near to 127 * 2^e, or where 32 bits
-// leave their normal range, is done in 64 bits as a whole.  So codes are those of the
-// definition, whatever the order of the sums.
+// leave their normal range, is done in 64 bits as a whole.  What is still within 2^-30 of a
+// half or a border is h gain, exact, divided by (mean h^2 + eps)^(1/2), a quotient, a root
+// and a quotient again that are each rounded once: values that lie there in earnest are met
+// exactly wherever the mean of squares is a number of 64 bits (products with the
+// reciprocals of c and of the root missed half of those in rows of one magnitude).  So
+// codes are those of the definition, whatever the order of the sums.
 #include "qlinear_rows.h"
 
 namespace qconv {
@@ -45,8 +49,8 @@ __device__ __forceinline__ float wave_sum(float v) {
     return v;
 }
 
-// 1 / sqrt(x) to 64 bits: the instruction's 2^-26 or so, and two steps of Newton's method
-// (exact where the result is).
+// 1 / sqrt(x) to some 2^-52, for r: the instruction's 2^-26 or so, and two steps of Newton's
+// method.
 __device__ __forceinline__ double inverse_root(double x) {
     double y = __builtin_amdgcn_rsq(x);
 #pragma unroll
@@ -163,8 +167,11 @@ __global__ void __launch_bounds__(256, WAVES == 1 && KEEP < 4 ? 6 : 1) norm_to_r
     const bool narrow = squares != 0 ? !extreme(m) && !extreme(top) && (from_border < -16 || from_border > 16) && r > 0x1p-120f && r < 0x1p120f
                                      : m == 0 && r < 0x1p120f;
     float scale;
+    int e = -126;
+    uint32_t any = 0;      // values that are not finite floats
+    bool wide = !narrow;   // the lane's codes are to be quotients in 64 bits
     if (narrow) {
-        const int e = max((int)(top >> 23) - 6 + (from_border > 0), 1) - 127;
+        e = max((int)(top >> 23) - 6 + (from_border > 0), 1) - 127;
         scale = m == 0 ? 0.0f : __builtin_bit_cast(float, (uint32_t)(e + 127) << 23);
         const float inv = m == 0 ? 0.0f : r * __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);   // r / 2^e
         // Adding 1.5 * 2^23 rounds to a whole number, ties to even, and leaves its two's
@@ -182,8 +189,15 @@ __global__ void __launch_bounds__(256, WAVES == 1 && KEEP < 4 ? 6 : 1) norm_to_r
             if (worst > 0.5f - 0x1p-14f) {
                 float h[8], g[8];
                 again(at, h, g);
+                // (products are off by 2^-42 at most; a quotient takes ten times as long)
+                double near = 0;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) q[i] = (uint32_t)round_wide((double)h[i] * r_wide * (double)g[i], e);
+                for (int i = 0; i < 8; ++i) {
+                    const double t = __builtin_ldexp((double)h[i] * (double)g[i] * r_wide, -e), b = __builtin_rint(t);
+                    near = __builtin_fmax(near, __builtin_fabs(t - b));
+                    q[i] = (uint32_t)(int)b;
+                }
+                wide = wide || near > 0.5 - 0x1p-30;
             }
             put(at, q);
         };
@@ -197,6 +211,7 @@ __global__ void __launch_bounds__(256, WAVES == 1 && KEEP < 4 ? 6 : 1) norm_to_r
             round8(at, h);
         }
     } else {
+        const double root = __builtin_sqrt(squares / (double)a.c + a.eps);
         double most_wide = 0;
         bool bad = false;
         for (int at = at0; at < c; at += kNext) {
@@ -204,7 +219,7 @@ __global__ void __launch_bounds__(256, WAVES == 1 && KEEP < 4 ? 6 : 1) norm_to_r
             again(at, h, g);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const double y = __builtin_fabs((double)h[i] * r_wide * (double)g[i]);
+                const double y = __builtin_fabs((double)h[i] * (double)g[i] / root);
                 bad = bad || !(y <= (double)__FLT_MAX__);   // (a NaN too)
                 most_wide = y > most_wide ? y : most_wide;
             }
@@ -214,7 +229,7 @@ __global__ void __launch_bounds__(256, WAVES == 1 && KEEP < 4 ? 6 : 1) norm_to_r
             const double other = __shfl_xor(most_wide, d);
             most_wide = other > most_wide ? other : most_wide;
         }
-        uint32_t any = __any(bad) ? 1u : 0u;
+        any = __any(bad) ? 1u : 0u;
         if constexpr (WAVES > 1) {
             __syncthreads();   // the sums before have been read
             if (lane == 0) part[wave] = most_wide, most[wave] = any;
@@ -225,18 +240,20 @@ __global__ void __launch_bounds__(256, WAVES == 1 && KEEP < 4 ? 6 : 1) norm_to_r
                 any |= most[w];
             }
         }
-        int e = -126;
         if (most_wide > 0 && !any) {
             const int p = (int)(__builtin_bit_cast(uint64_t, most_wide) >> 52) - 1023;
             e = max(p - 6 + (most_wide > 127.0 * __builtin_ldexp(1.0, p - 6)), -126);
         }
         scale = any ? __builtin_nanf("") : most_wide == 0 ? 0.0f : __builtin_ldexpf(1.0f, e);
+    }
+    if (wide) {
+        const double root = __builtin_sqrt(squares / (double)a.c + a.eps);
         for (int at = at0; at < whole; at += kNext) {
             float h[8], g[8];
             again(at, h, g);
             uint32_t q[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) q[i] = any ? 0u : (uint32_t)round_wide((double)h[i] * r_wide * (double)g[i], e);
+            for (int i = 0; i < 8; ++i) q[i] = any ? 0u : (uint32_t)round_wide((double)h[i] * (double)g[i] / root, e);
             put(at, q);
         }
     }
