@@ -633,8 +633,8 @@ int qconv_linear_grad_weight(const void *dy, int32_t dtype, int64_t lddy, int32_
  * of the groups, and x's scale multiplies that.
  * qconv_linear_groups_grad_input -- qconv_linear_grad_input by such weights; workspace
  * as there (qconv_linear_grad_workspace_bytes of m, w->channels, w->rows).  A scale is not
- * rounded: it enters the products as the sum of two parts, which are exact for bf16 and f16
- * scales and leave 2^-13 (bf16) or 2^-19 (f16 gradients) of a product at most for 32-bit ones
+ * rounded: it enters the products as the sum of two parts, which are exact for scales of dy's
+ * type and leave 2^-12 (bf16) or 2^-18 (f16 gradients) of a product at most for longer ones
  * (f16: of scales no more than 2^14 times smaller than the same group's largest; a group's
  * columns do not depend on other groups' scales).
  * Rules, limits and errors as of qconv_linear and qconv_linear_grad_input.

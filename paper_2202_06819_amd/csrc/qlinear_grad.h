@@ -14,12 +14,12 @@
 //
 // Scales of groups (GS) are seldom powers of two, so there a scale enters as the sum of two
 // parts: the first of as few bits as leave a 4-bit code times it exact in the 16-bit type,
-// the second what is left, and each takes a product of its own.  bf16 and f16 scales lose
-// nothing (f16 ones in a bf16 gradient: 11 bits are 5 and 5 and a sign); of 32-bit scales
-// the second product's rounding is 2^-13 of a product in bf16, 2^-19 in f16, at most.  So a
-// gradient is as far from 64 bits as 32-bit products are, at twice the matrix instructions
-// (4096 x 4096 x 4096 in bf16 189 us, 0.0017 off; with one rounded part 123 and 0.0024; 333
-// rows of 2824 by 1001 in f16 25.6 and 23.9).  Experts' 4-bit weights with one scale a row are
+// the second what is left, and each takes a product of its own.  Scales of the gradient's
+// own type lose nothing; of longer ones the second product's rounding is 2^-12 of a product
+// in bf16, 2^-18 in f16, at most (the rest is 2^-4 and 2^-7 of the scale).  So a gradient
+// is as far from 64 bits as 32-bit products are, at twice the matrix instructions
+// (4096 x 4096 x 4096 in bf16 191 us, 0.0017 off; with one rounded part 123 and 0.0024; 333
+// rows of 2824 by 1001 in f16 26.0 and 23.9).  Experts' 4-bit weights with one scale a row are
 // taken as one group.
 #pragma once
 
@@ -122,16 +122,19 @@ __device__ __forceinline__ uint32_t scaled_pair(uint32_t w, int half, float s0, 
     return pack2<T>((float)(int8_t)(w >> (16 * half)) * s0, (float)(int8_t)(w >> (16 * half + 8)) * s1);
 }
 
-// A scale as two parts that add up to it: the nearest number of 5 (bf16) or 8 (f16) bits,
-// which a 4-bit code leaves exact in the 16-bit type, and the rest.  (One that is not
-// finite, or that would round past the largest float, has its own bits or their first ones.)
+// A scale as two parts that add up to it: its first 5 (bf16) or 8 (f16) bits, which a 4-bit
+// code leaves exact in the 16-bit type, and the rest.  Where the rest is nothing, or would
+// vanish in 16 bits, the first part is taken one unit nearer to zero: the parts then have
+// the same sign and neither is zero, so that an infinity in p meets no product of its own
+// with zero, nor one of the other sign.  (A scale that is not finite is both parts for the
+// same reason.)
 template <class T>
 __device__ __forceinline__ void split_scale(float s, float &first, float &rest) {
-    constexpr uint32_t kHalf = __is_same(T, BF16) ? 0x40000u : 0x8000u, kKept = ~(2 * kHalf - 1);
-    const uint32_t b = __builtin_bit_cast(uint32_t, s), up = b + kHalf;
-    const bool finite = (b & 0x7f800000u) != 0x7f800000u, fits = (up & 0x7f800000u) != 0x7f800000u;
-    first = __builtin_bit_cast(float, finite ? (fits ? up : b) & kKept : b);
-    rest = finite ? s - first : 0.0f;
+    constexpr uint32_t kUnit = __is_same(T, BF16) ? 0x80000u : 0x10000u;   // the first part's last bit
+    const uint32_t b = __builtin_bit_cast(uint32_t, s), size = b & 0x7fffffffu, low = b & (kUnit - 1);
+    const bool finite = size < 0x7f800000u, normal = finite && size >= 0x00800000u;
+    first = normal ? __builtin_bit_cast(float, b - low - (low < kUnit / 64 ? kUnit : 0)) : s;
+    rest = finite ? s - first : s;
 }
 
 //

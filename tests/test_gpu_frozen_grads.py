@@ -3,8 +3,8 @@ weights of experts with one scale a row, of any values.
 
 Tolerances follow from the roundings alone.  A scale enters the product as two parts, the
 first of so few bits that a code times it is exact in the 16-bit type; the second is at most
-2^-5 (bf16) or 2^-8 (f16) of the scale, and a code times it is rounded once, half an ulp:
-2^-13 and 2^-19 of a product.  Twice as many products as the sum has terms are added in 32
+1 + 2^-6 times 2^-4 (bf16) or 2^-7 (f16) of the scale, and a code times it is rounded once,
+half an ulp: 2^-12 and 2^-18 of a product, and 2^-6 of that.  Twice as many products as the sum has terms are added in 32
 bits, each with an error of at most 2^-24 of the sum of their absolute values, and the
 result is rounded once, half an ulp."""
 import math
@@ -15,7 +15,7 @@ import torch
 pytestmark = pytest.mark.gpu
 
 HALF_ULP = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
-PARTS = {torch.bfloat16: 2.0 ** -13, torch.float16: 2.0 ** -19}
+PARTS = {torch.bfloat16: 2.0 ** -12 * (1 + 2.0 ** -6), torch.float16: 2.0 ** -18 * (1 + 2.0 ** -6)}
 DTYPES = (torch.bfloat16, torch.float16)
 SCALES = (torch.float16, torch.bfloat16, torch.float32)
 
@@ -137,6 +137,32 @@ def test_scales_at_the_edges(L, dtype, experts):
         assert bool((a[a.isinf()] > 0).eq(b[b.isinf()] > 0).all())
     # the largest float: no NaN (a code above one takes it past 32 bits)
     assert not got[:, channels == 6].isnan().any()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("scales", ["any", "five bits", "powers of two"])
+@pytest.mark.parametrize("m,c,k,experts", SIZES)
+def test_infinite_gradients(L, m, c, k, experts, scales, dtype):
+    """An infinity in dy gives infinities of the weights' signs, NaN where the weight is zero
+    or another infinity meets it, and nothing in other rows, whatever parts a scale has."""
+    dy, w, q, ends = _case(L, m, c, k, experts, 32, torch.float32, dtype)
+    if scales == "five bits":
+        w = w._replace(scale=(w.scale * 1024).round().clamp(1, 31) / 1024)
+    elif scales == "powers of two":
+        w = w._replace(scale=torch.exp2(torch.log2(w.scale).round()))
+    clean = _run(L, dy, w, ends, experts, c)
+    hit = torch.zeros(m, dtype=torch.bool, device="cuda")
+    for n, row in enumerate(range(0, m, max(m // 9, 1))):
+        dy[row, (row * 7) % k] = math.inf if n % 2 else -math.inf
+        if n % 4 == 3:
+            dy[row, (row * 7 + k // 2) % k] = math.inf
+        hit[row] = True
+    got = _run(L, dy, w, ends, experts, c)
+    want, _ = _expected(dy, _values(w, q), ends, k)
+    assert torch.equal(got[~hit], clean[~hit])
+    a, b = got[hit], want[hit]
+    assert torch.equal(a.isnan(), b.isnan()) and torch.equal(a.isinf(), b.isinf())
+    assert torch.equal(a[a.isinf()] > 0, b[b.isinf()] > 0) and not torch.isfinite(a).any()
 
 
 @pytest.mark.parametrize("m,c,k,experts", SIZES)
