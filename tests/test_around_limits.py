@@ -67,12 +67,13 @@ def test_products_are_refused_for_their_tiles_alone(tmp):
                 for experts in (0, 1, 3, 512, 4096):
                     if k * max(experts, 1) > 1 << 22 or (op == "grad_weight" and not experts):
                         continue
-                    for group in (0, 64):
-                        if (op == "grad_weight" and group) or not (group or experts):
+                    for bits, group in ((8, 0), (4, 0), (4, 64)):
+                        if (op == "grad_weight" and bits == 4) or not (group or experts):
                             continue
-                        steps.append(dict(op=op, m=m, c=c, k=k, bits=4, group=group, experts=experts))
+                        steps.append(dict(op=op, m=m, c=c, k=k, bits=bits, group=group, experts=experts))
                         want.append(_too_large(op, m, c, k, experts))
     assert any(want) and not all(want)
     for step, refused, (status, events) in zip(steps, want, record(tmp, steps)["events"]):
         assert status == (-2 if refused else 0), step
-        assert bool([e for e in events if e[0] == "launch"]) == (not refused), step
+        grids = [list(map(int, e[3].split())) for e in events if e[0] == "launch"]
+        assert bool(grids) == (not refused) and all(y <= 65535 and z == 1 for _, y, z in grids), step
