@@ -19,7 +19,7 @@
 // in bf16, 2^-18 in f16, at most (the rest is 2^-4 and 2^-7 of the scale).  So a gradient
 // is as far from 64 bits as 32-bit products are, at twice the matrix instructions
 // (4096 x 4096 x 4096 in bf16 191 us, 0.0017 off; with one rounded part 123 and 0.0024; 333
-// rows of 2824 by 1001 in f16 26.0 and 23.9).  Experts' 4-bit weights with one scale a row are
+// rows of 2824 by 1001 in f16 25.4 and 24.1).  Experts' 4-bit weights with one scale a row are
 // taken as one group.
 #pragma once
 
@@ -333,13 +333,19 @@ __device__ __forceinline__ void grad_product(GradArgs a, GroupArg groups, int sp
     };
     struct Codes {
         i32x2 q[FJ];
-        f32x4 scale[2 * kParts];
+        f32x4 scale[kParts][2];
+    };
+    // In tiles of 64 the scales' second parts are read and used after the first ones (14
+    // registers of 128 spilled otherwise, in f16), in larger ones beside them.
+    constexpr bool kLate = TJ == 64;
+    auto read_scales = [&](const uint8_t *buf, int ks, int part, f32x4 (&s)[2]) {
+        const float *sc = reinterpret_cast<const float *>(buf + kCodes + kP + (GS ? (jrow0 >> 5) * 512 : 0)) + part * 64 + ks * 32 + g * 8;
+        s[0] = *reinterpret_cast<const f32x4 *>(sc);
+        s[1] = *reinterpret_cast<const f32x4 *>(sc + 4);
     };
     auto read_codes = [&](const uint8_t *buf, int ks) {
         Codes c;
-        const float *sc = reinterpret_cast<const float *>(buf + kCodes + kP + (GS ? (jrow0 >> 5) * 512 : 0)) + ks * 32 + g * 8;
-#pragma unroll
-        for (int n = 0; n < 2 * kParts; ++n) c.scale[n] = *reinterpret_cast<const f32x4 *>(sc + (n >> 1) * 64 + (n & 1) * 4);
+        read_scales(buf, ks, 0, c.scale[0]);
         const int t = ks * 32 + g * 8 + (r >> 1);
 #pragma unroll
         for (int f = 0; f < FJ; ++f)
@@ -349,7 +355,7 @@ __device__ __forceinline__ void grad_product(GradArgs a, GroupArg groups, int sp
     };
     // Pair n (0..3) of a fragment's eight codes, times part `part` of their scales.
     auto pair_of = [&](const Codes &c, int f, int n, int part) {
-        const f32x4 s = c.scale[part * 2 + (n >> 1)];
+        const f32x4 s = c.scale[part][n >> 1];
         return scaled_pair<T>((uint32_t)c.q[f][n >> 1], n & 1, GS ? s[(n & 1) * 2] : s[(n & 1) * 2] * to,
                               GS ? s[(n & 1) * 2 + 1] : s[(n & 1) * 2 + 1] * to);
     };
@@ -365,13 +371,15 @@ __device__ __forceinline__ void grad_product(GradArgs a, GroupArg groups, int sp
         v8 y[FI + kAhead];
 #pragma unroll
         for (int f = 0; f < kAhead; ++f) y[f] = ahead[f];
-        const Codes c = read_codes(then, ks ^ 1);
+        Codes c = read_codes(then, ks ^ 1);
         u32x4_t next[kParts * FJ];
 #pragma unroll
         for (int i = 0; i < FI; ++i) {
             const int f = i + kAhead;
             y[f] = f < FI ? read_p(cur, ks, f) : read_p(then, ks ^ 1, f - FI);
             spread(i);
+            constexpr int kRest = kLate ? FI - 1 : 0;
+            if (kParts > 1 && i == kRest) read_scales(then, ks ^ 1, kParts - 1, c.scale[kParts - 1]);
 #pragma unroll
             for (int n = kParts * FJ - 1; n >= 0; --n) {   // (the small products first)
                 const int j = FJ - 1 - n % FJ, part = n / FJ;
@@ -382,7 +390,8 @@ __device__ __forceinline__ void grad_product(GradArgs a, GroupArg groups, int sp
 #pragma unroll
             for (int n = (i - kFirst) * kPairs / kGroups; n < (i - kFirst + 1) * kPairs / kGroups; ++n) {
                 if (n < 0 || i < kFirst) continue;
-                const int part = n % kParts, pair = n / kParts, k = part * FJ + (pair >> 2);
+                const int part = kLate ? n / (4 * FJ) : n % kParts, pair = kLate ? n % (4 * FJ) : n / kParts;
+                const int k = part * FJ + (pair >> 2);
                 next[k][pair & 3] = pair_of(c, pair >> 2, pair & 3, part);
                 asm volatile("" : "+v"(next[k][pair & 3]));   // here, not where the value is next used
             }
@@ -439,7 +448,8 @@ __device__ __forceinline__ void grad_product(GradArgs a, GroupArg groups, int sp
     u32x4_t x[kParts * FJ];
     v8 ahead[kAhead];
     {
-        const Codes c = read_codes(smem, 0);
+        Codes c = read_codes(smem, 0);
+        if (kParts > 1) read_scales(smem, 0, kParts - 1, c.scale[kParts - 1]);
 #pragma unroll
         for (int f = 0; f < kParts * FJ; ++f)
 #pragma unroll
